@@ -393,6 +393,101 @@ int rfast_diagnostics_static(rfast_ctx* ctx, const float* d_xstar, double* d_out
 int rfast_profile_enable(rfast_ctx* ctx, int32_t on);
 int rfast_kernel_time(rfast_ctx* ctx, int32_t which, double* ms_sum, int64_t* launches);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators of one training or serving step, for programs that hold their own tensors.  They take no context:
+ * everything comes with the call, work is enqueued on hip_stream (NULL = the null stream) and nothing is allocated, copied to
+ * the host or waited for, so that a call can be captured into a HIP graph.  Two calls may overlap on different streams if
+ * they share neither workspace nor outputs.  What is written must not overlap what is read unless the text says so.  Tensors
+ * may begin at any address that is a multiple of their element's size; a matrix has its rows `ld` elements apart.
+ * Errors: a negative rfast_status; rfast_last_error(NULL) gives the text (of the calling thread's last failure). */
+typedef enum rfast_type { RFAST_F32 = 0, RFAST_BF16 = 1 } rfast_type;
+
+/* Softmax cross-entropy of `rows` rows of K logits with its gradient, in one pass over the logits:
+ *   lse = log sum_k exp(l_k),  loss = lse - l_label,  grad_k = grad_scale (exp(l_k - lse) - [k == label]).
+ * logits: device, type logits_type, ld_logits >= K.  labels: device int32 [rows]; a row whose label lies outside [0, K) (-1 by
+ * convention) is padding: loss 0, gradient 0, whatever its logits.  loss: device fp32 [rows] (NULL: not wanted).  lse: device
+ * fp32 [rows] (NULL: not wanted).  grad: device, type grad_type, ld_grad >= K (NULL: not wanted); may be the logits themselves
+ * if the types and the distances of rows are the same.  d_rows: device int32 [1] or NULL; only the first
+ * min(*d_rows, rows) rows are touched, the others stay as they were.
+ * A logit of -infinity is a class that is masked out: probability and gradient 0.  A row that is masked out entirely has no
+ * distribution: lse -infinity, loss and gradient 0.  A label at a masked class of another row: loss +infinity, gradient as above.
+ * A logit that is NaN or +infinity makes its row's loss, lse and gradient NaN.
+ * Sums and exponentials are in 32 bits. */
+int rfast_softmax_xent(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits,
+                       const int32_t* labels, float grad_scale, float* loss, float* lse, void* grad, int32_t grad_type,
+                       int64_t ld_grad, const int32_t* d_rows, void* hip_stream);
+
+/* Low-rank adapters of many requests, nodes or tenants beside one shared projection W:
+ *   y_t = W x_t + scale B_a A_a x_t,   a = the adapter of row t's segment.
+ * x: bf16 [rows][ld_x >= d].  W: bf16 [K][d].  A: bf16 [adapters][rank][d].  B: bf16 [adapters][K][rank] (contiguous).
+ * Row t belongs to segment s with row_ptr[s] <= t < row_ptr[s+1] (device int32 [segments+1], ascending from row_ptr[0] = 0; a
+ * segment may be empty).  Rows from row_ptr[segments] on belong to nobody: nothing of them is written (`rows` is what
+ * the tensors hold; numbers outside [0, rows] count as its ends, and with numbers out of order it is not said whose a row is).  Segment s has the
+ * adapter adapter[s] (device int32 [segments]; NULL: adapter s); segments may share one, and a number outside
+ * [0, adapters) means none: W alone. */
+typedef struct rfast_lora_shape {
+  int32_t rows, segments, adapters;
+  int32_t d, K, rank;        /* features, outputs, rank (1 .. 64) */
+  int64_t ld_x, ld_y;        /* of x and dx; of y and dy          */
+  int32_t y_type;            /* forward: rfast_type of y; backward: RFAST_BF16 (dy) */
+  float scale;
+} rfast_lora_shape;
+/* Device workspace in bytes (pure function; 0 if a size is out of range).  pass 0: rfast_lora_forward, 1: rfast_lora_backward
+ * without dx, 2: with dx. */
+size_t rfast_lora_workspace_bytes(const rfast_lora_shape* shape, int32_t pass);
+/* y: y_type [rows][ld_y >= K].  Products of bf16 are summed in 32 bits, and A_a x_t, which the second product reads, keeps its
+ * 24 bits (as three bf16), so that a y of 32 bits is as good as one computed in 32 bits.
+ * workspace: device, 256-byte aligned, contents arbitrary and not kept from one call to the next. */
+int rfast_lora_forward(const rfast_lora_shape* shape, const void* x, const void* W, const void* A, const void* B,
+                       const int32_t* row_ptr, const int32_t* adapter, void* y, void* workspace, size_t workspace_bytes,
+                       void* hip_stream);
+/* Gradients from dy (bf16 [rows][ld_y >= K]), W frozen:
+ *   e_t = scale B_a^T dy_t,   dA_a = sum_t e_t x_t^T,   dB_a = scale sum_t dy_t (A_a x_t)^T,   dx_t = W^T dy_t + A_a^T e_t.
+ * dA fp32 [adapters][rank][d], dB fp32 [adapters][K][rank]: sums over all segments of an adapter, zero where it has no row, in an
+ * order that the sizes alone decide (the same call gives the same bits).  dx: bf16 [rows][ld_x] or NULL. */
+int rfast_lora_backward(const rfast_lora_shape* shape, const void* x, const void* W, const void* A, const void* B,
+                        const int32_t* row_ptr, const int32_t* adapter, const void* dy, void* dx, float* dA, float* dB,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* AdamW over many tensors with one launch.  Of a tensor with t steps before this one, elementwise in 32 bits:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - gamma weight_decay) p - (gamma / (1 - beta1^(t+1))) m / (sqrt(v) / sqrt(1 - beta2^(t+1)) + eps).
+ * state_bits 32: m and v are fp32.  state_bits 8: m and sqrt(v) are held as 8-bit floats (e4m3) with an fp32 scale for every 256
+ * coordinates counted from the tensor's first, largest magnitude / 448; the step itself uses the unrounded ones.  The root, whose
+ * range is half that of v, is never rounded to zero: one that is not zero is held as the smallest code at least, so that no coordinate with a
+ * momentum meets a vanished denominator.  A moment that is not finite is held as NaN and counts for no scale. */
+typedef struct rfast_adamw rfast_adamw;
+typedef struct rfast_adamw_tensor {
+  void* param;             /* device, param_type [count], updated                                              */
+  const void* grad;        /* device, grad_type [count]                                                        */
+  void* m;                 /* device, fp32 [count] or codes uint8 [count]                                      */
+  void* v;                 /* device, fp32 [count] (v) or codes uint8 [count] (of sqrt(v))                     */
+  float* m_scale;          /* device, fp32 [ceil(count / 256)]; state_bits 32: NULL                            */
+  float* v_scale;
+  void* copy;              /* device, bf16 [count] that receives the new parameters rounded, or NULL            */
+  int64_t count;           /* 0 and more                                                                       */
+  double weight_decay;
+  int64_t steps;           /* steps this tensor has taken so far                                               */
+} rfast_adamw_tensor;
+typedef struct rfast_adamw_options {
+  int32_t param_type, grad_type, state_bits;
+  double beta1, beta2, eps;  /* [0, 1), [0, 1), > 0; in double, as 1 - beta2 would lose digits */
+} rfast_adamw_options;
+/* Device workspace in bytes for these counts (0 if one is out of range).  tensors: HOST array; of it only `count` is read. */
+size_t rfast_adamw_workspace_bytes(int32_t tensors, const rfast_adamw_tensor* host_tensors);
+/* Uploads the table of tensors (waits for the stream).  Memory that a step writes may not overlap another tensor's (RFAST_EINVAL).
+ * The tensors and the workspace (256-byte aligned) stay the caller's and must outlive the handle. */
+int rfast_adamw_create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* host_tensors,
+                       const rfast_adamw_options* options, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+/* One step with step size gamma.  d_active: device uint8 [tensors] or NULL (all): tensors whose flag is zero keep parameters,
+ * moments and counter.  The counters live on the device, so a captured step counts on with every replay; steps of one handle
+ * must be ordered by the caller. */
+int rfast_adamw_step(rfast_adamw* h, double gamma, const uint8_t* d_active, void* hip_stream);
+/* Waits for the stream; steps of every tensor, HOST int32 [tensors]. */
+int rfast_adamw_steps(rfast_adamw* h, int32_t* host_steps, void* hip_stream);
+int rfast_adamw_set_steps(rfast_adamw* h, const int32_t* host_steps, void* hip_stream);
+void rfast_adamw_destroy(rfast_adamw* h);
+
 const char* rfast_last_error(const rfast_ctx* ctx);
 void rfast_destroy(rfast_ctx* ctx);
 

@@ -28,6 +28,22 @@ class RfastDiag(C.Structure):
                                            "loss_at_xbar")]
 
 
+class RfastLoraShape(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("segments", C.c_int32), ("adapters", C.c_int32), ("d", C.c_int32), ("K", C.c_int32),
+                ("rank", C.c_int32), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("y_type", C.c_int32), ("scale", C.c_float)]
+
+
+class RfastAdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64), ("weight_decay", C.c_double),
+                ("steps", C.c_int64)]
+
+
+class RfastAdamwOptions(C.Structure):
+    _fields_ = [("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32), ("beta1", C.c_double),
+                ("beta2", C.c_double), ("eps", C.c_double)]
+
+
 OBJECTIVES = {"diag_quadratic": 0, "least_squares": 1, "logistic": 2, "softmax_bf16": 3}
 RFAST_FIELDS = {"X": 0, "Z": 1, "G": 2, "V_RING": 3, "RHO_RING": 4, "RHO_TILDE": 5, "T_NODE": 6, "TAU_R": 7,
                 "TAU_C": 8, "SLOT_R": 9, "SLOT_C": 10, "ROUND": 11, "SIGMA_RING": 12, "DELIV_R": 13, "DELIV_C": 14,
@@ -35,7 +51,9 @@ RFAST_FIELDS = {"X": 0, "Z": 1, "G": 2, "V_RING": 3, "RHO_RING": 4, "RHO_TILDE":
                 "SCHED_DROP_C": 20, "SCHED_BATCH": 21, "MOMENTUM": 22}
 EXPORTS = ["rfast_common_roots", "rfast_workspace_bytes", "rfast_create", "rfast_init", "rfast_round", "rfast_run", "rfast_run_generated", "rfast_run_events", "rfast_use_graphs", "rfast_use_blocks", "rfast_block_info", "rfast_set_tile_group", "rfast_set_wait_limits", "rfast_sync_round", "rfast_sync_run", "rfast_rebase", "rfast_set_rebase_interval", "rfast_set_optimizer", "rfast_set_gamma_schedule", "rfast_check",
            "rfast_read_state", "rfast_write_state", "rfast_diagnostics", "rfast_diagnostics_static", "rfast_profile_enable", "rfast_kernel_time", "rfast_last_error",
-           "rfast_destroy"]
+           "rfast_destroy", "rfast_softmax_xent", "rfast_lora_workspace_bytes", "rfast_lora_forward", "rfast_lora_backward",
+           "rfast_adamw_workspace_bytes", "rfast_adamw_create", "rfast_adamw_step", "rfast_adamw_steps", "rfast_adamw_set_steps",
+           "rfast_adamw_destroy"]
 
 
 def lib():
@@ -104,6 +122,26 @@ def lib():
     L.rfast_last_error.argtypes = [vp]
     L.rfast_destroy.restype = None
     L.rfast_destroy.argtypes = [vp]
+    L.rfast_softmax_xent.restype = C.c_int
+    L.rfast_softmax_xent.argtypes = [i32, i32, vp, i32, i64, vp, C.c_float, vp, vp, vp, i32, i64, vp, vp]
+    L.rfast_lora_workspace_bytes.restype = sz
+    L.rfast_lora_workspace_bytes.argtypes = [C.POINTER(RfastLoraShape), i32]
+    L.rfast_lora_forward.restype = C.c_int
+    L.rfast_lora_forward.argtypes = [C.POINTER(RfastLoraShape)] + [vp] * 8 + [sz, vp]
+    L.rfast_lora_backward.restype = C.c_int
+    L.rfast_lora_backward.argtypes = [C.POINTER(RfastLoraShape)] + [vp] * 11 + [sz, vp]
+    L.rfast_adamw_workspace_bytes.restype = sz
+    L.rfast_adamw_workspace_bytes.argtypes = [i32, C.POINTER(RfastAdamwTensor)]
+    L.rfast_adamw_create.restype = C.c_int
+    L.rfast_adamw_create.argtypes = [C.POINTER(vp), i32, C.POINTER(RfastAdamwTensor), C.POINTER(RfastAdamwOptions), vp, sz, vp]
+    L.rfast_adamw_step.restype = C.c_int
+    L.rfast_adamw_step.argtypes = [vp, C.c_double, vp, vp]
+    L.rfast_adamw_steps.restype = C.c_int
+    L.rfast_adamw_steps.argtypes = [vp, vp, vp]
+    L.rfast_adamw_set_steps.restype = C.c_int
+    L.rfast_adamw_set_steps.argtypes = [vp, vp, vp]
+    L.rfast_adamw_destroy.restype = None
+    L.rfast_adamw_destroy.argtypes = [vp]
     _lib = L
     return L
 

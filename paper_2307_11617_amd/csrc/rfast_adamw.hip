@@ -1,0 +1,408 @@
+// AdamW over many tensors, moments in 32 bits or in 8.
+//
+// Elementwise; a coordinate in 32 bits moves 28 bytes (parameter, gradient, two moments in; all but the gradient out) for some 60
+// vector instructions, so the kernel is bound by memory where the tensors are large and by latency where they are small.
+//  - One launch for all tensors: the coordinates of every tensor are cut into chunks, and a table says whose a chunk is.  A
+//    workgroup takes chunks in strides of the grid.
+//  - 8 bits: a block of 256 coordinates, which share a scale, is one wavefront's four coordinates per lane, so the largest magnitude is
+//    found in registers and every byte is still moved once.
+//  - Counters of steps are on the device (a replayed graph has to count).  Every workgroup reads them, and the last one to finish moves
+//    them on; who is last is told by a word per group of workgroups and one for the groups, so that no word is hit by thousands.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "rfast_operators.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock = 256;                    // coordinates per scale
+constexpr int kSlice = kThreads / 64 * kBlock; // coordinates that the wavefronts of a workgroup take at a time
+constexpr int kGroups = 64;                    // words for workgroups that are through
+constexpr int kMostWorkgroups = 2048;          // eight per compute unit
+constexpr float kCodeMost = 448.f;             // largest finite e4m3
+constexpr float kCodeLeast = 0.001953125f;     // smallest e4m3 above zero, 2^-9
+constexpr size_t kAlign = 256;
+size_t up(size_t b) { return (b + kAlign - 1) / kAlign * kAlign; }
+
+struct Row {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  u16* copy;
+  int64_t count;
+  int64_t first;  // its first chunk
+  double decay;
+};
+
+struct Args {
+  const Row* rows;
+  const int32_t* whose;  // [chunks] tensor
+  int32_t* steps;        // [tensors]
+  unsigned* through;     // [kGroups * 16 + 1] workgroups that are through, 64 bytes apart
+  const uint8_t* active;
+  int32_t tensors, chunks;
+  double gamma, log_beta1, log_beta2;
+  float beta1, beta2, rest1, rest2, eps;  // rest = 1 - beta
+};
+
+// beta^t from log(beta) without the cancellation of 1 - beta^t
+__device__ inline double one_less_power(double log_beta, int t) { return -expm1((double)t * log_beta); }
+
+__device__ inline float finite_magnitude(float v) {
+  const float a = fabsf(v);
+  return a < INFINITY ? a : 0.f;  // false for NaN too
+}
+
+// Four values as e4m3 times scale; values that are not finite become NaN.
+__device__ inline uint32_t codes_of(const float* v, float inverse, bool root) {
+  float q[4];
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    q[j] = v[j] * inverse;
+    if (root && v[j] > 0.f) q[j] = fmaxf(q[j], kCodeLeast);
+    odd |= !(fabsf(v[j]) < INFINITY);
+  }
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+  if (odd) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (!(fabsf(v[j]) < INFINITY)) w |= 0x7F << (8 * j);
+  }
+  return (uint32_t)w;
+}
+__device__ inline void values_of(uint32_t w, float scale, float* v) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  v[0] = lo[0] * scale; v[1] = lo[1] * scale; v[2] = hi[0] * scale; v[3] = hi[1] * scale;
+}
+
+typedef unsigned int any_u32 __attribute__((aligned(1)));
+template <bool STREAM> __device__ inline uint32_t load_codes(const uint8_t* p, int64_t left) {
+  if (left >= 4) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const any_u32*>(p));
+    else return *reinterpret_cast<const any_u32*>(p);
+  }
+  uint32_t w = 0;
+  for (int j = 0; j < 4; ++j)
+    if (j < left) w |= (uint32_t)p[j] << (8 * j);
+  return w;
+}
+template <bool STREAM> __device__ inline void store_codes(uint8_t* p, int64_t left, uint32_t w) {
+  if (left >= 4) {
+    if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<any_u32*>(p));
+    else *reinterpret_cast<any_u32*>(p) = w;
+    return;
+  }
+  for (int j = 0; j < 4; ++j)
+    if (j < left) p[j] = (uint8_t)(w >> (8 * j));
+}
+
+// The moments of four coordinates of a row: read, moved on, written.  With 8 bits all 64 lanes of the wavefront have to come
+// along (they share the scale); lanes past the row's end have left <= 0.
+template <int BITS, bool STREAM> struct Moments {
+  float m[4], v[4];  // v: the root with 8 bits
+  uint32_t cm, cv;
+  float sm, sv;
+  __device__ void read(const void* pm, const void* pv, const float* ms, const float* vs, int64_t k, int64_t left) {
+    if constexpr (BITS == 32) {
+      if (left > 0) {
+        load_four<STREAM>((const float*)pm + k, left, m);
+        load_four<STREAM>((const float*)pv + k, left, v);
+      }
+    } else {
+      cm = cv = 0;
+      if (left > 0) {
+        cm = load_codes<STREAM>((const uint8_t*)pm + k, left);
+        cv = load_codes<STREAM>((const uint8_t*)pv + k, left);
+        sm = ms[k / kBlock];
+        sv = vs[k / kBlock];
+      }
+    }
+  }
+  // root: sqrt(v) after the step
+  __device__ void step(const float* g, float beta1, float rest1, float beta2, float rest2, float* root) {
+    if constexpr (BITS == 8) {
+      values_of(cm, sm, m);
+      values_of(cv, sv, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = m[j] * beta1 + g[j] * rest1;
+      v[j] = v[j] * beta2 + (g[j] * g[j]) * rest2;
+      root[j] = sqrtf(v[j]);
+    }
+  }
+  __device__ void write(void* pm, void* pv, float* ms, float* vs, int64_t k, int64_t left, const float* root) {
+    if constexpr (BITS == 32) {
+      if (left > 0) {
+        store_four<STREAM>((float*)pm + k, left, m);
+        store_four<STREAM>((float*)pv + k, left, v);
+      }
+    } else {
+      float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < left) {
+          top_m = fmaxf(top_m, finite_magnitude(m[j]));
+          top_v = fmaxf(top_v, finite_magnitude(root[j]));
+        }
+      top_m = wave_max(top_m);
+      top_v = wave_max(top_v);
+      if (left <= 0) return;
+      store_codes<STREAM>((uint8_t*)pm + k, left, codes_of(m, top_m > 0.f ? 1.f / top_m * kCodeMost : 0.f, false));
+      store_codes<STREAM>((uint8_t*)pv + k, left, codes_of(root, top_v > 0.f ? 1.f / top_v * kCodeMost : 0.f, true));
+      if (k % kBlock == 0) {
+        ms[k / kBlock] = top_m * (1.f / kCodeMost);
+        vs[k / kBlock] = top_v * (1.f / kCodeMost);
+      }
+    }
+  }
+};
+
+// U: slices of a chunk, whose loads are all under way before the first is used
+template <class P, class G, int BITS, int U, bool STREAM>
+__global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const int i = __builtin_amdgcn_readfirstlane(a.whose[chunk]);
+    if (a.active && a.active[i] == 0) continue;
+    const Row r = a.rows[i];
+    const int t = a.steps[i] + 1;
+    const int64_t k0 = (chunk - r.first) * (U * kSlice) + wave * kBlock + lane * 4;
+    Moments<BITS, STREAM> state[U];
+    float p[U][4], g[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + u * kSlice, left = r.count - k;
+      if (left > 0) {
+        load_four<STREAM>((const P*)r.param + k, left, p[u]);
+        load_four<STREAM>((const G*)r.grad + k, left, g[u]);
+      }
+      state[u].read(r.m, r.v, r.m_scale, r.v_scale, k, left);
+    }
+    const float first = (float)(a.gamma / one_less_power(a.log_beta1, t));
+    const float second = (float)(1.0 / sqrt(one_less_power(a.log_beta2, t)));
+    const float keep = (float)(1.0 - a.gamma * r.decay);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + u * kSlice, left = r.count - k;
+      float root[4];
+      state[u].step(g[u], a.beta1, a.rest1, a.beta2, a.rest2, root);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[u][j] = p[u][j] * keep - (state[u].m[j] * first) / (root[j] * second + a.eps);
+      if (left > 0) {
+        store_four<STREAM>((P*)r.param + k, left, p[u]);
+        if (r.copy) store_four<STREAM>(r.copy + k, left, p[u]);
+      }
+      state[u].write(r.m, r.v, r.m_scale, r.v_scale, k, left, root);
+    }
+  }
+  // The last workgroup moves the counters on.  (No workgroup reads them any more: each has read them before it counts itself.)
+  __shared__ bool last;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned group = blockIdx.x % kGroups;
+    const unsigned in_group = (gridDim.x - group + kGroups - 1) / kGroups, groups = gridDim.x < kGroups ? gridDim.x : kGroups;
+    last = false;
+    if (__hip_atomic_fetch_add(a.through + group * 16, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == in_group - 1) {
+      __hip_atomic_store(a.through + group * 16, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (__hip_atomic_fetch_add(a.through + kGroups * 16, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups - 1) {
+        __hip_atomic_store(a.through + kGroups * 16, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = true;
+      }
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  for (int i = threadIdx.x; i < a.tensors; i += kThreads)
+    if (!a.active || a.active[i] != 0) a.steps[i] += 1;
+}
+
+struct Layout {
+  size_t rows, whose, steps, through, total;
+};
+bool count_chunks(int32_t tensors, const rfast_adamw_tensor* t, int64_t slices, int64_t* chunks) {
+  *chunks = 0;
+  for (int32_t i = 0; i < tensors; ++i) {
+    if (t[i].count < 0 || t[i].count > (int64_t)1 << 46) return false;
+    *chunks += (t[i].count + slices * kSlice - 1) / (slices * kSlice);
+    if (*chunks > 0x7fffffff - kMostWorkgroups) return false;
+  }
+  return true;
+}
+Layout layout_of(int32_t tensors, int64_t chunks) {
+  Layout l;
+  l.rows = 0;
+  l.whose = up(l.rows + (size_t)tensors * sizeof(Row));
+  l.steps = up(l.whose + (size_t)chunks * 4);
+  l.through = up(l.steps + (size_t)tensors * 4);
+  l.total = up(l.through + (kGroups * 16 + 1) * 4);
+  return l;
+}
+// Slices per chunk: four keep enough bytes under way per wavefront, one spreads small tensors over the card.
+int64_t slices_for(int32_t tensors, const rfast_adamw_tensor* t, int64_t* chunks) {
+  if (!count_chunks(tensors, t, 4, chunks)) return 0;
+  if (*chunks >= 2 * kMostWorkgroups) return 4;
+  return count_chunks(tensors, t, 1, chunks) ? 1 : 0;
+}
+
+}  // namespace
+
+struct rfast_adamw {
+  Args a;
+  int param_type, grad_type, bits, slices;
+  bool stream;
+};
+
+namespace {
+
+template <class P, class G, int BITS> hipError_t launch(const rfast_adamw* h, const Args& a, hipStream_t s) {
+  const dim3 grid((unsigned)std::min(std::max(a.chunks, 1), kMostWorkgroups)), block(kThreads);
+  if (h->slices == 1) hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 1, false>), grid, block, 0, s, a);
+  else if (h->stream) hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 4, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 4, false>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+template <class P, class G> hipError_t launch(const rfast_adamw* h, const Args& a, hipStream_t s) {
+  return h->bits == 32 ? launch<P, G, 32>(h, a, s) : launch<P, G, 8>(h, a, s);
+}
+
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+
+int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, const rfast_adamw_options* o, void* d_workspace,
+           size_t workspace_bytes, hipStream_t stream) {
+  if (!t || !o || !d_workspace) return rfast_refuse(RFAST_EINVAL, "NULL argument");
+  if (tensors < 1) return rfast_refuse(RFAST_EINVAL, "need at least one tensor");
+  if ((o->param_type != RFAST_F32 && o->param_type != RFAST_BF16) || (o->grad_type != RFAST_F32 && o->grad_type != RFAST_BF16))
+    return rfast_refuse(RFAST_EINVAL, "param_type and grad_type must be RFAST_F32 or RFAST_BF16");
+  if (o->state_bits != 8 && o->state_bits != 32) return rfast_refuse(RFAST_EINVAL, "state_bits must be 8 or 32");
+  if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1)) return rfast_refuse(RFAST_ERANGE, "beta1 and beta2 must lie in [0, 1)");
+  if (!(o->eps > 0 && o->eps < 1e30)) return rfast_refuse(RFAST_ERANGE, "eps must be positive and finite");
+  if (!aligned(d_workspace, kAlign)) return rfast_refuse(RFAST_EINVAL, "workspace must be 256-byte aligned");
+  int64_t chunks;
+  const int64_t slices = slices_for(tensors, t, &chunks);
+  if (slices == 0) return rfast_refuse(RFAST_EINVAL, "a tensor's count is out of range");
+  const Layout l = layout_of(tensors, chunks);
+  if (workspace_bytes < l.total) return rfast_refuse(RFAST_ENOMEM, "workspace too small");
+  const size_t pw = o->param_type == RFAST_F32 ? 4 : 2, gw = o->grad_type == RFAST_F32 ? 4 : 2, sw = o->state_bits == 32 ? 4 : 1;
+  std::vector<Row> rows((size_t)tensors);
+  std::vector<int32_t> whose((size_t)chunks), steps((size_t)tensors);
+  struct Span { uintptr_t at, end; bool written; };
+  std::vector<Span> spans{{(uintptr_t)d_workspace, (uintptr_t)d_workspace + l.total, true}};
+  int64_t first = 0, bytes = 0;
+  for (int32_t i = 0; i < tensors; ++i) {
+    const rfast_adamw_tensor& q = t[i];
+    const std::string who = "tensor " + std::to_string(i) + ": ";
+    if (!(q.weight_decay >= 0 && q.weight_decay < 1e30)) return rfast_refuse(RFAST_ERANGE, who + "weight_decay must be finite and >= 0");
+    if (q.steps < 0 || q.steps > 0x7ffffffe) return rfast_refuse(RFAST_ERANGE, who + "steps out of range");
+    steps[i] = (int32_t)q.steps;
+    rows[i] = {q.param, q.grad, q.m, q.v, q.m_scale, q.v_scale, (u16*)q.copy, q.count, first, q.weight_decay};
+    const int64_t n = (q.count + slices * kSlice - 1) / (slices * kSlice);
+    std::fill(whose.begin() + first, whose.begin() + first + n, i);
+    first += n;
+    if (q.count == 0) continue;
+    if (!q.param || !q.grad || !q.m || !q.v) return rfast_refuse(RFAST_EINVAL, who + "NULL pointer");
+    if (o->state_bits == 8 ? !q.m_scale || !q.v_scale : q.m_scale || q.v_scale)
+      return rfast_refuse(RFAST_EINVAL, who + "scales are needed with states in 8 bits, and only there");
+    if (!aligned(q.param, pw) || !aligned(q.grad, gw) || !aligned(q.m, sw) || !aligned(q.v, sw) || !aligned(q.m_scale, 4) ||
+        !aligned(q.v_scale, 4) || !aligned(q.copy, 2))
+      return rfast_refuse(RFAST_EINVAL, who + "an address is no multiple of its element's size");
+    const size_t count = (size_t)q.count, blocks = (count + kBlock - 1) / kBlock;
+    auto span = [&](const void* p, size_t len, bool written) {
+      if (p) spans.push_back({(uintptr_t)p, (uintptr_t)p + len, written});
+    };
+    span(q.param, count * pw, true); span(q.grad, count * gw, false); span(q.m, count * sw, true); span(q.v, count * sw, true);
+    span(q.m_scale, blocks * 4, true); span(q.v_scale, blocks * 4, true); span(q.copy, count * 2, true);
+    bytes += q.count * (int64_t)(pw + gw + 2 * sw);
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  uintptr_t end = 0, end_written = 0;  // of what begins before
+  for (const Span& s : spans) {
+    if (s.at < end_written || (s.written && s.at < end))
+      return rfast_refuse(RFAST_EINVAL, "memory that a step writes overlaps other memory of the step");
+    end = std::max(end, s.end);
+    if (s.written) end_written = std::max(end_written, s.end);
+  }
+  char* base = (char*)d_workspace;
+  hipError_t e = hipMemcpyAsync(base + l.rows, rows.data(), rows.size() * sizeof(Row), hipMemcpyHostToDevice, stream);
+  if (e == hipSuccess && chunks) e = hipMemcpyAsync(base + l.whose, whose.data(), whose.size() * 4, hipMemcpyHostToDevice, stream);
+  if (e == hipSuccess) e = hipMemcpyAsync(base + l.steps, steps.data(), steps.size() * 4, hipMemcpyHostToDevice, stream);
+  const std::vector<unsigned> none(kGroups * 16 + 1, 0u);
+  if (e == hipSuccess) e = hipMemcpyAsync(base + l.through, none.data(), none.size() * 4, hipMemcpyHostToDevice, stream);
+  if (e == hipSuccess) e = hipStreamSynchronize(stream);
+  if (e != hipSuccess) return rfast_refuse_hip(e, "upload of the table of tensors");
+  rfast_adamw* h = new rfast_adamw;
+  h->param_type = o->param_type;
+  h->grad_type = o->grad_type;
+  h->bits = o->state_bits;
+  h->slices = (int)slices;
+  h->stream = bytes > (int64_t)256 << 20;  // more than the caches hold from one step to the next
+  h->a = {(const Row*)(base + l.rows), (const int32_t*)(base + l.whose), (int32_t*)(base + l.steps), (unsigned*)(base + l.through),
+          nullptr, tensors, (int32_t)chunks, 0.0, std::log(o->beta1), std::log(o->beta2),
+          (float)o->beta1, (float)o->beta2, (float)(1.0 - o->beta1), (float)(1.0 - o->beta2), (float)o->eps};
+  *out = h;
+  return RFAST_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rfast_adamw_workspace_bytes(int32_t tensors, const rfast_adamw_tensor* t) {
+  int64_t chunks;
+  if (tensors < 1 || !t || slices_for(tensors, t, &chunks) == 0) return 0;
+  return layout_of(tensors, chunks).total;
+}
+
+int rfast_adamw_create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, const rfast_adamw_options* o,
+                       void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!out) return rfast_refuse(RFAST_EINVAL, "out is NULL");
+  *out = nullptr;
+  try {
+    return create(out, tensors, t, o, d_workspace, workspace_bytes, (hipStream_t)hip_stream);
+  } catch (const std::exception&) {
+    return rfast_refuse(RFAST_EINVAL, "host memory ran out");
+  }
+}
+
+int rfast_adamw_step(rfast_adamw* h, double gamma, const uint8_t* d_active, void* hip_stream) {
+  if (!h) return rfast_refuse(RFAST_EINVAL, "NULL handle");
+  if (!(std::fabs(gamma) < 1e30)) return rfast_refuse(RFAST_ERANGE, "gamma must be finite");
+  Args a = h->a;
+  a.gamma = gamma;
+  a.active = d_active;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const bool pf = h->param_type == RFAST_F32, gf = h->grad_type == RFAST_F32;
+  const hipError_t e = pf ? (gf ? launch<float, float>(h, a, s) : launch<float, u16>(h, a, s))
+                          : (gf ? launch<u16, float>(h, a, s) : launch<u16, u16>(h, a, s));
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "AdamW launch");
+}
+
+int rfast_adamw_steps(rfast_adamw* h, int32_t* host_steps, void* hip_stream) {
+  if (!h || !host_steps) return rfast_refuse(RFAST_EINVAL, "NULL argument");
+  hipError_t e = hipMemcpyAsync(host_steps, h->a.steps, (size_t)h->a.tensors * 4, hipMemcpyDeviceToHost, (hipStream_t)hip_stream);
+  if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "read of the counters");
+}
+
+int rfast_adamw_set_steps(rfast_adamw* h, const int32_t* host_steps, void* hip_stream) {
+  if (!h || !host_steps) return rfast_refuse(RFAST_EINVAL, "NULL argument");
+  for (int32_t i = 0; i < h->a.tensors; ++i)
+    if (host_steps[i] < 0 || host_steps[i] == 0x7fffffff) return rfast_refuse(RFAST_ERANGE, "steps out of range");
+  hipError_t e = hipMemcpyAsync(h->a.steps, host_steps, (size_t)h->a.tensors * 4, hipMemcpyHostToDevice, (hipStream_t)hip_stream);
+  if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "write of the counters");
+}
+
+void rfast_adamw_destroy(rfast_adamw* h) { delete h; }
+
+}  // extern "C"

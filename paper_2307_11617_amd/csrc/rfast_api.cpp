@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "rfast_internal.h"
+#include "rfast_operators.h"
 #include "rfast_relay.h"
 
 size_t rfast_gemv_scratch_floats(int32_t n, const rfast_problem* prob);
@@ -19,7 +20,7 @@ bool rfast_softmax_shape_ok(const rfast_problem* prob);
 
 namespace {
 
-std::string g_create_error;
+thread_local std::string g_create_error;  // of the calls that have no context
 
 constexpr size_t kAlign = 256;
 inline size_t up(size_t b) { return (b + kAlign - 1) / kAlign * kAlign; }
@@ -596,6 +597,9 @@ int after_round(rfast_ctx* c) {
 }
 
 }  // namespace
+
+int rfast_refuse(int code, const std::string& msg) { return fail(nullptr, code, msg); }
+int rfast_refuse_hip(hipError_t e, const char* what) { return hipfail(nullptr, e, what); }
 
 extern "C" int rfast_round(rfast_ctx* c, const uint8_t* d_active, const int32_t* d_delay_R, const int32_t* d_delay_C,
                            const uint8_t* d_drop_R, const uint8_t* d_drop_C, float gamma, const int32_t* d_batch_idx);
