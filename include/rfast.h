@@ -65,22 +65,30 @@ typedef enum rfast_objective {
   RFAST_OBJ_DIAG_QUADRATIC = 0, /* f_i = 1/2 sum_k h_ik (x_k - c_ik)^2, gradient + noise_std*N(0,I) */
   RFAST_OBJ_LEAST_SQUARES = 1,  /* f_i = 1/(2m) ||A_i x - b_i||^2                                   */
   RFAST_OBJ_LOGISTIC = 2,       /* f_i = mean_s [log(1+exp(a_s.x)) - y_s a_s.x] + lambda/2 ||x||^2  */
-  RFAST_OBJ_SOFTMAX_BF16 = 3    /* softmax regression, W = x as d x K row-major, bf16 MFMA GEMMs;
+  RFAST_OBJ_SOFTMAX_BF16 = 3,   /* softmax regression, W = x as d x K row-major, bf16 MFMA GEMMs;
                                    needs d % 64 == 0, K in {32,64,96,128}, rows per gradient % 64 == 0 */
+  RFAST_OBJ_LORA_SOFTMAX = 4    /* softmax regression through low-rank adapters: logits (W0 + scale B A) x with W0 frozen and the
+                                   same for all nodes, x_i = A (rank x d), then B (K x rank), both row-major, p = rank (d + K);
+                                   rounded to bf16 for the products (see rfast_lora_forward), as the gradient of the logits is;
+                                   rank 1 .. 64, any d and K.  With A = B = 0 every gradient is zero: give rfast_init an x0. */
 } rfast_objective;
 
 typedef struct rfast_problem {
   int32_t kind;        /* rfast_objective */
   int32_t samples;     /* rows held per node (LS: m; logistic/softmax: pool size); 0 for diag quadratic */
   int32_t batch;       /* rows per sampled gradient; 0 = all `samples` rows (full local gradient)       */
-  int32_t d, K;        /* softmax only: features, classes; p must equal d*K                             */
+  int32_t d, K;        /* softmax only: features, classes; p must equal d*K (adapters: rank*(d+K))      */
   float lambda;        /* logistic only: l2 coefficient                                                 */
   float noise_std;     /* diag quadratic only: std of the additive gradient noise                       */
   uint64_t noise_seed; /* diag quadratic only: key of the counter-based generator (see below)           */
   const void* data0;   /* device. diag: h  fp32 [n][p]. LS/logistic: rows fp32 [n][samples][p].
-                          softmax: pool bf16 [n][samples][d]                                            */
+                          softmax, with or without adapters: pool bf16 [n][samples][d]                  */
   const void* data1;   /* device. diag: c  fp32 [n][p]. LS: b fp32 [n][samples]. logistic: y fp32 (0/1)
-                          [n][samples]. softmax: labels int32 [n][samples]                              */
+                          [n][samples]. softmax: labels int32 [n][samples] (adapters: a label outside
+                          [0, K) counts as a row without loss)                                          */
+  int32_t rank;        /* adapters only */
+  float adapter_scale; /* adapters only */
+  const void* data2;   /* device. adapters only: W0 bf16 [K][d]                                         */
 } rfast_problem;
 /* Gradient noise of the diagonal quadratic: coordinates are taken in groups of
  * four; group q of (node i, sample version t) is Philox4x32-10 (Salmon et al.,
@@ -120,7 +128,12 @@ typedef enum rfast_field {
   RFAST_SCHED_DROP_R = 19,  /* uint8 [nnzR_off] */
   RFAST_SCHED_DROP_C = 20,  /* uint8 [nnzC_off] */
   RFAST_SCHED_BATCH = 21,   /* int32 [n][batch] */
-  RFAST_MOMENTUM = 22       /* fp32 [n][p]  heavy-ball buffers m_i (only after rfast_set_optimizer gave one) */
+  RFAST_MOMENTUM = 22,      /* fp32 [n][p]  heavy-ball buffers m_i (only after rfast_set_optimizer gave one) */
+  /* after rfast_set_adamw: moments of every node, fp32 [n][p] or e4m3 codes uint8 [n][p] (V: of the root), and the latters' scales */
+  RFAST_ADAMW_M = 23,
+  RFAST_ADAMW_V = 24,
+  RFAST_ADAMW_M_SCALE = 25, /* fp32 [n][ceil(p / 256)], state_bits 8 only */
+  RFAST_ADAMW_V_SCALE = 26
 } rfast_field;
 
 typedef struct rfast_diag {
@@ -339,6 +352,18 @@ int rfast_set_rebase_interval(rfast_ctx* ctx, int32_t rounds);
  * the buffers change meaning, rfast_init must follow before the next round
  * (rounds return RFAST_EINVAL until it has). */
 int rfast_set_optimizer(rfast_ctx* ctx, float momentum, float weight_decay, float* d_momentum);
+/* AdamW variant (instead of rfast_set_optimizer's; the later call counts): every node takes its local descent along
+ *   S1   m_i = beta1 m_i + (1 - beta1) z_i,  q_i = beta2 q_i + (1 - beta2) z_i^2,
+ *        v_i = x_i - gamma (mhat_i / (sqrt(qhat_i) + eps) + weight_decay x_i)
+ * with the tracked direction z_i in the place of the gradient, mhat = m / (1 - beta1^t), qhat = q / (1 - beta2^t) and t = t_i + 1, the
+ * number of the node's activation; only an activated node touches its moments.  The same holds for rfast_sync_round.  The weight
+ * decay is decoupled: it is part of no gradient and of no loss.  The moments are held as rfast_adamw_create describes (state_bits 32 or 8, the
+ * scales counted from each node's first coordinate).  d_state: device memory of rfast_adamw_state_bytes(n, p, state_bits), 256-byte aligned,
+ * owned by the caller, must outlive the context.  Rounds take the kernels per round (rfast_use_blocks has no effect), with one
+ * launch more for the moments.  rfast_init must follow before the next round. */
+size_t rfast_adamw_state_bytes(int32_t n, int64_t p, int32_t state_bits);
+int rfast_set_adamw(rfast_ctx* ctx, double beta1, double beta2, double eps, double weight_decay, int32_t state_bits,
+                    void* d_state, size_t state_bytes);
 /* Step-decayed learning rate (same experiment, hyper-parameter ii): round number r
  * (RFAST_ROUND, counted from rfast_init) runs with gamma * factor^(r div step_rounds),
  * where gamma is what the round call passes.  step_rounds = 0 (default) switches it off.
@@ -360,7 +385,7 @@ int rfast_read_state(rfast_ctx* ctx, int32_t field, void* host_dst, size_t bytes
 /* Waits for the stream and overwrites one field from HOST memory: the inverse
  * of rfast_read_state, for checkpoint / resume.  Restoring X, Z, G, V_RING,
  * SIGMA_RING, RHO_TILDE, T_NODE, TAU_R, TAU_C, DELIV_R, DELIV_C, T_HIST,
- * ROUND (and MOMENTUM when used) into a context created with the same arguments reproduces the run bit
+ * ROUND (and MOMENTUM or the ADAMW fields when used) into a context created with the same arguments reproduces the run bit
  * for bit.  RHO_RING (derived), SLOT_R and SLOT_C (per-round plan) cannot be
  * written (RFAST_EINVAL). */
 int rfast_write_state(rfast_ctx* ctx, int32_t field, const void* host_src, size_t bytes);

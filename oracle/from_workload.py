@@ -21,6 +21,9 @@ def make_oracle(w, coords=None, x0=None, momentum=0.0, weight_decay=0.0):
         obj = ob.LeastSquares(d["A"], d["b"])
     elif w.objective == "logistic":
         obj = ob.Logistic(d["X"], d["y"])
+    elif w.objective == "lora_softmax":
+        from rfast_workloads.problems import bf16_bits_to_f32
+        obj = ob.LoraSoftmax(bf16_bits_to_f32(d["Xb"]), d["labels"], bf16_bits_to_f32(d["W0"]), w.extra["rank"], w.extra["scale"])
     else:
         from rfast_workloads.problems import bf16_bits_to_f32
         obj = ob.SoftmaxBf16(bf16_bits_to_f32(d["Xb"]), d["labels"], w.extra["d"], w.extra["K"])

@@ -189,3 +189,45 @@ class SoftmaxBf16:
         logits = self.X[i] @ Wq
         lse = np.logaddexp.reduce(logits, axis=1)
         return float(np.mean(lse - logits[np.arange(logits.shape[0]), self.lab[i]]))
+
+
+class LoraSoftmax:
+    """Softmax regression through low-rank adapters beside a frozen projection: x is A (rank x d, row-major), then B (K x rank);
+    logits = (W0 + scale B A) x_row with bf16(A) and bf16(B), products and sums in wide precision; E = bf16((P - onehot) / batch);
+    grad A = scale (E B)^T X, grad B = scale E^T (X A^T).  A label outside [0, K) is a row without loss.  f_i = mean cross-entropy over
+    the node's pool (evaluated with the same rounded adapters).  `rounding=False` leaves both roundings out (for differences)."""
+
+    def __init__(self, X_pool, labels, W0, rank, scale, rounding=True):
+        self.X = np.asarray(X_pool, dtype=np.float64)
+        self.lab = np.asarray(labels, dtype=np.int64)
+        self.W0 = np.asarray(W0, dtype=np.float64)
+        self.K, self.d = self.W0.shape
+        self.rank, self.scale = int(rank), float(scale)
+        self.p = self.rank * (self.d + self.K)
+        self.round = _round_bf16 if rounding else (lambda a: np.asarray(a, dtype=np.float64))
+
+    def _split(self, x):
+        q = self.round(x)
+        return q[:self.rank * self.d].reshape(self.rank, self.d), q[self.rank * self.d:].reshape(self.K, self.rank)
+
+    def _log_p(self, X, A, B):
+        logits = X @ self.W0.T + self.scale * (X @ A.T) @ B.T
+        top = logits.max(axis=1, keepdims=True)
+        return logits - top - np.log(np.exp(logits - top).sum(axis=1, keepdims=True))
+
+    def grad(self, i, x, version, batch=None):
+        rows = np.arange(self.X.shape[1]) if batch is None else np.asarray(batch)
+        X, lab = self.X[i][rows], self.lab[i][rows]
+        A, B = self._split(x)
+        E = np.exp(self._log_p(X, A, B))
+        ok = (lab >= 0) & (lab < self.K)
+        E[np.nonzero(ok)[0], lab[ok]] -= 1.0
+        E[~ok] = 0.0
+        E = self.round(E / len(rows))
+        return np.concatenate([(self.scale * (E @ B).T @ X).reshape(-1), (self.scale * E.T @ (X @ A.T)).reshape(-1)])
+
+    def loss(self, i, x):
+        A, B = self._split(x)
+        lp, lab = self._log_p(self.X[i], A, B), self.lab[i]
+        ok = np.nonzero((lab >= 0) & (lab < self.K))[0]
+        return float(-lp[ok, lab[ok]].sum() / len(lab))

@@ -20,7 +20,8 @@ class RFastError(RuntimeError):
 class RfastProblem(C.Structure):
     _fields_ = [("kind", C.c_int32), ("samples", C.c_int32), ("batch", C.c_int32), ("d", C.c_int32),
                 ("K", C.c_int32), ("lam", C.c_float), ("noise_std", C.c_float), ("noise_seed", C.c_uint64),
-                ("data0", C.c_void_p), ("data1", C.c_void_p)]
+                ("data0", C.c_void_p), ("data1", C.c_void_p), ("rank", C.c_int32), ("adapter_scale", C.c_float),
+                ("data2", C.c_void_p)]
 
 
 class RfastDiag(C.Structure):
@@ -44,16 +45,17 @@ class RfastAdamwOptions(C.Structure):
                 ("beta2", C.c_double), ("eps", C.c_double)]
 
 
-OBJECTIVES = {"diag_quadratic": 0, "least_squares": 1, "logistic": 2, "softmax_bf16": 3}
+OBJECTIVES = {"diag_quadratic": 0, "least_squares": 1, "logistic": 2, "softmax_bf16": 3, "lora_softmax": 4}
 RFAST_FIELDS = {"X": 0, "Z": 1, "G": 2, "V_RING": 3, "RHO_RING": 4, "RHO_TILDE": 5, "T_NODE": 6, "TAU_R": 7,
                 "TAU_C": 8, "SLOT_R": 9, "SLOT_C": 10, "ROUND": 11, "SIGMA_RING": 12, "DELIV_R": 13, "DELIV_C": 14,
                 "T_HIST": 15, "SCHED_ACTIVE": 16, "SCHED_DELAY_R": 17, "SCHED_DELAY_C": 18, "SCHED_DROP_R": 19,
-                "SCHED_DROP_C": 20, "SCHED_BATCH": 21, "MOMENTUM": 22}
+                "SCHED_DROP_C": 20, "SCHED_BATCH": 21, "MOMENTUM": 22, "ADAMW_M": 23, "ADAMW_V": 24, "ADAMW_M_SCALE": 25,
+                "ADAMW_V_SCALE": 26}
 EXPORTS = ["rfast_common_roots", "rfast_workspace_bytes", "rfast_create", "rfast_init", "rfast_round", "rfast_run", "rfast_run_generated", "rfast_run_events", "rfast_use_graphs", "rfast_use_blocks", "rfast_block_info", "rfast_set_tile_group", "rfast_set_wait_limits", "rfast_sync_round", "rfast_sync_run", "rfast_rebase", "rfast_set_rebase_interval", "rfast_set_optimizer", "rfast_set_gamma_schedule", "rfast_check",
            "rfast_read_state", "rfast_write_state", "rfast_diagnostics", "rfast_diagnostics_static", "rfast_profile_enable", "rfast_kernel_time", "rfast_last_error",
            "rfast_destroy", "rfast_softmax_xent", "rfast_lora_workspace_bytes", "rfast_lora_forward", "rfast_lora_backward",
            "rfast_adamw_workspace_bytes", "rfast_adamw_create", "rfast_adamw_step", "rfast_adamw_steps", "rfast_adamw_set_steps",
-           "rfast_adamw_destroy"]
+           "rfast_adamw_destroy", "rfast_adamw_state_bytes", "rfast_set_adamw"]
 
 
 def lib():
@@ -102,6 +104,10 @@ def lib():
     L.rfast_set_rebase_interval.argtypes = [vp, i32]
     L.rfast_set_optimizer.restype = C.c_int
     L.rfast_set_optimizer.argtypes = [vp, C.c_float, C.c_float, vp]
+    L.rfast_adamw_state_bytes.restype = sz
+    L.rfast_adamw_state_bytes.argtypes = [i32, i64, i32]
+    L.rfast_set_adamw.restype = C.c_int
+    L.rfast_set_adamw.argtypes = [vp, C.c_double, C.c_double, C.c_double, C.c_double, i32, vp, sz]
     L.rfast_set_gamma_schedule.restype = C.c_int
     L.rfast_set_gamma_schedule.argtypes = [vp, i32, C.c_float]
     L.rfast_check.restype = C.c_int
@@ -256,6 +262,15 @@ def rfast_set_optimizer(ctx, momentum, weight_decay, momentum_buffer=None):
     _chk(lib().rfast_set_optimizer(ctx, momentum, weight_decay, _dev_ptr(momentum_buffer)), ctx)
 
 
+def rfast_adamw_state_bytes(n, p, state_bits):
+    return int(lib().rfast_adamw_state_bytes(n, p, state_bits))
+
+
+def rfast_set_adamw(ctx, beta1, beta2, eps, weight_decay, state_bits, state):
+    """state: uint8 device tensor of rfast_adamw_state_bytes."""
+    _chk(lib().rfast_set_adamw(ctx, beta1, beta2, eps, weight_decay, state_bits, _dev_ptr(state), 0 if state is None else state.numel()), ctx)
+
+
 def rfast_set_gamma_schedule(ctx, step_rounds, factor):
     _chk(lib().rfast_set_gamma_schedule(ctx, step_rounds, factor), ctx)
 
@@ -306,23 +321,29 @@ class RFast:
     forwards to the C ABI.  torch is used for device memory and the stream only."""
 
     def __init__(self, n, p, R, Cg, D, burst, objective, data0, data1, samples=0, batch=0, d=0, K=0, lam=0.0,
-                 noise_std=0.0, noise_seed=0, device="cuda:0"):
+                 noise_std=0.0, noise_seed=0, device="cuda:0", rank=0, adapter_scale=1.0, data2=None):
+        """data2, rank, adapter_scale: the shared projection (bfloat16 [K][d]) and the adapters of "lora_softmax"."""
         import torch
         self.torch = torch
+        self.adamw_bits = 0
         self.device = torch.device(device)
         self.n, self.p, self.D, self.M = n, p, D, D + 2
         self.nnzR_off, self.nnzC_off = len(R[1]) - n, len(Cg[1]) - n
         self.data0 = data0.to(self.device).contiguous()
         self.data1 = data1.to(self.device).contiguous()
         kind = OBJECTIVES[objective]
-        need0 = {0: n * p, 1: n * samples * p, 2: n * samples * p, 3: n * samples * d}[kind]
+        need0 = {0: n * p, 1: n * samples * p, 2: n * samples * p, 3: n * samples * d, 4: n * samples * d}[kind]
         need1 = n * p if kind == 0 else n * samples
-        dt0 = torch.bfloat16 if kind == 3 else torch.float32
-        dt1 = torch.int32 if kind == 3 else torch.float32
+        dt0 = torch.bfloat16 if kind >= 3 else torch.float32
+        dt1 = torch.int32 if kind >= 3 else torch.float32
         if self.data0.numel() != need0 or self.data1.numel() != need1 or self.data0.dtype != dt0 or self.data1.dtype != dt1:
             raise RFastError(-1, "objective data has the wrong size or dtype")
+        self.data2 = None if data2 is None else data2.to(self.device).contiguous()
+        if kind == 4 and (self.data2 is None or self.data2.numel() != K * d or self.data2.dtype != torch.bfloat16):
+            raise RFastError(-1, "data2: need the shared projection as K*d bfloat16 values")
         self.prob = RfastProblem(OBJECTIVES[objective], samples, batch, d, K, lam, noise_std, noise_seed,
-                                 self.data0.data_ptr(), self.data1.data_ptr())
+                                 self.data0.data_ptr(), self.data1.data_ptr(), rank, adapter_scale,
+                                 None if self.data2 is None else self.data2.data_ptr())
         nbytes = rfast_workspace_bytes(n, p, len(R[1]), len(Cg[1]), D, self.prob)
         if nbytes == 0:
             raise RFastError(-1, "sizes out of range")
@@ -395,10 +416,18 @@ class RFast:
 
     def set_optimizer(self, momentum=0.0, weight_decay=0.0):
         """Optimizer variant; init() must follow.  The buffer of the heavy-ball terms is allocated here."""
-        self.momentum_buffer = None
+        buffer = None
         if momentum != 0.0:
-            self.momentum_buffer = self.torch.zeros(self.n * self.p, dtype=self.torch.float32, device=self.device)
-        rfast_set_optimizer(self.ctx, momentum, weight_decay, self.momentum_buffer)
+            buffer = self.torch.zeros(self.n * self.p, dtype=self.torch.float32, device=self.device)
+        rfast_set_optimizer(self.ctx, momentum, weight_decay, buffer)
+        self.momentum_buffer, self.adamw_bits = buffer, 0
+
+    def set_adamw(self, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state_bits=32):
+        """AdamW variant; init() must follow.  The moments' memory is allocated here."""
+        nbytes = rfast_adamw_state_bytes(self.n, self.p, state_bits)
+        state = self.torch.empty(max(nbytes, 256), dtype=self.torch.uint8, device=self.device)
+        rfast_set_adamw(self.ctx, betas[0], betas[1], eps, weight_decay, state_bits, state)
+        self.momentum_buffer, self.adamw_bits, self.adamw_state = None, state_bits, state
 
     def set_gamma_schedule(self, step_rounds, factor):
         rfast_set_gamma_schedule(self.ctx, step_rounds, factor)
@@ -420,6 +449,10 @@ class RFast:
                   "SCHED_DROP_R": ((self.nnzR_off,), np.uint8), "SCHED_DROP_C": ((self.nnzC_off,), np.uint8),
                   "SCHED_BATCH": ((n, self.prob.batch if self.prob.kind != 0 else 0), np.int32),
                   "MOMENTUM": ((n, p), np.float32)}
+        if field.startswith("ADAMW"):
+            if field.endswith("SCALE"):
+                return (n, (p + 255) // 256), np.float32
+            return (n, p), np.uint8 if self.adamw_bits == 8 else np.float32
         return shapes[field]
 
     def read(self, field):
@@ -438,6 +471,8 @@ class RFast:
 
     def _checkpoint_fields(self):
         extra = ("MOMENTUM",) if getattr(self, "momentum_buffer", None) is not None else ()
+        if self.adamw_bits:
+            extra = ("ADAMW_M", "ADAMW_V") + (("ADAMW_M_SCALE", "ADAMW_V_SCALE") if self.adamw_bits == 8 else ())
         return self.CHECKPOINT_FIELDS + extra
 
     def checkpoint(self):

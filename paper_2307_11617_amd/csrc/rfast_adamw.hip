@@ -13,6 +13,7 @@
 #include <new>
 #include <vector>
 
+#include "rfast_internal.h"
 #include "rfast_operators.h"
 
 namespace {
@@ -227,6 +228,56 @@ __global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
     if (!a.active || a.active[i] != 0) a.steps[i] += 1;
 }
 
+// The AdamW variant of a round: the same moments, of the nodes about to act, from the tracked directions z; what the step would
+// subtract, over gamma, is left for S1.  One workgroup per kSlice coordinates of a node.
+struct RoundArgs {
+  const float* z;
+  int64_t z_stride;  // from node to node
+  const float* x;
+  float* dir;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  const int2* plan;  // {node, counter}, or NULL: every node
+  const int32_t* t;
+  int64_t p;
+  double log_beta1, log_beta2;
+  float beta1, beta2, rest1, rest2, eps, decay;
+};
+
+template <int BITS> __global__ void __launch_bounds__(kThreads) rfast_adamw_round_kernel(RoundArgs a) {
+  int i = blockIdx.y, t;
+  if (a.plan) {
+    const int2 slot = a.plan[i];
+    if (slot.x < 0) return;
+    i = slot.x;
+    t = slot.y + 1;
+  } else {
+    t = a.t[i] + 1;
+  }
+  const int64_t k = (int64_t)blockIdx.x * kSlice + threadIdx.x * 4, left = a.p - k;
+  const int64_t row = (int64_t)i * a.p, blocks = (a.p + kBlock - 1) / kBlock;
+  constexpr int WIDE = BITS / 8;
+  void *m = (char*)a.m + row * WIDE, *v = (char*)a.v + row * WIDE;
+  float* ms = BITS == 8 ? a.m_scale + i * blocks : nullptr;
+  float* vs = BITS == 8 ? a.v_scale + i * blocks : nullptr;
+  Moments<BITS, false> state;
+  float g[4], x[4], root[4];
+  if (left > 0) {
+    load_four<false>(a.z + i * a.z_stride + k, left, g);
+    load_four<false>(a.x + row + k, left, x);
+  }
+  state.read(m, v, ms, vs, k, left);
+  const float first = (float)(1.0 / one_less_power(a.log_beta1, t));
+  const float second = (float)(1.0 / sqrt(one_less_power(a.log_beta2, t)));
+  state.step(g, a.beta1, a.rest1, a.beta2, a.rest2, root);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = (state.m[j] * first) / (root[j] * second + a.eps) + a.decay * x[j];
+  if (left > 0) store_four<false>(a.dir + row + k, left, x);
+  state.write(m, v, ms, vs, k, left, root);
+}
+
 struct Layout {
   size_t rows, whose, steps, through, total;
 };
@@ -354,6 +405,21 @@ int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, cons
 }
 
 }  // namespace
+
+hipError_t rfast_launch_adamw_round(rfast_ctx* c, bool sync, int parity) {
+  const RfastDev& d = c->d;
+  const RfastAdamwState& w = c->adamw;
+  RoundArgs a = {d.z, d.p, d.x, d.mom, w.m, w.v, w.m_scale, w.v_scale, sync ? nullptr : d.active_plan, d.t, d.p, std::log(w.beta1),
+                 std::log(w.beta2), (float)w.beta1, (float)w.beta2, (float)(1.0 - w.beta1), (float)(1.0 - w.beta2), (float)w.eps, (float)w.decay};
+  if (sync && parity) {  // the current z is in slot 1 of the v ring
+    a.z = d.v_ring + d.p;
+    a.z_stride = (int64_t)d.M * d.p;
+  }
+  const dim3 grid((unsigned)((d.p + kSlice - 1) / kSlice), (unsigned)d.n);
+  if (w.bits == 32) hipLaunchKernelGGL(rfast_adamw_round_kernel<32>, grid, dim3(kThreads), 0, c->stream, a);
+  else hipLaunchKernelGGL(rfast_adamw_round_kernel<8>, grid, dim3(kThreads), 0, c->stream, a);
+  return hipGetLastError();
+}
 
 extern "C" {
 

@@ -48,7 +48,7 @@ struct Offsets {
 
 bool sizes_ok(int32_t n, int64_t p, int32_t nnzR, int32_t nnzC, int32_t D, const rfast_problem* prob) {
   if (n < 1 || n > 65535 || p < 1 || nnzR < n || nnzC < n || D < 0 || D + 2 > 64 || prob == nullptr) return false;  // n rides in gridDim.y
-  if (prob->kind < 0 || prob->kind > RFAST_OBJ_SOFTMAX_BF16) return false;
+  if (prob->kind < 0 || prob->kind > RFAST_OBJ_LORA_SOFTMAX) return false;
   if (prob->kind != RFAST_OBJ_DIAG_QUADRATIC && (prob->samples < 1 || prob->batch < 0 || prob->batch > prob->samples))
     return false;
   if ((prob->kind == RFAST_OBJ_LEAST_SQUARES || prob->kind == RFAST_OBJ_LOGISTIC) &&
@@ -57,6 +57,7 @@ bool sizes_ok(int32_t n, int64_t p, int32_t nnzR, int32_t nnzC, int32_t D, const
   if (prob->kind == RFAST_OBJ_SOFTMAX_BF16 &&
       (prob->d < 1 || prob->K < 1 || (int64_t)prob->d * prob->K != p || !rfast_softmax_shape_ok(prob)))
     return false;  // MFMA tiling: d % 64 == 0, K in {32, 64, 96, 128}, rows per gradient % 64 == 0
+  if (prob->kind == RFAST_OBJ_LORA_SOFTMAX && !rfast_adapters_shape_ok(n, p, prob)) return false;
   return true;
 }
 
@@ -126,7 +127,7 @@ Offsets layout(int32_t n, int64_t p, int32_t nnzR, int32_t nnzC, int32_t D, cons
   o.gen_cdf = L.take(n * 4);
   o.xbar = L.take(vec);
   o.resid = L.take(rfast_gemv_scratch_floats(n, prob) * 4);
-  o.gscratch = L.take(rfast_softmax_scratch_bytes(n, prob));
+  o.gscratch = L.take(rfast_softmax_scratch_bytes(n, prob) + rfast_adapters_scratch_bytes(n, prob));
   o.diag = L.take(64 * sizeof(double));
   // the team kernels' packets and progress words: which team a problem gets depends on the graph and the device, so
   // room for the largest one (at most kTeamMost workgroups)
@@ -263,6 +264,8 @@ int hipfail(rfast_ctx* c, hipError_t e, const char* what) {
   return fail(c, RFAST_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+size_t adamw_scales(const RfastDev& d) { return (size_t)d.n * (((size_t)d.p + 255) / 256); }
+
 size_t field_bytes(const rfast_ctx* c, int32_t field) {
   const RfastDev& d = c->d;
   const size_t vec = (size_t)d.p * 4;
@@ -285,7 +288,9 @@ size_t field_bytes(const rfast_ctx* c, int32_t field) {
     case RFAST_SCHED_DROP_R: return (size_t)d.eR;
     case RFAST_SCHED_DROP_C: return (size_t)d.eC;
     case RFAST_SCHED_BATCH: return (size_t)d.n * (d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC ? 0 : d.prob.batch) * 4;
-    case RFAST_MOMENTUM: return d.mom ? d.n * vec : (size_t)-1;
+    case RFAST_MOMENTUM: return d.mom && !d.dir_given ? d.n * vec : (size_t)-1;
+    case RFAST_ADAMW_M: case RFAST_ADAMW_V: return c->adamw.bits ? (size_t)d.n * d.p * (c->adamw.bits / 8) : (size_t)-1;
+    case RFAST_ADAMW_M_SCALE: case RFAST_ADAMW_V_SCALE: return c->adamw.bits == 8 ? adamw_scales(d) * 4 : (size_t)-1;
     default: return (size_t)-1;
   }
 }
@@ -532,7 +537,7 @@ void context_gone() {
 // profiled ones, whose state and gradient kernels are to be timed apart, and rounds that would have to wait for a stream
 // that is under capture just now (the runtime allows no such dependency, whatever the event was recorded behind).
 bool team_usable(const rfast_ctx* c) {
-  if (!c->use_blocks || c->team.W <= 0 || c->capturing || c->profiling) return false;
+  if (c->adamw.bits || !c->use_blocks || c->team.W <= 0 || c->capturing || c->profiling) return false;
   if (((volatile unsigned*)c->team_told)[0] != 0) return false;  // the workgroups of a team of this context do not all find room
   if (c->stream != nullptr) {
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
@@ -702,6 +707,8 @@ int rfast_create(rfast_ctx** out, int32_t n, int64_t p, const int32_t* R_rowptr,
   const int32_t nnzR = R_rowptr[n], nnzC = C_rowptr[n];
   if (!sizes_ok(n, p, nnzR, nnzC, D, prob)) return fail(nullptr, RFAST_EINVAL, "sizes or problem description out of range");
   if (!prob->data0 || !prob->data1) return fail(nullptr, RFAST_EINVAL, "problem data pointers are NULL");
+  if (prob->kind == RFAST_OBJ_LORA_SOFTMAX && (!prob->data2 || (uintptr_t)prob->data2 % 2 != 0))
+    return fail(nullptr, RFAST_EINVAL, "the shared projection data2 is NULL or misaligned");
   if (((uintptr_t)d_workspace % kAlign) != 0) return fail(nullptr, RFAST_EINVAL, "workspace must be 256-byte aligned");
   if ((p % 4) == 0 && ((((uintptr_t)prob->data0) | ((uintptr_t)prob->data1)) % 16) != 0)
     return fail(nullptr, RFAST_EINVAL, "problem data must be 16-byte aligned");
@@ -860,6 +867,15 @@ int rfast_init(rfast_ctx* c, const float* d_x0, const int32_t* d_batch_idx0) {
   hipError_t e = hipSuccess;
   auto chk = [&](hipError_t r) { if (e == hipSuccess) e = r; };
   if (d.mom) chk(hipMemsetAsync(d.mom, 0, d.n * vec, c->stream));
+  if (c->adamw.bits) {
+    const size_t wide = c->adamw.bits == 32 ? 4 : 1;
+    chk(hipMemsetAsync(c->adamw.m, 0, (size_t)d.n * d.p * wide, c->stream));
+    chk(hipMemsetAsync(c->adamw.v, 0, (size_t)d.n * d.p * wide, c->stream));
+    if (c->adamw.bits == 8) {
+      chk(hipMemsetAsync(c->adamw.m_scale, 0, adamw_scales(d) * 4, c->stream));
+      chk(hipMemsetAsync(c->adamw.v_scale, 0, adamw_scales(d) * 4, c->stream));
+    }
+  }
   if (d_x0) chk(hipMemcpyAsync(d.x, d_x0, d.n * vec, hipMemcpyDeviceToDevice, c->stream));
   else chk(hipMemsetAsync(d.x, 0, d.n * vec, c->stream));
   chk(hipMemsetAsync(d.g, 0, 2 * d.n * vec, c->stream));
@@ -910,7 +926,7 @@ static int check_round_args(rfast_ctx* c, const uint8_t* d_active, const int32_t
   const bool separable = d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC;
   if (!separable && d.prob.batch > 0 && !d_batch_idx) return fail(c, RFAST_EINVAL, "sample rows are required when batch > 0");
   if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
   return state_usable(c);
 }
 
@@ -940,6 +956,10 @@ static int float_round(rfast_ctx* c, float gamma, const int32_t* d_batch_idx, bo
   const bool separable = c->d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC;
   gamma = gamma_now(c, gamma);
   hipError_t e;
+  if (c->adamw.bits) {
+    e = rfast_launch_adamw_round(c, false, 0);
+    if (e != hipSuccess) return hipfail(c, e, "AdamW launch");
+  }
   if (separable) {
     time_begin(c, 0);
     e = rfast_launch_state(c, RFAST_MODE_FUSED, gamma, warm);
@@ -1049,7 +1069,7 @@ static int32_t wave_least_rounds(const rfast_ctx* c) {
 // step of the step-size schedule; and it reads and writes every ring slot once, which a large
 // state earns back only over enough rounds.
 static int32_t block_length(const rfast_ctx* c, int32_t rounds, int64_t at_round) {
-  if (!c->use_blocks || c->capturing) return 0;
+  if (!c->use_blocks || c->capturing || c->adamw.bits) return 0;
   const bool gemv = rfast_tiny_eligible(c) || c->team.W > 0;  // (every round of these takes the multi-round kernels)
   if (!gemv && (c->no_tiles || !rfast_wave_eligible(c))) return 0;
   if (gemv && !rfast_tiny_eligible(c) && !team_usable(c)) return 0;
@@ -1175,7 +1195,7 @@ int rfast_run(rfast_ctx* c, int32_t rounds, const uint8_t* d_active, const int32
       if (!d_active || (d.eR && (!d_delay_R || !d_drop_R)) || (d.eC && (!d_delay_C || !d_drop_C)))
         return fail(c, RFAST_EINVAL, "NULL schedule pointer");
       if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
       if (B > 0 && !d_batch_idx) return fail(c, RFAST_EINVAL, "sample rows are required when batch > 0");
       const int rc = run_block(c, len, d_active + (size_t)r * d.n, d_delay_R ? d_delay_R + (size_t)r * d.eR : nullptr,
                                d_delay_C ? d_delay_C + (size_t)r * d.eC : nullptr,
@@ -1210,7 +1230,7 @@ int rfast_run(rfast_ctx* c, int32_t rounds, const uint8_t* d_active, const int32
     if (c->use_blocks && rfast_chain_eligible(c)) {
       rc = chained_rounds(c, ahead, gamma, d_active + (size_t)r * d.n, d_batch_idx ? d_batch_idx + (size_t)r * d.n * B : nullptr);
       if (rc != RFAST_OK) return rc;
-    } else if (c->no_tiles && c->use_blocks && !c->profiling && d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC) {
+    } else if (c->no_tiles && c->use_blocks && !c->profiling && !c->adamw.bits && d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC) {
       for (int32_t q = 0; q < ahead;) {
         use_plan_set(c, q);
         int32_t len = ahead - q;  // one step size per launch (and no rebase inside: the stretch ends there)
@@ -1253,7 +1273,7 @@ int rfast_run_generated(rfast_ctx* c, int32_t rounds, uint64_t seed, const float
   // A generated round takes no host argument that varies from round to round (the
   // generator reads the round number on the device), so kGraphRounds of them are
   // captured once into a HIP graph and replayed: one launch per kGraphRounds rounds.
-  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
   if (const int rc = state_usable(c)) return rc;
   const bool graphs = c->use_graphs && !c->profiling;
   while (rounds > 0) {
@@ -1299,7 +1319,7 @@ int rfast_run_events(rfast_ctx* c, int32_t iterations, uint64_t seed, const floa
   if (max_delay < 0 || max_delay > d.d_max) return fail(c, RFAST_ERANGE, "max_delay must lie in [0, D - burst + 1]");
   if (!(p_drop >= 0.f && p_drop <= 1.f)) return fail(c, RFAST_ERANGE, "p_drop must lie in [0, 1]");
   if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
   if (const int rc = state_usable(c)) return rc;
   // selection thresholds: node i is drawn when cdf[i-1] <= u < cdf[i], u a 32-bit word
   std::vector<uint32_t> cdf(d.n);
@@ -1344,11 +1364,15 @@ int rfast_sync_round(rfast_ctx* c, float gamma, const int32_t* d_batch_idx) {
   const bool separable = d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC;
   if (!separable && d.prob.batch > 0 && !d_batch_idx) return fail(c, RFAST_EINVAL, "sample rows are required when batch > 0");
   if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+  if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
   if (const int rc = state_usable(c)) return rc;
   if (d.prob.kind != RFAST_OBJ_SOFTMAX_BF16 && team_usable(c)) return rfast_sync_run(c, 1, gamma, d_batch_idx);
   gamma = gamma_now(c, gamma);
   hipError_t e;
+  if (c->adamw.bits) {
+    e = rfast_launch_adamw_round(c, true, c->sync_parity);
+    if (e != hipSuccess) return hipfail(c, e, "AdamW launch");
+  }
   time_begin(c, 0);
   e = rfast_launch_sync(c, separable ? 2 : 0, gamma, c->sync_parity);
   time_end(c, 0);
@@ -1374,14 +1398,14 @@ int rfast_sync_run(rfast_ctx* c, int32_t rounds, float gamma, const int32_t* d_b
   if (const int rc = state_usable(c)) return rc;
   const RfastDev& d = c->d;
   const size_t B = d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC ? 0 : (size_t)d.prob.batch;
-  const bool multi = c->use_blocks && rfast_sync_wave_eligible(c);
+  const bool multi = c->use_blocks && !c->adamw.bits && rfast_sync_wave_eligible(c);
   const bool team = d.prob.kind != RFAST_OBJ_SOFTMAX_BF16 && team_usable(c);
   for (int32_t r = 0; r < rounds;) {
     if (team) {  // least squares / logistic regression: the steps up to the next decay of the step size in one launch
       int32_t len = std::min(rounds - r, 1 << 20);
       if (c->gamma_step > 0) len = (int32_t)std::min<int64_t>(len, c->gamma_step - c->host_round % c->gamma_step);
       if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
       if (B > 0 && !d_batch_idx) return fail(c, RFAST_EINVAL, "sample rows are required when batch > 0");
       if (fold_sync(c) != RFAST_OK) return RFAST_EHIP;
       time_begin(c, 0);
@@ -1403,7 +1427,7 @@ int rfast_sync_run(rfast_ctx* c, int32_t rounds, float gamma, const int32_t* d_b
     }
     if (len >= 2) {
       if (!std::isfinite(gamma)) return fail(c, RFAST_EINVAL, "gamma is not finite");
-      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer");
+      if (c->needs_init) return fail(c, RFAST_EINVAL, "rfast_init must follow rfast_set_optimizer or rfast_set_adamw");
       if (fold_sync(c) != RFAST_OK) return RFAST_EHIP;
       time_begin(c, 0);
       hipError_t e = rfast_launch_sync_wave(c, gamma_now(c, gamma), len);
@@ -1431,9 +1455,51 @@ int rfast_set_optimizer(rfast_ctx* c, float momentum, float weight_decay, float*
   c->d.beta = momentum;
   c->d.wd = weight_decay;
   c->d.mom = momentum != 0.f ? d_momentum : nullptr;
+  c->d.dir_given = 0;
+  c->adamw = RfastAdamwState();
   c->needs_init = true;
   const hipError_t e = rfast_wave_prime(c);  // the variant has instantiations of its own
   if (e != hipSuccess) return hipfail(c, e, "loading the multi-round kernel");
+  return RFAST_OK;
+}
+
+size_t rfast_adamw_state_bytes(int32_t n, int64_t p, int32_t state_bits) {
+  if (n < 1 || n > 65535 || p < 1 || p > (int64_t)1 << 40 || (state_bits != 8 && state_bits != 32)) return 0;
+  const size_t count = (size_t)n * (size_t)p;
+  return up(count * 4) + 2 * up(count * (size_t)(state_bits / 8)) + (state_bits == 8 ? 2 * up((size_t)n * (((size_t)p + 255) / 256) * 4) : 0);
+}
+
+int rfast_set_adamw(rfast_ctx* c, double beta1, double beta2, double eps, double weight_decay, int32_t state_bits, void* d_state,
+                    size_t state_bytes) {
+  if (!c) return RFAST_EINVAL;
+  if (state_bits != 8 && state_bits != 32) return fail(c, RFAST_EINVAL, "state_bits must be 8 or 32");
+  if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return fail(c, RFAST_ERANGE, "beta1 and beta2 must lie in [0, 1)");
+  if (!(eps > 0 && eps < 1e30)) return fail(c, RFAST_ERANGE, "eps must be positive and finite");
+  if (!(weight_decay >= 0 && weight_decay < 1e30)) return fail(c, RFAST_ERANGE, "weight_decay must be finite and >= 0");
+  if (!d_state || (uintptr_t)d_state % kAlign != 0) return fail(c, RFAST_EINVAL, "the states need memory at a multiple of 256 bytes");
+  if (state_bytes < rfast_adamw_state_bytes(c->d.n, c->d.p, state_bits)) return fail(c, RFAST_ENOMEM, "memory for the states too small");
+  drop_graph(c);  // a captured graph holds the old kernel arguments
+  const size_t count = (size_t)c->d.n * (size_t)c->d.p, wide = (size_t)(state_bits / 8);
+  char* at = (char*)d_state;
+  auto take = [&](size_t bytes) { char* p = at; at += up(bytes); return p; };
+  c->d.beta = 0.f;
+  c->d.wd = 0.f;
+  c->d.mom = (float*)take(count * 4);
+  c->d.dir_given = 1;
+  RfastAdamwState a;
+  a.bits = state_bits;
+  a.beta1 = beta1;
+  a.beta2 = beta2;
+  a.eps = eps;
+  a.decay = weight_decay;
+  a.m = take(count * wide);
+  a.v = take(count * wide);
+  if (state_bits == 8) {
+    a.m_scale = (float*)take(adamw_scales(c->d) * 4);
+    a.v_scale = (float*)take(adamw_scales(c->d) * 4);
+  }
+  c->adamw = a;
+  c->needs_init = true;
   return RFAST_OK;
 }
 
@@ -1519,6 +1585,10 @@ int rfast_read_state(rfast_ctx* c, int32_t field, void* host_dst, size_t bytes) 
       src = d.gen_batch + (size_t)c->gen_last * d.n * (d.prob.kind == RFAST_OBJ_DIAG_QUADRATIC ? 0 : d.prob.batch);
       break;
     case RFAST_MOMENTUM: src = d.mom; break;
+    case RFAST_ADAMW_M: src = c->adamw.m; break;
+    case RFAST_ADAMW_V: src = c->adamw.v; break;
+    case RFAST_ADAMW_M_SCALE: src = c->adamw.m_scale; break;
+    case RFAST_ADAMW_V_SCALE: src = c->adamw.v_scale; break;
     default: break;
   }
   if (field == RFAST_RHO_RING) {
@@ -1602,6 +1672,10 @@ int rfast_write_state(rfast_ctx* c, int32_t field, const void* host_src, size_t 
     case RFAST_DELIV_C: dst = d.deliv_c; break;
     case RFAST_T_HIST: dst = d.t_hist; break;
     case RFAST_MOMENTUM: dst = d.mom; break;
+    case RFAST_ADAMW_M: dst = c->adamw.m; break;
+    case RFAST_ADAMW_V: dst = c->adamw.v; break;
+    case RFAST_ADAMW_M_SCALE: dst = c->adamw.m_scale; break;
+    case RFAST_ADAMW_V_SCALE: dst = c->adamw.v_scale; break;
     default: break;
   }
   if (field == RFAST_ROUND) c->host_round = *(const int32_t*)host_src;

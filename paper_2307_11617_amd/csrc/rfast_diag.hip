@@ -370,5 +370,9 @@ hipError_t rfast_launch_diag(rfast_ctx* c, const float* d_xstar, double* d_out) 
     const hipError_t e = rfast_softmax_loss(c, d_out + 5);
     if (e != hipSuccess) return e;
   }
+  if (kind == RFAST_OBJ_LORA_SOFTMAX) {
+    const hipError_t e = rfast_adapters_loss(c, d_out + 5);
+    if (e != hipSuccess) return e;
+  }
   return hipGetLastError();
 }

@@ -491,6 +491,7 @@ hipError_t rfast_launch_gradient(rfast_ctx* c, const int32_t* batch_idx) {
     case RFAST_OBJ_LEAST_SQUARES:
     case RFAST_OBJ_LOGISTIC: return gemv_pair(c, batch_idx, false);
     case RFAST_OBJ_SOFTMAX_BF16: return rfast_softmax_gradient(c, batch_idx, false);
+    case RFAST_OBJ_LORA_SOFTMAX: return rfast_adapters_gradient(c, batch_idx, false);
     default: return hipErrorInvalidValue;
   }
 }
@@ -502,6 +503,7 @@ hipError_t rfast_launch_init_grad(rfast_ctx* c, const int32_t* batch_idx0) {
     case RFAST_OBJ_LEAST_SQUARES:
     case RFAST_OBJ_LOGISTIC: e = gemv_pair(c, batch_idx0, true); break;
     case RFAST_OBJ_SOFTMAX_BF16: e = rfast_softmax_gradient(c, batch_idx0, true); break;
+    case RFAST_OBJ_LORA_SOFTMAX: e = rfast_adapters_gradient(c, batch_idx0, true); break;
     default: return hipErrorInvalidValue;
   }
   if (e != hipSuccess) return e;

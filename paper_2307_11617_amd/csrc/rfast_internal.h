@@ -135,6 +135,7 @@ struct RfastDev {
   // optimizer variant: heavy-ball buffers m_i [n][p] (caller's memory, NULL when beta == 0)
   float* mom;
   float beta, wd;
+  int32_t dir_given;  // mom holds the direction of S1 itself, formed by the AdamW kernel ahead of the round
   // gradient scratch
   float* resid;           // [n][rows] residuals of the GEMV pair / unused
   void* gscratch;         // softmax: bf16 W copy and E matrix
@@ -147,8 +148,19 @@ struct RfastTeam {
   int W = 0, C = 0, per_lane = 0, tiles = 0;
 };
 
+// AdamW variant: moments of every node [n][p], in the caller's memory (bits 0: not in use)
+struct RfastAdamwState {
+  int32_t bits = 0;
+  double beta1 = 0, beta2 = 0, eps = 0, decay = 0;
+  void* m = nullptr;         // fp32, or e4m3 codes
+  void* v = nullptr;         // fp32, or e4m3 codes of the root
+  float* m_scale = nullptr;  // 8 bits: [n][ceil(p / 256)]
+  float* v_scale = nullptr;
+};
+
 struct rfast_ctx {
   RfastDev d;
+  RfastAdamwState adamw;
   hipStream_t stream;
   int32_t nnzR, nnzC;
   std::string err;
@@ -264,6 +276,9 @@ hipError_t rfast_launch_generate(rfast_ctx* c, uint64_t seed, const float* d_p_a
                                  int rounds = 1);
 hipError_t rfast_launch_sync(rfast_ctx* c, int phase, float gamma, int parity);
 hipError_t rfast_launch_sync_plan(rfast_ctx* c, int rounds);
+// AdamW variant: moves the moments of the nodes about to act and leaves the direction of their S1 in d.mom.  sync: all nodes, with
+// the z of the synchronous mode of this parity; else the round's active ones
+hipError_t rfast_launch_adamw_round(rfast_ctx* c, bool sync, int parity);
 bool rfast_sync_wave_eligible(const rfast_ctx* c);  // several synchronous steps per launch
 hipError_t rfast_launch_sync_wave(rfast_ctx* c, float gamma, int rounds);
 hipError_t rfast_launch_init_grad(rfast_ctx* c, const int32_t* batch_idx0);
@@ -274,5 +289,10 @@ hipError_t rfast_static_scratch_init();  // address of the static scratch array 
 int64_t rfast_static_max_coords();
 hipError_t rfast_launch_diag_static(rfast_ctx* c, const float* d_xstar, double* d_out, double l2_half_n);
 hipError_t rfast_softmax_loss(rfast_ctx* c, double* d_out);  // adds sum_i f_i(xbar) to *d_out
+// softmax regression through low-rank adapters beside a shared projection
+bool rfast_adapters_shape_ok(int32_t n, int64_t p, const rfast_problem* prob);
+size_t rfast_adapters_scratch_bytes(int32_t n, const rfast_problem* prob);
+hipError_t rfast_adapters_gradient(rfast_ctx* c, const int32_t* batch_idx, bool init);
+hipError_t rfast_adapters_loss(rfast_ctx* c, double* d_out);
 bool rfast_softmax_prep_is_fused(const rfast_problem* prob);
 size_t rfast_grad_scratch_bytes(int32_t n, int64_t p, const rfast_problem* prob);

@@ -154,8 +154,11 @@ __device__ inline void state_update(const RfastDev& s, float gamma, int2 slot, i
     // S1: local descent; with the optimizer variant along the heavy-ball buffer m <- beta m + z
     T dir = z_i;
     if (MOM) {
-      dir = fma_s(s.beta, m_i, z_i);
-      V<VEC>::st(s.mom + node_off, dir);
+      dir = m_i;  // (AdamW: its kernel has left the direction there)
+      if (!s.dir_given) {
+        dir = fma_s(s.beta, m_i, z_i);
+        V<VEC>::st(s.mom + node_off, dir);
+      }
     }
     const T v = fma_s(-gamma, dir, x_i);
     // S2a: pull the stamped neighbour copies and mix with row-stochastic weights
@@ -370,7 +373,9 @@ __global__ void __launch_bounds__(kThreads) rfast_sync_descent_kernel(RfastDev s
     using Vk = V<decltype(vec)::value>;
     const auto x = Vk::ld(s.x + (size_t)i * s.p + k);
     auto dir = Vk::ld(sync_z(s, parity, i) + k);
-    if (s.mom) {
+    if (s.dir_given) {
+      dir = Vk::ld(s.mom + (size_t)i * s.p + k);
+    } else if (s.mom) {
       dir = fma_s(s.beta, Vk::ld(s.mom + (size_t)i * s.p + k), dir);
       Vk::st(s.mom + (size_t)i * s.p + k, dir);
     }

@@ -86,4 +86,12 @@ def config4(seed=0, rounds=3000, d=1024, K=128, samples=2048, batch=256):
                batch=batch, samples=samples, tol=2e-3, extra={"d": d, "K": K})
 
 
+def adapters(seed=0, n=8, rounds=0, d=64, K=32, rank=4, samples=128, batch=32, gamma=0.3):
+    """Not one of the five: the softmax workload's pool with low-rank adapters beside a frozen projection as the trained vectors."""
+    r, c = graphs.exponential(n)
+    return _mk(f"adapters_exp{n}_d{d}_K{K}_r{rank}", n, rank * (d + K), r, c, 4, gamma, rounds, "lora_softmax",
+               problems.lora_softmax(n, d, K, rank, samples, seed), 0.5, 0.05, seed, batch=batch, samples=samples, tol=2e-3,
+               extra={"d": d, "K": K, "rank": rank, "scale": 2.0 / rank})
+
+
 CONFIGS = [config0, config1, config2, config3, config4]

@@ -28,6 +28,8 @@ def make_gpu(w, device="cuda:0"):
         d0 = torch.from_numpy(d["Xb"].view(np.int16)).view(torch.bfloat16)
         d1 = torch.from_numpy(d["labels"])
         kw = dict(samples=d["Xb"].shape[1], batch=w.sched.batch, d=w.extra["d"], K=w.extra["K"])
+        if w.objective == "lora_softmax":
+            kw.update(rank=w.extra["rank"], adapter_scale=w.extra["scale"], data2=torch.from_numpy(d["W0"].view(np.int16)).view(torch.bfloat16))
     return RFast(w.n, w.p, csr(w.R), csr(w.C), w.D, w.burst, w.objective, d0, d1, device=device, **kw)
 
 

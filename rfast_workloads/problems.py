@@ -99,3 +99,14 @@ def softmax_pool(n: int, d: int, K: int, samples: int, seed: int, alpha: float =
         Xb[i] = to_bf16_bits(f32(xi))
         lab[i] = li
     return {"Xb": Xb, "labels": lab, "mu": mu}
+
+
+def lora_softmax(n: int, d: int, K: int, rank: int, samples: int, seed: int):
+    """The pool of softmax_pool, a frozen projection W0 ~ N(0, 1/d) in bf16, and starting points x0 [n][rank (d + K)]: A ~ N(0, 1/d),
+    B ~ N(0, 1/rank)/4 of every node (with B = 0 nothing would be pushed to A, with A = B = 0 nothing at all)."""
+    pool = softmax_pool(n, d, K, samples, seed)
+    rng = _rng(seed, 14)
+    w0 = to_bf16_bits(f32(rng.standard_normal((K, d)) / np.sqrt(d)))
+    a = rng.standard_normal((n, rank * d)) / np.sqrt(d)
+    b = rng.standard_normal((n, K * rank)) / (4.0 * np.sqrt(rank))
+    return {**pool, "W0": w0, "x0": f32(np.concatenate([a, b], axis=1))}

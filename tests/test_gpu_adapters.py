@@ -1,0 +1,335 @@
+"""GPU parity of rounds with the adapter objective and of the AdamW variant, on every way a round comes in."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import harness  # noqa: E402
+from oracle.from_workload import make_oracle  # noqa: E402
+from oracle.push_pull import PushPullOracle  # noqa: E402
+from oracle.rfast_oracle import RFastOracle  # noqa: E402
+from paper_2307_11617_amd import RFastError, rfast_diagnostics_static, rfast_set_adamw  # noqa: E402
+from rfast_workloads import configs, graphs, problems  # noqa: E402
+from rfast_workloads.schedule import ScheduleSpec  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+B1, B2, EPS = 0.9, 0.999, 1e-8
+
+
+def adapters(**kw):
+    w = configs.adapters(**kw)
+    return w, w.data["x0"]
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n=5, d=37, K=11, rank=3, samples=50, batch=0), dict(n=3, d=130, K=70, rank=17, samples=90, batch=33),
+                                dict(n=12, d=128, K=128, rank=8, samples=300, batch=96), dict(n=4, d=64, K=10, rank=64, samples=40, batch=8),
+                                dict(n=2, d=8, K=2, rank=1, samples=9, batch=3)])
+def test_adapter_rounds(kw):
+    w, x0 = adapters(**kw)
+    worst, orc, gpu = harness.run_parity(w, 60, every=20, x0=x0)
+    print(f"\n[{w.name}] worst {worst}")
+    d, ref = gpu.diagnostics(), orc.diagnostics()
+    # the node averages agree to w.tol, and bf16 of them nearly everywhere: two roundings of 2^-8 each at most
+    assert abs(d["loss_at_xbar"] - ref["loss_at_xbar"]) <= 1e-2 * abs(ref["loss_at_xbar"])
+    assert d["conservation_sq"] <= 1e-8 * max(d["gsum_sq"], 1.0)
+    out = torch.zeros(6, dtype=torch.float64, device="cuda:0")
+    rfast_diagnostics_static(gpu.ctx, None, out)
+    torch.cuda.synchronize()
+    assert out[5].item() == d["loss_at_xbar"]
+
+
+def test_adapter_rounds_with_momentum_and_decay():
+    w, x0 = adapters(n=6, d=96, K=20, rank=5, samples=80, batch=40)
+    harness.run_parity(w, 80, every=40, x0=x0, momentum=0.9, weight_decay=1e-2, gamma_schedule=(30, 0.5))
+
+
+def test_adapter_gradient_of_given_points():
+    """g at x0 of every node, full local data, against the oracle, elementwise; labels out of range are rows without loss."""
+    w, x0 = adapters(n=7, d=72, K=19, rank=6, samples=77, batch=0)
+    w.data["labels"][2, 5:9] = -1
+    w.data["labels"][3, :] = 19
+    orc, gpu = make_oracle(w, x0=x0), harness.make_gpu(w)
+    gpu.init(x0, None)
+    got = gpu.read("G")
+    gpu.check()
+    # E is bf16 on both sides, decided in fp32 here: an entry next to a tie goes the other way, 2^-8 of itself; all sums in fp32
+    for i in range(w.n):
+        top = np.abs(orc.g[i]).max()
+        assert np.abs(got[i] - orc.g[i]).max() <= 2.0 ** -9 * top + 1e-7, i
+    assert not got[3].any()
+    assert harness.rel_l2(got, orc.g) <= 1e-4
+
+
+def test_adapter_sample_rows_out_of_range_are_reported():
+    w, x0 = adapters(n=4, samples=40, batch=8)
+    gpu = harness.make_gpu(w)
+    bad = w.sched.initial_batch().copy()
+    bad[2, 3] = 40
+    gpu.init(x0, bad)
+    with pytest.raises(RFastError, match="-4"):
+        gpu.check()
+
+
+def test_adapter_rounds_generated_events_graphs_and_single_calls():
+    """The same schedule by any entry point gives the same bits."""
+    w, x0 = adapters(n=8, d=64, K=24, rank=4, samples=64, batch=16)
+    p_active = torch.full((w.n,), 0.6, device="cuda:0")
+
+    def run(graphs_on, calls):
+        gpu = harness.make_gpu(w)
+        gpu.init(x0, w.sched.initial_batch())
+        from paper_2307_11617_amd import rfast_use_graphs
+        rfast_use_graphs(gpu.ctx, graphs_on)
+        for c in calls:
+            gpu.run_generated(c, 77, p_active, 3, 0.1, 0.2)
+        gpu.check()
+        return gpu.read("X"), gpu.read("Z")
+
+    a = run(False, [40])
+    for graphs_on, calls in ((True, [40]), (True, [20, 20]), (False, [1] * 40)):
+        b = run(graphs_on, calls)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+    gpu = harness.make_gpu(w)
+    gpu.init(x0, w.sched.initial_batch())
+    gpu.run_events(30, 5, None, 3, 0.1, 0.2)
+    gpu.check()
+    assert int(gpu.read("ROUND")[0]) == 30 and np.isfinite(gpu.read("X")).all() and gpu.read("T_NODE").sum() == 30
+
+
+def test_adapter_workload_is_refused_where_it_does_not_fit():
+    for kw in (dict(rank=0), dict(rank=65)):
+        with pytest.raises((RFastError, ZeroDivisionError)):
+            harness.make_gpu(configs.adapters(n=3, samples=20, batch=4, **kw))
+    w, _ = adapters(n=3, samples=20, batch=4)
+    w.p += 1
+    with pytest.raises(RFastError):
+        harness.make_gpu(w)
+    w.p -= 1
+    w.data["W0"] = w.data["W0"][:, :-1].copy()
+    with pytest.raises(RFastError):
+        harness.make_gpu(w)
+
+
+# ---------------------------------------------------------------------------------------------------------- AdamW variant
+class AdamwOracle(RFastOracle):
+    def __init__(self, *a, decay=0.0, **kw):
+        super().__init__(*a, **kw)
+        self.am, self.av, self.decay, self.momentum = np.zeros_like(self.x), np.zeros_like(self.x), decay, 1.0
+
+    def direction(self, i):
+        t = int(self.t[i]) + 1
+        self.am[i] = B1 * self.am[i] + (1 - B1) * self.z[i]
+        self.av[i] = B2 * self.av[i] + (1 - B2) * self.z[i] ** 2
+        return self.am[i] / (1 - B1 ** t) / (np.sqrt(self.av[i] / (1 - B2 ** t)) + EPS) + self.decay * self.x[i]
+
+    def activate(self, i, *a, **kw):
+        self.m[i] = self.direction(i) - self.z[i]  # S1 takes m + z with momentum 1
+        super().activate(i, *a, **kw)
+
+
+class AdamwPushPull(PushPullOracle):
+    def __init__(self, *a, decay=0.0, **kw):
+        super().__init__(*a, **kw)
+        self.am, self.av, self.decay, self.momentum = np.zeros_like(self.x), np.zeros_like(self.x), decay, 1.0
+
+    def step(self, gamma, batch=None):
+        t = self.t + 1
+        self.am = B1 * self.am + (1 - B1) * self.z
+        self.av = B2 * self.av + (1 - B2) * self.z ** 2
+        self.m = self.am / (1 - B1 ** t) / (np.sqrt(self.av / (1 - B2 ** t)) + EPS) + self.decay * self.x - self.z
+        super().step(gamma, batch)
+
+
+def quad(n, p, seed, gamma=0.02):
+    rng = np.random.default_rng(seed)
+    wr, wc = graphs.random_digraph(n, rng, extra=0.5)
+    R, C = graphs.from_dense(wr), graphs.from_dense(wc)
+    sched = ScheduleSpec(n, R.nnz_off, C.nnz_off, np.full(n, 0.6), 3, 0.2, seed=seed)
+    return configs.Workload(f"adamw_n{n}_p{p}", n, p, R, C, 5, 3, gamma, 0, "diag_quadratic", problems.diag_quadratic(n, p, seed), sched,
+                            0.05, 99 + seed, 1e-4)
+
+
+def oracle_of(w, cls, x0, decay):
+    plain = make_oracle(w, x0=x0)
+    return cls(w.n, w.p, w.R, w.C, w.D, w.burst, plain.obj, x0=x0, batch0=w.sched.initial_batch(), decay=decay)
+
+
+@pytest.mark.parametrize("make", [lambda: quad(9, 2052, 3), lambda: quad(6, 259, 4), lambda: quad(40, 64, 5), lambda: configs.config0(rounds=0),
+                                  lambda: configs.config1(p=520, samples=256, batch=32, rounds=0),
+                                  lambda: configs.config4(d=64, K=32, samples=128, batch=64, rounds=0),
+                                  lambda: configs.adapters(n=6, d=48, K=16, rank=4)])
+def test_adamw_rounds(make):
+    """32-bit moments, several rounds per call, against the oracle.  The direction m / sqrt(v) has size one wherever z is, so what the two sides differ
+    by is of the step size's order at most where z is next to nothing: norms of x, gamma and w.tol as in the other parity tests."""
+    w = make()
+    w.gamma = 1e-2
+    x0 = w.data.get("x0", np.random.default_rng(1).standard_normal((w.n, w.p)).astype(np.float32))
+    orc, gpu = oracle_of(w, AdamwOracle, x0, 0.01), harness.make_gpu(w)
+    gpu.set_adamw((B1, B2), EPS, 0.01)
+    gpu.init(x0, w.sched.initial_batch())
+    for r0, r1 in ((0, 1), (1, 30), (30, 60)):
+        st, dev = harness.upload_chunk(gpu, w, r0, r1)
+        gpu.run(r1 - r0, dev["active"], dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, dev["batch_idx"])
+        for k in range(r1 - r0):
+            orc.round(st["active"][k], st["delay_R"][k], st["delay_C"][k], st["drop_R"][k], st["drop_C"][k], w.gamma,
+                      None if st["batch_idx"] is None else st["batch_idx"][k])
+        gpu.check()
+        assert np.array_equal(gpu.read("T_NODE"), orc.slots()["t"])
+        tol = 10 * w.tol
+        for name, ref, floor in (("X", orc.x, 0.0), ("Z", orc.z, 1e-3 * np.linalg.norm(orc.g)), ("ADAMW_M", orc.am, 1e-3 * np.linalg.norm(orc.g)),
+                                 ("ADAMW_V", orc.av, 1e-6 * np.linalg.norm(orc.g) ** 2)):
+            err = harness.rel_l2(gpu.read(name), ref, floor)
+            assert err <= tol, (name, r1, err)
+
+
+def half_step(value, scale):
+    return 2.0 ** -4 * np.abs(value) + 2.0 ** -9 * scale
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("p", [1024, 1030, 255])
+def test_adamw_round_by_round(bits, p):
+    """Each round from the library's own state before it: the published v = x - gamma direction and the moments, elementwise."""
+    w = quad(7, p, 11, gamma=0.05)
+    gpu = harness.make_gpu(w)
+    gpu.set_adamw((B1, B2), EPS, 0.1, bits)
+    gpu.init(np.random.default_rng(2).standard_normal((w.n, p)).astype(np.float32), None)
+    blocks = (p + 255) // 256
+
+    def held():
+        m, v = gpu.read("ADAMW_M"), gpu.read("ADAMW_V")
+        if bits == 32:
+            return m.astype(np.float64), v.astype(np.float64), None, None
+        wide = lambda s: np.repeat(s, 256, axis=1)[:, :p].astype(np.float64)  # noqa: E731
+        value = lambda c: torch.from_numpy(c).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)  # noqa: E731
+        sm, sv = wide(gpu.read("ADAMW_M_SCALE")), wide(gpu.read("ADAMW_V_SCALE"))
+        return value(m) * sm, (value(v) * sv) ** 2, sm, sv
+
+    assert gpu._shape("ADAMW_M")[0] == (w.n, p) and (bits == 32 or gpu.read("ADAMW_M_SCALE").shape == (w.n, blocks))
+    for r in range(12):
+        x, z, t = gpu.read("X").astype(np.float64), gpu.read("Z").astype(np.float64), gpu.read("T_NODE")
+        m0, v0, _, _ = held()
+        st, dev = harness.upload_chunk(gpu, w, r, r + 1)
+        gpu.run(1, dev["active"], dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, None)
+        gpu.check()
+        m1, v1, sm, sv = held()
+        ring = gpu.read("V_RING")
+        out = {j for i in range(w.n) for j in w.R.col[w.R.rowptr[i]:w.R.rowptr[i + 1]] if j != i}
+        for i in range(w.n):
+            if not st["active"][0][i]:
+                assert np.array_equal(m0[i], m1[i]) and np.array_equal(v0[i], v1[i])
+                continue
+            m, v = B1 * m0[i] + (1 - B1) * z[i], B2 * v0[i] + (1 - B2) * z[i] ** 2
+            k = t[i] + 1
+            d = m / (1 - B1 ** k) / (np.sqrt(v / (1 - B2 ** k)) + EPS) + 0.1 * x[i]
+            u = 2.0 ** -24
+            me = 4 * u * (B1 * np.abs(m0[i]) + (1 - B1) * np.abs(z[i])) + 1e-40
+            ve = 6 * u * v + 1e-40
+            den = np.sqrt(v / (1 - B2 ** k)) + EPS
+            if i in out:
+                err = w.gamma * (20 * u * np.abs(d) + 20 * u * np.abs(m) / (1 - B1 ** k) / den + me / (1 - B1 ** k) / den) + 4 * u * np.abs(x[i])
+                got = ring[i, k % (w.D + 2)].astype(np.float64)
+                assert (np.abs(got - (x[i] - w.gamma * d)) <= err).all(), (r, i)
+            if bits == 32:
+                assert (np.abs(m1[i] - m) <= me).all() and (np.abs(v1[i] - v) <= ve).all()
+            else:
+                assert (np.abs(m1[i] - m) <= half_step(m, sm[i]) + 2 * me + 8 * u * np.abs(m)).all()
+                root = np.sqrt(v)
+                assert (np.abs(np.sqrt(v1[i]) - root) <= half_step(root, sv[i]) + 8 * u * root).all() and (v1[i][v > 0] > 0).all()
+
+
+@pytest.mark.parametrize("p", [2048, 515])
+def test_adamw_synchronous_steps(p):
+    w = configs.config2(p=p, rounds=0)
+    w.gamma = 1e-2
+    x0 = np.random.default_rng(0).standard_normal((w.n, p)).astype(np.float32)
+    plain, gpu = make_oracle(w, x0=x0), harness.make_gpu(w)
+    orc = AdamwPushPull(w.R.dense(), w.C.dense(), plain.obj, x0=x0, decay=0.05)
+    gpu.set_adamw((B1, B2), EPS, 0.05)
+    gpu.init(x0, None)
+    for steps in (1, 1, 20, 3):
+        gpu.sync_run(steps, w.gamma)
+        for _ in range(steps):
+            orc.step(w.gamma)
+        assert harness.rel_l2(gpu.read("X"), orc.x) <= 10 * w.tol and harness.rel_l2(gpu.read("ADAMW_V"), orc.av) <= 10 * w.tol
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_entry_points_agree_and_checkpoints_resume(bits):
+    """Calls of any length, replayed graphs and a restored checkpoint give the same bits; so does the first call after another variant."""
+    w, x0 = adapters(n=6, d=40, K=12, rank=3, samples=40, batch=8)
+    p_active = torch.full((w.n,), 0.7, device="cuda:0")
+    from paper_2307_11617_amd import rfast_use_graphs
+
+    def start(graphs_on=False, other=False):
+        gpu = harness.make_gpu(w)
+        if other:
+            gpu.set_optimizer(0.9, 0.01)
+            gpu.init(x0, w.sched.initial_batch())
+            gpu.run_generated(20, 9, p_active, 2, 0.1, 1e-2)
+        gpu.set_adamw((B1, B2), EPS, 0.01, bits)
+        with pytest.raises(RFastError):
+            gpu.run_generated(1, 9, p_active, 2, 0.1, 1e-2)   # init must follow
+        gpu.init(x0, w.sched.initial_batch())
+        rfast_use_graphs(gpu.ctx, graphs_on)
+        return gpu
+
+    def state(gpu):
+        gpu.check()
+        return [gpu.read(f) for f in ("X", "Z", *[f for f in gpu._checkpoint_fields() if f.startswith("ADAMW")])]
+
+    ref = start()
+    ref.run_generated(48, 9, p_active, 2, 0.1, 1e-2)
+    want = state(ref)
+    for gpu, calls in ((start(), [1, 7, 40]), (start(True), [48]), (start(True), [32, 16]), (start(other=True), [48])):
+        for c in calls:
+            gpu.run_generated(c, 9, p_active, 2, 0.1, 1e-2)
+        for a, b in zip(want, state(gpu)):
+            assert np.array_equal(a, b)
+    half = start()
+    half.run_generated(30, 9, p_active, 2, 0.1, 1e-2)
+    ck = half.checkpoint()
+    assert "ADAMW_M" in ck and ("ADAMW_V_SCALE" in ck) == (bits == 8) and "MOMENTUM" not in ck
+    later = start()
+    later.restore(ck)
+    later.run_generated(18, 9, p_active, 2, 0.1, 1e-2)
+    for a, b in zip(want, state(later)):
+        assert np.array_equal(a, b)
+    with pytest.raises(RFastError):
+        later.read("MOMENTUM")
+    # and back: the plain method again
+    later.set_optimizer()
+    later.init(x0, w.sched.initial_batch())
+    plain = harness.make_gpu(w)
+    plain.init(x0, w.sched.initial_batch())
+    for g in (later, plain):
+        g.run_generated(10, 9, p_active, 2, 0.1, 1e-2)
+    assert np.array_equal(later.read("X"), plain.read("X"))
+    with pytest.raises(RFastError):
+        later.read("ADAMW_M")
+
+
+def test_adamw_events():
+    w = quad(8, 512, 21)
+    a, b = harness.make_gpu(w), harness.make_gpu(w)
+    for g in (a, b):
+        g.set_adamw()
+        g.init(None, None)
+    a.run_events(40, 3, None, 2, 0.1, 1e-2)
+    for _ in range(40):
+        b.run_events(1, 3, None, 2, 0.1, 1e-2)
+    a.check()
+    assert np.array_equal(a.read("X"), b.read("X")) and a.read("T_NODE").sum() == 40
+
+
+def test_adamw_refusals():
+    w = quad(3, 64, 1)
+    gpu = harness.make_gpu(w)
+    state = torch.empty(1 << 16, dtype=torch.uint8, device="cuda:0")
+    for args in ((1.0, 0.9, 1e-8, 0.0, 32), (0.9, -1.0, 1e-8, 0.0, 32), (0.9, 0.9, 0.0, 0.0, 32), (0.9, 0.9, 1e-8, -1.0, 32), (0.9, 0.9, 1e-8, 0.0, 16)):
+        with pytest.raises(RFastError):
+            rfast_set_adamw(gpu.ctx, *args, state)
+    for s in (None, state[:100], state[4:]):
+        with pytest.raises(RFastError):
+            rfast_set_adamw(gpu.ctx, 0.9, 0.9, 1e-8, 0.0, 32, s)
+    gpu.init(None, None)  # nothing of the refused calls stays
+    gpu.sync_run(1, 0.1)
