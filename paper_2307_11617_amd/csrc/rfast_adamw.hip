@@ -55,6 +55,16 @@ struct Args {
 // beta^t from log(beta) without the cancellation of 1 - beta^t
 __device__ inline double one_less_power(double log_beta, int t) { return -expm1((double)t * log_beta); }
 
+// a / b to about one unit in the last place: the step is not carried on like the moments, whose bits decide codes, and a division that
+// is rounded correctly takes twice the instructions.  (b is at least eps and no denormal for any eps that has a use; where its reciprocal is
+// not finite or zero, so is the quotient to fp32.)
+__device__ inline float over(float a, float b) {
+  const float r = __builtin_amdgcn_rcpf(b);
+  const float q = a * r;
+  const float e = fmaf(-q, b, a);
+  return fabsf(e) < INFINITY ? fmaf(e, r, q) : q;
+}
+
 __device__ inline float finite_magnitude(float v) {
   const float a = fabsf(v);
   return a < INFINITY ? a : 0.f;  // false for NaN too
@@ -86,10 +96,7 @@ __device__ inline void values_of(uint32_t w, float scale, float* v) {
 
 typedef unsigned int any_u32 __attribute__((aligned(1)));
 template <bool STREAM> __device__ inline uint32_t load_codes(const uint8_t* p, int64_t left) {
-  if (left >= 4) {
-    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const any_u32*>(p));
-    else return *reinterpret_cast<const any_u32*>(p);
-  }
+  if (left >= 4) return wide_load<any_u32, STREAM>(p);
   uint32_t w = 0;
   for (int j = 0; j < 4; ++j)
     if (j < left) w |= (uint32_t)p[j] << (8 * j);
@@ -97,8 +104,7 @@ template <bool STREAM> __device__ inline uint32_t load_codes(const uint8_t* p, i
 }
 template <bool STREAM> __device__ inline void store_codes(uint8_t* p, int64_t left, uint32_t w) {
   if (left >= 4) {
-    if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<any_u32*>(p));
-    else *reinterpret_cast<any_u32*>(p) = w;
+    wide_store<any_u32, STREAM>(p, w);
     return;
   }
   for (int j = 0; j < 4; ++j)
@@ -122,8 +128,8 @@ template <int BITS, bool STREAM> struct Moments {
       if (left > 0) {
         cm = load_codes<STREAM>((const uint8_t*)pm + k, left);
         cv = load_codes<STREAM>((const uint8_t*)pv + k, left);
-        sm = ms[k / kBlock];
-        sv = vs[k / kBlock];
+        sm = wide_load<float, false>(ms + k / kBlock);
+        sv = wide_load<float, false>(vs + k / kBlock);
       }
     }
   }
@@ -169,54 +175,62 @@ template <int BITS, bool STREAM> struct Moments {
   }
 };
 
-// U: slices of a chunk, whose loads are all under way before the first is used
+// Slices of a chunk of row r, this lane's coordinates from k0 on.  WHOLE: all of them exist, and their loads go out together without a condition;
+// else each is looked at on its own.
+template <class P, class G, int BITS, int U, bool STREAM, bool WHOLE>
+__device__ inline void step_chunk(const Args& a, const Row& r, int t, int64_t k0) {
+  Moments<BITS, STREAM> state[U];
+  float p[U][4], g[U][4];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t k = k0 + u * kSlice, left = WHOLE ? 4 : r.count - k;
+    if (left > 0) {
+      load_four<STREAM>((const P*)r.param + k, left, p[u]);
+      load_four<STREAM>((const G*)r.grad + k, left, g[u]);
+    }
+    state[u].read(r.m, r.v, r.m_scale, r.v_scale, k, left);
+  }
+  const float first = (float)(a.gamma / one_less_power(a.log_beta1, t));
+  const float second = (float)(1.0 / sqrt(one_less_power(a.log_beta2, t)));
+  const float keep = (float)(1.0 - a.gamma * r.decay);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t k = k0 + u * kSlice, left = WHOLE ? 4 : r.count - k;
+    float root[4];
+    state[u].step(g[u], a.beta1, a.rest1, a.beta2, a.rest2, root);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[u][j] = p[u][j] * keep - over(state[u].m[j] * first, root[j] * second + a.eps);
+    if (left > 0) {
+      store_four<STREAM>((P*)r.param + k, left, p[u]);
+      if (r.copy) store_four<STREAM>(r.copy + k, left, p[u]);
+    }
+    state[u].write(r.m, r.v, r.m_scale, r.v_scale, k, left, root);
+  }
+}
+
 template <class P, class G, int BITS, int U, bool STREAM>
 __global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
     const int i = __builtin_amdgcn_readfirstlane(a.whose[chunk]);
     if (a.active && a.active[i] == 0) continue;
     const Row r = a.rows[i];
     const int t = a.steps[i] + 1;
-    const int64_t k0 = (chunk - r.first) * (U * kSlice) + wave * kBlock + lane * 4;
-    Moments<BITS, STREAM> state[U];
-    float p[U][4], g[U][4];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + u * kSlice, left = r.count - k;
-      if (left > 0) {
-        load_four<STREAM>((const P*)r.param + k, left, p[u]);
-        load_four<STREAM>((const G*)r.grad + k, left, g[u]);
-      }
-      state[u].read(r.m, r.v, r.m_scale, r.v_scale, k, left);
-    }
-    const float first = (float)(a.gamma / one_less_power(a.log_beta1, t));
-    const float second = (float)(1.0 / sqrt(one_less_power(a.log_beta2, t)));
-    const float keep = (float)(1.0 - a.gamma * r.decay);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + u * kSlice, left = r.count - k;
-      float root[4];
-      state[u].step(g[u], a.beta1, a.rest1, a.beta2, a.rest2, root);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[u][j] = p[u][j] * keep - (state[u].m[j] * first) / (root[j] * second + a.eps);
-      if (left > 0) {
-        store_four<STREAM>((P*)r.param + k, left, p[u]);
-        if (r.copy) store_four<STREAM>(r.copy + k, left, p[u]);
-      }
-      state[u].write(r.m, r.v, r.m_scale, r.v_scale, k, left, root);
-    }
+    const int64_t begin = (chunk - r.first) * (U * kSlice), k0 = begin + threadIdx.x * 4;
+    if (begin + U * kSlice <= r.count) step_chunk<P, G, BITS, U, STREAM, true>(a, r, t, k0);
+    else step_chunk<P, G, BITS, U, STREAM, false>(a, r, t, k0);
   }
-  // The last workgroup moves the counters on.  (No workgroup reads them any more: each has read them before it counts itself.)
+  // The last workgroup moves the counters on.  No workgroup reads them any more: each has used what it read before it counts itself,
+  // and nothing else is handed over, so the words need no ordering of memory (a release across the eight L2s writes them back:
+  // with it, 256 small tensors took 48 us instead of XX).
   __shared__ bool last;
   __syncthreads();
   if (threadIdx.x == 0) {
     const unsigned group = blockIdx.x % kGroups;
     const unsigned in_group = (gridDim.x - group + kGroups - 1) / kGroups, groups = gridDim.x < kGroups ? gridDim.x : kGroups;
     last = false;
-    if (__hip_atomic_fetch_add(a.through + group * 16, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == in_group - 1) {
+    if (__hip_atomic_fetch_add(a.through + group * 16, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == in_group - 1) {
       __hip_atomic_store(a.through + group * 16, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (__hip_atomic_fetch_add(a.through + kGroups * 16, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups - 1) {
+      if (__hip_atomic_fetch_add(a.through + kGroups * 16, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1) {
         __hip_atomic_store(a.through + kGroups * 16, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         last = true;
       }
@@ -273,7 +287,7 @@ template <int BITS> __global__ void __launch_bounds__(kThreads) rfast_adamw_roun
   const float second = (float)(1.0 / sqrt(one_less_power(a.log_beta2, t)));
   state.step(g, a.beta1, a.rest1, a.beta2, a.rest2, root);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = (state.m[j] * first) / (root[j] * second + a.eps) + a.decay * x[j];
+  for (int j = 0; j < 4; ++j) x[j] = over(state.m[j] * first, root[j] * second + a.eps) + a.decay * x[j];
   if (left > 0) store_four<false>(a.dir + row + k, left, x);
   state.write(m, v, ms, vs, k, left, root);
 }

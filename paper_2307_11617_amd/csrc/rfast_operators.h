@@ -24,12 +24,23 @@ __device__ inline float from_bf16(u16 b) { return __uint_as_float((uint32_t)b <<
 __device__ inline u16 to_bf16(float f) { return __builtin_bit_cast(u16, (__bf16)f); }
 __device__ inline uint32_t to_bf16_pair(float a, float b) { return to_bf16(a) | ((uint32_t)to_bf16(b) << 16); }
 
+// (pointers that come out of a table in memory would be taken for ones of any address space)
+#define RFAST_GLOBAL __attribute__((address_space(1)))
+template <class V, bool STREAM> __device__ inline V wide_load(const void* p) {
+  const RFAST_GLOBAL V* g = (const RFAST_GLOBAL V*)(uintptr_t)p;
+  if constexpr (STREAM) return __builtin_nontemporal_load(g);
+  else return *g;
+}
+template <class V, bool STREAM> __device__ inline void wide_store(void* p, V v) {
+  RFAST_GLOBAL V* g = (RFAST_GLOBAL V*)(uintptr_t)p;
+  if constexpr (STREAM) __builtin_nontemporal_store(v, g);
+  else *g = v;
+}
+
 // Four neighbours of an array of `T` (float or u16 = bf16) from p on, as floats; `left` (1 or more) of them exist.
 template <bool STREAM> __device__ inline void load_four(const float* p, int64_t left, float* v) {
   if (left >= 4) {
-    any_f32x4 t;
-    if constexpr (STREAM) t = __builtin_nontemporal_load(reinterpret_cast<const any_f32x4*>(p));
-    else t = *reinterpret_cast<const any_f32x4*>(p);
+    const any_f32x4 t = wide_load<any_f32x4, STREAM>(p);
     v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
   } else {
     for (int j = 0; j < 4; ++j) v[j] = j < left ? p[j] : 0.f;
@@ -37,9 +48,7 @@ template <bool STREAM> __device__ inline void load_four(const float* p, int64_t 
 }
 template <bool STREAM> __device__ inline void load_four(const u16* p, int64_t left, float* v) {
   if (left >= 4) {
-    any_u32x2 t;
-    if constexpr (STREAM) t = __builtin_nontemporal_load(reinterpret_cast<const any_u32x2*>(p));
-    else t = *reinterpret_cast<const any_u32x2*>(p);
+    const any_u32x2 t = wide_load<any_u32x2, STREAM>(p);
     v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xFFFF0000u);
     v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xFFFF0000u);
   } else {
@@ -49,8 +58,7 @@ template <bool STREAM> __device__ inline void load_four(const u16* p, int64_t le
 template <bool STREAM> __device__ inline void store_four(float* p, int64_t left, const float* v) {
   if (left >= 4) {
     const any_f32x4 t = {v[0], v[1], v[2], v[3]};
-    if constexpr (STREAM) __builtin_nontemporal_store(t, reinterpret_cast<any_f32x4*>(p));
-    else *reinterpret_cast<any_f32x4*>(p) = t;
+    wide_store<any_f32x4, STREAM>(p, t);
   } else {
     for (int j = 0; j < 4; ++j)
       if (j < left) p[j] = v[j];
@@ -59,8 +67,7 @@ template <bool STREAM> __device__ inline void store_four(float* p, int64_t left,
 template <bool STREAM> __device__ inline void store_four(u16* p, int64_t left, const float* v) {
   if (left >= 4) {
     const any_u32x2 t = {to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3])};
-    if constexpr (STREAM) __builtin_nontemporal_store(t, reinterpret_cast<any_u32x2*>(p));
-    else *reinterpret_cast<any_u32x2*>(p) = t;
+    wide_store<any_u32x2, STREAM>(p, t);
   } else {
     for (int j = 0; j < 4; ++j)
       if (j < left) p[j] = to_bf16(v[j]);

@@ -25,49 +25,54 @@ struct Args {
   float scale;
 };
 
-template <class T> constexpr int kGroup = 16 / (int)sizeof(T);  // logits per 16-byte load
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
-// A group of logits from p on, of which `left` (1 or more) exist; the others are classes that are masked out.
-__device__ inline void load_group(const float* p, int left, float* v) {
-  if (left >= 4) load_four<false>(p, 4, v);
-  else
+// A group of neighbouring logits: what a 16-byte load holds.
+template <class T> struct Group;
+template <> struct Group<float> {
+  static constexpr int N = 4;
+  any_f32x4 raw;
+  __device__ void load(const float* p) { raw = *reinterpret_cast<const any_f32x4*>(p); }
+  __device__ void load(const float* p, int left) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = q < left ? p[q] : -INFINITY;
-}
-__device__ inline void load_group(const u16* p, int left, float* v) {
-  if (left >= 8) {
-    const any_u32x4 t = *reinterpret_cast<const any_u32x4*>(p);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[2 * q] = __uint_as_float(t[q] << 16);
-      v[2 * q + 1] = __uint_as_float(t[q] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = q < left ? from_bf16(p[q]) : -INFINITY;
+    for (int j = 0; j < N; ++j) raw[j] = j < left ? p[j] : -INFINITY;
   }
-}
-template <int N> __device__ inline void store_group(float* p, int left, const float* v) {
+  __device__ float at(int j) const { return raw[j]; }
+};
+template <> struct Group<u16> {
+  static constexpr int N = 8;
+  any_u32x4 raw;
+  __device__ void load(const u16* p) { raw = *reinterpret_cast<const any_u32x4*>(p); }
+  __device__ void load(const u16* p, int left) {
 #pragma unroll
-  for (int q = 0; q < N; q += 4)
-    if (left > q) store_four<false>(p + q, left - q, v + q);
+    for (int j = 0; j < N; j += 2) raw[j >> 1] = (j < left ? p[j] : 0xFF80u) | (uint32_t)(j + 1 < left ? p[j + 1] : 0xFF80u) << 16;
+  }
+  __device__ float at(int j) const { return __uint_as_float(j & 1 ? raw[j >> 1] & 0xFFFF0000u : raw[j >> 1] << 16); }
+};
+template <int N> __device__ inline void store_group(float* p, const float* v) {
+#pragma unroll
+  for (int q = 0; q < N; q += 4) store_four<false>(p + q, 4, v + q);
 }
-template <int N> __device__ inline void store_group(u16* p, int left, const float* v) {
+template <int N> __device__ inline void store_group(u16* p, const float* v) {
   if constexpr (N == 8) {
-    if (left >= 8) {
-      const any_u32x4 t = {to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3]), to_bf16_pair(v[4], v[5]), to_bf16_pair(v[6], v[7])};
-      *reinterpret_cast<any_u32x4*>(p) = t;
-      return;
-    }
+    const any_u32x4 t = {to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3]), to_bf16_pair(v[4], v[5]), to_bf16_pair(v[6], v[7])};
+    *reinterpret_cast<any_u32x4*>(p) = t;
+  } else {
+    store_four<false>(p, 4, v);
   }
-#pragma unroll
-  for (int q = 0; q < N; q += 4)
-    if (left > q) store_four<false>(p + q, left - q, v + q);
 }
 
-// over the row's lanes: those of a wavefront, or of the workgroup through `box` (two arrays used in turn)
+// Over the row's lanes: LANES neighbours of a wavefront, or a workgroup's through `box`.
 template <int LANES, class F> __device__ inline float row_reduce(float v, float* box, F f) {
-  v = wave_reduce(v, f);
+  if constexpr (LANES >= 64) {
+    v = wave_reduce(v, f);
+  } else {
+    v = f(v, lane_of<0xB1>(v));
+    v = f(v, lane_of<0x4E>(v));
+    v = f(v, lane_of<0x141>(v));
+    if constexpr (LANES >= 16) v = f(v, lane_of<0x140>(v));
+    if constexpr (LANES >= 32) v = f(v, __shfl_xor(v, 16, 64));
+  }
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -78,88 +83,112 @@ template <int LANES, class F> __device__ inline float row_reduce(float v, float*
   return v;
 }
 
-// What a row comes to, from its largest logit (-infinity: none above it) and the sum of exp(l - shift)
-struct RowEnd {
-  float lse, inverse, shift, log_sum;  // probability of l = exp(l - shift) * inverse
-};
-__device__ inline float shift_of(float top) { return top == -INFINITY ? 0.f : top; }
-__device__ inline RowEnd row_end(float shift, float sum) {
-  if (sum == 0.f) return {-INFINITY, 0.f, 0.f, 0.f};  // every class is masked out
-  const float l = logf(sum);
-  return {shift + l, 1.f / sum, shift, l};
-}
-// (not lse - l_label: beside a large shift the logarithm would lose its digits)
-__device__ inline float loss_of(const RowEnd& e, float label_logit) { return e.lse == -INFINITY ? 0.f : e.log_sum + (e.shift - label_logit); }
-__device__ inline float grad_of(const RowEnd& e, float l, bool at_label, float scale) {
-  if (e.lse == -INFINITY) return 0.f;
-  return (__expf(l - e.shift) * e.inverse - (at_label ? 1.f : 0.f)) * scale;
+// exp(l - shift).  The difference is taken before the multiplication by log2(e): in one multiply-add the largest logit of a row would not come
+// to exactly 1, nor the loss of a certain one to 0, and beside logits of 1e38 the product would overflow.
+__device__ inline float power(float l, float shift) { return __builtin_amdgcn_exp2f((l - shift) * kLog2e); }
+__device__ inline float shift_of(float top) { return top == -INFINITY ? 0.f : top; }  // (a row without a logit above -infinity: sum 0)
+// loss = log sum - (l_label - shift), not lse - l_label: beside a large shift the logarithm would lose its digits
+__device__ inline void finish_row(const Args& a, int64_t row, float shift, float sum, bool counts, float own) {
+  const float log_sum = kLn2 * __builtin_amdgcn_logf(sum);  // sum is 0, or 1 and more, or NaN
+  if (a.lse) a.lse[row] = sum == 0.f ? -INFINITY : shift + log_sum;
+  if (a.loss) a.loss[row] = !counts || sum == 0.f ? 0.f : log_sum + (shift - own);
 }
 
 template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane, int lanes) {
   for (int k = lane; k < K; k += lanes) grad[k] = (OUT)0;
 }
 
-// LANES lanes hold a row, GROUPS groups of logits each.  LANES = 64: four rows per workgroup.
+// LANES lanes hold a row, GROUPS groups of logits each.  LANES <= 64: 256 / LANES rows per workgroup.
+// The last group of a row whose length is no multiple of a group begins earlier, so that every load is a whole group without a condition
+// (a condition per load would have each of them waited for before the next is sent): the overlap is in the sum once, and its
+// gradient is written twice alike.
 template <class IN, class OUT, int LANES, int GROUPS>
-__global__ void __launch_bounds__(LANES == 64 ? 256 : LANES) rfast_xent_kernel(Args a) {
-  constexpr int N = kGroup<IN>;
+__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 1) rfast_xent_kernel(Args a) {
+  constexpr int N = Group<IN>::N, ROWS = LANES <= 64 ? 256 / LANES : 1, SPAN = LANES * N;
   __shared__ float box[2][16];
-  const int lane = LANES == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  const int64_t row = LANES == 64 ? block * 4 + (threadIdx.x >> 6) : block;
+  const int lane = threadIdx.x % LANES;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / LANES;
+  // (of a wavefront that has several rows, those past the end leave: the others' lanes only look at each other)
   if (row >= a.rows || (a.d_rows && row >= *a.d_rows)) return;
   const IN* l = (const IN*)a.logits + row * a.ld_logits;
   OUT* grad = a.grad ? (OUT*)a.grad + row * a.ld_grad : nullptr;
-  const int label = a.labels[row];
+  const int label = a.labels[row], last = a.K - N;  // last: where the last group begins (below 0: a row shorter than a group)
   const bool counts = label >= 0 && label < a.K;
   if (!counts && !a.lse) {
     if (lane == 0 && a.loss) a.loss[row] = 0.f;
     if (grad) zero_row(grad, a.K, lane, LANES);
     return;
   }
-  float v[GROUPS][N];
+  Group<IN> v[GROUPS];
+  if (LANES > 8 || GROUPS > 1 || last >= 0) {
 #pragma unroll
-  for (int q = 0; q < GROUPS; ++q) {
-    const int k = (q * LANES + lane) * N;
-    if (k < a.K) load_group(l + k, a.K - k, v[q]);
-    else
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[q][j] = -INFINITY;
+    for (int q = 0; q < GROUPS; ++q) v[q].load(l + min(q * SPAN + lane * N, last));
+  } else {
+    v[0].load(l, a.K);
   }
-  float own = 0.f;  // the label's logit, held by one lane
+  float own = 0.f;
   if (counts) own = sizeof(IN) == 4 ? ((const float*)l)[label] : from_bf16(((const u16*)l)[label]);
   float top = -INFINITY;
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q)
 #pragma unroll
-    for (int j = 0; j < N; ++j) top = fmaxf(top, v[q][j]);
+    for (int j = 0; j < N; ++j) top = fmaxf(top, v[q].at(j));
   const float shift = shift_of(row_reduce<LANES>(top, box[0], [](float x, float y) { return fmaxf(x, y); }));
+  // The compiler would keep the unpacked logits of one pass for the next, at twice the registers of the packed ones.
+  auto forget = [&] {
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) asm volatile("" : "+v"(v[q].raw));
+  };
+  forget();
   float sum = 0.f;
 #pragma unroll
-  for (int q = 0; q < GROUPS; ++q)
+  for (int q = 0; q < GROUPS; ++q) {
+    if ((q + 1) * SPAN <= a.K) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) sum += __expf(v[q][j] - shift);
-  const RowEnd e = row_end(shift, row_reduce<LANES>(sum, box[1], [](float x, float y) { return x + y; }));
-  if (lane == 0) {
-    if (a.lse) a.lse[row] = e.lse;
-    if (a.loss) a.loss[row] = counts ? loss_of(e, own) : 0.f;
+      for (int j = 0; j < N; ++j) sum += power(v[q].at(j), shift);
+    } else {
+      const int again = q * SPAN + lane * N - max(min(q * SPAN + lane * N, last), 0);  // what lanes before have
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float e = power(v[q].at(j), shift);
+        sum += j >= again ? e : 0.f;
+      }
+    }
   }
+  sum = row_reduce<LANES>(sum, box[1], [](float x, float y) { return x + y; });
+  if (lane == 0) finish_row(a, row, shift, sum, counts, own);
   if (!grad) return;
+  if (!counts || sum == 0.f) {
+    zero_row(grad, a.K, lane, LANES);
+    return;
+  }
+  const float c = a.scale / sum;
+  forget();
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q) {
-    const int k = (q * LANES + lane) * N;
-    if (k >= a.K) break;
+    const int k = q * SPAN + lane * N, at = max(min(k, last), 0);
     float g[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) g[j] = counts ? grad_of(e, v[q][j], k + j == label, a.scale) : 0.f;
-    store_group<N>(grad + k, a.K - k, g);
+    for (int j = 0; j < N; ++j) g[j] = power(v[q].at(j), shift) * c;
+    if ((unsigned)(label - at) < (unsigned)N) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) g[j] -= j == label - at ? a.scale : 0.f;
+    }
+    if (k >= a.K) continue;
+    if (LANES > 8 || GROUPS > 1 || last >= 0) {
+      store_group<N>(grad + at, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; j += 4)
+        if (a.K > j) store_four<false>(grad + j, a.K - j, g + j);
+    }
   }
 }
 
 // Rows that no workgroup's registers hold.
 template <class IN, class OUT>
 __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
-  constexpr int N = kGroup<IN>;
+  constexpr int N = Group<IN>::N, SPAN = 1024 * N;
   __shared__ float box[2][16];
   const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (row >= a.rows || (a.d_rows && row >= *a.d_rows)) return;
@@ -174,34 +203,48 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
   }
   float own = 0.f;
   if (counts) own = sizeof(IN) == 4 ? ((const float*)l)[label] : from_bf16(((const u16*)l)[label]);
-  float top = -INFINITY, sum = 0.f;  // of this lane's logits so far; sum of exp(l - shift_of(top))
-  for (int64_t k = (int64_t)threadIdx.x * N; k < a.K; k += 1024 * N) {
-    float v[N];
-    load_group(l + k, (int)(a.K - k), v);
+  // this lane's largest logit so far and its sum of exp(l - that)
+  float top = -INFINITY, sum = 0.f;
+  const int64_t first = (int64_t)threadIdx.x * N;
+  for (int64_t k = first; k < a.K; k += SPAN) {
+    Group<IN> v;
+    if (k + N <= a.K) v.load(l + k);
+    else v.load(l + k, (int)(a.K - k));
     float m = top;
 #pragma unroll
-    for (int j = 0; j < N; ++j) m = fmaxf(m, v[j]);
+    for (int j = 0; j < N; ++j) m = fmaxf(m, v.at(j));
     const float shift = shift_of(m);
-    sum *= top == -INFINITY ? 1.f : __expf(top - shift);  // (top = -infinity: the sum is 0, or NaN)
+    if (m > top) sum *= power(top, shift);  // (top = -infinity: the sum is 0, or NaN)
     top = m;
 #pragma unroll
-    for (int j = 0; j < N; ++j) sum += __expf(v[j] - shift);
+    for (int j = 0; j < N; ++j) sum += power(v.at(j), shift);
   }
   const float shift = shift_of(row_reduce<1024>(top, box[0], [](float x, float y) { return fmaxf(x, y); }));
-  sum *= top == -INFINITY ? 1.f : __expf(top - shift);
-  const RowEnd e = row_end(shift, row_reduce<1024>(sum, box[1], [](float x, float y) { return x + y; }));
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[row] = e.lse;
-    if (a.loss) a.loss[row] = counts ? loss_of(e, own) : 0.f;
-  }
+  if (shift > top) sum *= power(top, shift);
+  sum = row_reduce<1024>(sum, box[1], [](float x, float y) { return x + y; });
+  if (threadIdx.x == 0) finish_row(a, row, shift, sum, counts, own);
   if (!grad) return;
   // (where the gradient takes the logits' place, `own` has been read before any lane writes: the reductions are barriers)
-  for (int64_t k = (int64_t)threadIdx.x * N; k < a.K; k += 1024 * N) {
-    float v[N], g[N];
-    load_group(l + k, (int)(a.K - k), v);
+  if (!counts || sum == 0.f) {
+    zero_row(grad, a.K, threadIdx.x, 1024);
+    return;
+  }
+  const float c = a.scale / sum;
+  for (int64_t k = first; k < a.K; k += SPAN) {
+    Group<IN> v;
+    const bool whole = k + N <= a.K;
+    if (whole) v.load(l + k);
+    else v.load(l + k, (int)(a.K - k));
+    float g[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) g[j] = counts ? grad_of(e, v[j], k + j == label, a.scale) : 0.f;
-    store_group<N>(grad + k, (int)(a.K - k), g);
+    for (int j = 0; j < N; ++j) g[j] = power(v.at(j), shift) * c - (k + j == label ? a.scale : 0.f);
+    if (whole) {
+      store_group<N>(grad + k, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; j += 4)
+        if (a.K - k > j) store_four<false>(grad + k + j, a.K - k - j, g + j);
+    }
   }
 }
 
@@ -211,22 +254,31 @@ dim3 grid_of(int64_t blocks) {  // a dimension of a launch has fewer than 2^32 l
 }
 
 template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
-  constexpr int N = kGroup<IN>;
+  constexpr int N = Group<IN>::N;
   const auto go = [&](auto lanes, auto groups) {
-    constexpr int L = decltype(lanes)::value, G = decltype(groups)::value;
-    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G>), grid_of(L == 64 ? ((int64_t)a.rows + 3) / 4 : a.rows), dim3(L == 64 ? 256 : L), 0, s, a);
+    constexpr int L = decltype(lanes)::value, G = decltype(groups)::value, rows = L <= 64 ? 256 / L : 1;
+    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G>), grid_of(((int64_t)a.rows + rows - 1) / rows), dim3(L <= 64 ? 256 : L), 0, s, a);
     return hipGetLastError();
   };
   using std::integral_constant;
-  const int64_t per64 = (a.K + 64 * N - 1) / (64 * N);  // groups per lane of a wavefront
-  if (per64 <= 1) return go(integral_constant<int, 64>(), integral_constant<int, 1>());
-  if (per64 <= 2) return go(integral_constant<int, 64>(), integral_constant<int, 2>());
-  if (per64 <= 4) return go(integral_constant<int, 64>(), integral_constant<int, 4>());
-  if (per64 <= 8) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
-  if (per64 <= 16) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
-  if (per64 <= 32) return go(integral_constant<int, 256>(), integral_constant<int, 8>());
-  if (per64 <= 64) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
-  if (per64 <= 128) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+  const auto fits = [&](int lanes, int groups) { return (int64_t)a.K <= (int64_t)lanes * groups * N; };
+#define RFAST_TRY(L, G) \
+  if (fits(L, G)) return go(integral_constant<int, L>(), integral_constant<int, G>())
+  RFAST_TRY(8, 1);
+  RFAST_TRY(8, 2);
+  RFAST_TRY(16, 2);
+  RFAST_TRY(32, 2);
+  RFAST_TRY(64, 2);
+  RFAST_TRY(64, 4);
+  RFAST_TRY(256, 2);
+  RFAST_TRY(256, 4);
+  RFAST_TRY(256, 8);
+  RFAST_TRY(512, 8);
+  RFAST_TRY(512, 16);
+  if constexpr (N == 4) {
+    RFAST_TRY(1024, 16);
+  }
+#undef RFAST_TRY
   hipLaunchKernelGGL((rfast_xent_long_kernel<IN, OUT>), grid_of(a.rows), dim3(1024), 0, s, a);
   return hipGetLastError();
 }

@@ -13,14 +13,16 @@ import numpy as np
 from .binding import RFastError, RfastAdamwOptions, RfastAdamwTensor, RfastLoraShape, lib, rfast_last_error
 
 F32, BF16 = 0, 1
-_torch = None
+_torch = _types = _stream_of = None
 
 
 def _t():
-    global _torch
+    global _torch, _types, _stream_of
     if _torch is None:
         import torch
-        _torch = torch
+        _torch, _types = torch, {torch.float32: F32, torch.bfloat16: BF16}
+        # (the handle alone, where torch offers it: a Stream object costs a microsecond more than the call it is made for)
+        _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
     return _torch
 
 
@@ -30,36 +32,39 @@ def _need(ok, msg):
 
 
 def _type(t, name):
-    torch = _t()
-    _need(t.dtype in (torch.float32, torch.bfloat16), f"{name}: need float32 or bfloat16, got {t.dtype}")
-    return F32 if t.dtype == torch.float32 else BF16
+    k = _types.get(t.dtype)
+    if k is None:
+        raise RFastError(-1, f"{name}: need float32 or bfloat16, got {t.dtype}")
+    return k
 
 
 def _call(device, f, *args):
     """f on the current stream of `device` (its last argument), with that device current."""
-    torch = _t()
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index is None or device.index == torch.cuda.current_device():
-        code = f(*args, stream)
+    index = device.index
+    if index == _torch.cuda.current_device():
+        code = f(*args, _stream_of(index))
     else:
-        with torch.cuda.device(device):
-            code = f(*args, stream)
+        with _torch.cuda.device(index):
+            code = f(*args, _stream_of(index))
     if code != 0:
         raise RFastError(code, rfast_last_error(None))
 
 
 def _matrix(t, name, rows, cols, dtype, device):
     """Distance of the rows of a [rows][cols] tensor whose columns are neighbours."""
-    _need(t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, f"{name}: need shape ({rows}, {cols}), got {tuple(t.shape)}")
-    _need(t.device == device, f"{name}: need a tensor on {device}, got {t.device}")
-    _need(dtype is None or t.dtype == dtype, f"{name}: need {dtype}, got {t.dtype}")
-    _need(cols <= 1 or t.stride(1) == 1, f"{name}: the elements of a row must be neighbours")
+    if tuple(t.shape) != (rows, cols) or t.device != device or (dtype is not None and t.dtype != dtype):
+        raise RFastError(-1, f"{name}: need a tensor of shape ({rows}, {cols}) and type {dtype or t.dtype} on {device}, "
+                             f"got {tuple(t.shape)}, {t.dtype} on {t.device}")
+    if t.is_contiguous():
+        return cols if cols > 0 else 1
+    if cols > 1 and t.stride(1) != 1:
+        raise RFastError(-1, f"{name}: the elements of a row must be neighbours")
     return t.stride(0) if rows > 1 else max(cols, 1)
 
 
 def _vector(t, name, count, dtype, device):
-    _need(t.dtype == dtype and t.device == device and t.is_contiguous() and t.numel() == count,
-          f"{name}: need a contiguous {dtype} tensor of {count} elements on {device}")
+    if t.dtype != dtype or t.device != device or t.numel() != count or not t.is_contiguous():
+        raise RFastError(-1, f"{name}: need a contiguous {dtype} tensor of {count} elements on {device}")
     return t.data_ptr()
 
 
@@ -69,20 +74,22 @@ def rfast_softmax_xent(logits, labels, grad_scale=1.0, grad_dtype=None, grad=Non
     lse: float32 [T] to receive log sum exp.  rows: int32 [1] on the device; only that many rows are taken, the others of the
     outputs are not written."""
     torch = _t()
-    _need(logits.dim() == 2 and logits.is_cuda, "logits: need a matrix on the GPU")
+    if logits.dim() != 2 or not logits.is_cuda or logits.shape[1] < 1:
+        raise RFastError(-1, "logits: need a matrix on the GPU with at least one class")
     T, K = logits.shape
     dev = logits.device
-    _need(K >= 1, "logits: need at least one class")
-    ld = _matrix(logits, "logits", T, K, None, dev)
-    lt = _type(logits, "logits")
+    ld, lt = _matrix(logits, "logits", T, K, None, dev), _type(logits, "logits")
     p_labels = _vector(labels, "labels", T, torch.int32, dev)
     if loss is None:
         loss = torch.empty(T, dtype=torch.float32, device=dev)
-    p_loss = _vector(loss, "loss", T, torch.float32, dev)
+        p_loss = loss.data_ptr()
+    else:
+        p_loss = _vector(loss, "loss", T, torch.float32, dev)
     p_lse = None if lse is None else _vector(lse, "lse", T, torch.float32, dev)
     if grad is None:
         grad = torch.empty((T, K), dtype=grad_dtype or logits.dtype, device=dev)
-    if grad is False:
+        ldg, gt, p_grad = K, _type(grad, "grad"), grad.data_ptr()
+    elif grad is False:
         grad, p_grad, gt, ldg = None, None, F32, 0
     else:
         _need(grad_dtype is None or grad.dtype == grad_dtype, "grad: its type is not grad_dtype")
@@ -98,25 +105,24 @@ def rfast_lora_workspace_bytes(shape, which):
 
 
 def _lora(x, w, a, b, row_ptr, adapter, y_type, ld_y, scale, which):
-    torch = _t()
-    dev, bf16 = x.device, torch.bfloat16
-    _need(x.dim() == 2 and x.is_cuda, "x: need a matrix on the GPU")
-    _need(a.dim() == 3 and b.dim() == 3 and w.dim() == 2, "need w [K][d], a [adapters][rank][d], b [adapters][K][rank]")
+    torch = _torch
+    bf16, dev = torch.bfloat16, x.device
+    if x.dim() != 2 or not x.is_cuda or w.dim() != 2 or a.dim() != 3:
+        raise RFastError(-1, "need x [rows][d] on the GPU, w [K][d], a [adapters][rank][d], b [adapters][K][rank]")
     T, d = x.shape
     K, (n, r, _) = w.shape[0], a.shape
-    _need(tuple(w.shape) == (K, d) and tuple(a.shape) == (n, r, d) and tuple(b.shape) == (n, K, r),
-          "need x [rows][d], w [K][d], a [adapters][rank][d], b [adapters][K][rank]")
-    for t, name in ((w, "w"), (a, "a"), (b, "b")):
-        _need(t.dtype == bf16 and t.device == dev and t.is_contiguous(), f"{name}: need a contiguous bfloat16 tensor on {dev}")
+    for t, name, want in ((w, "w", (K, d)), (a, "a", (n, r, d)), (b, "b", (n, K, r))):
+        if t.dtype != bf16 or t.device != dev or tuple(t.shape) != want or not t.is_contiguous():
+            raise RFastError(-1, f"{name}: need a contiguous bfloat16 tensor of shape {want} on {dev}, got {t.dtype}, {tuple(t.shape)} on {t.device}")
     ld_x = _matrix(x, "x", T, d, bf16, dev)
     S = row_ptr.numel() - 1
-    _need(S >= 1, "row_ptr: need segments + 1 numbers")
     p_ptr = _vector(row_ptr, "row_ptr", S + 1, torch.int32, dev)
     p_ad = None if adapter is None else _vector(adapter, "adapter", S, torch.int32, dev)
     shape = RfastLoraShape(T, S, n, d, K, r, ld_x, ld_y, y_type, scale)
-    nbytes = rfast_lora_workspace_bytes(shape, which)
-    _need(nbytes > 0 or T == 0, "sizes out of range (rank 1 .. 64)")
-    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
+    nbytes = lib().rfast_lora_workspace_bytes(C.byref(shape), which)
+    if nbytes == 0 and T > 0:
+        raise RFastError(-1, "sizes out of range (at least one segment; rank 1 .. 64)")
+    ws = torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)
     return dev, shape, (x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), p_ptr, p_ad), ws
 
 
@@ -128,10 +134,10 @@ def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, o
     torch = _t()
     T, K = x.shape[0], w.shape[0]
     if out is None:
-        out = torch.empty((T, K), dtype=out_dtype or torch.bfloat16, device=x.device)
+        out, ld_y = torch.empty((T, K), dtype=out_dtype or torch.bfloat16, device=x.device), max(K, 1)
     else:
         _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
-    ld_y = _matrix(out, "out", T, K, None, x.device)
+        ld_y = _matrix(out, "out", T, K, None, x.device)
     dev, shape, ptrs, ws = _lora(x, w, a, b, row_ptr, adapter, _type(out, "out"), ld_y, scale, 0)
     _call(dev, lib().rfast_lora_forward, C.byref(shape), *ptrs, out.data_ptr(), ws.data_ptr(), ws.numel())
     return out
@@ -143,19 +149,16 @@ def rfast_lora_backward(x, w, a, b, row_ptr, adapter, dy, scale=1.0, need_dx=Tru
     torch = _t()
     T, d = x.shape
     ld_y = _matrix(dy, "dy", T, w.shape[0], torch.bfloat16, x.device)
-    if dx is None and need_dx:
-        dx = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
-    dev, shape, ptrs, ws = _lora(x, w, a, b, row_ptr, adapter, BF16, ld_y, scale, 1 if dx is None else 2)
-    if da is None:
-        da = torch.empty(a.shape, dtype=torch.float32, device=dev)
-    if db is None:
-        db = torch.empty(b.shape, dtype=torch.float32, device=dev)
-    p_dx = None
+    with_dx = need_dx or dx is not None
+    dev, shape, ptrs, ws = _lora(x, w, a, b, row_ptr, adapter, BF16, ld_y, scale, 2 if with_dx else 1)
     if dx is not None:
         _need(_matrix(dx, "dx", T, d, torch.bfloat16, dev) == shape.ld_x or T <= 1, "dx: its rows must be as far apart as x's")
-        p_dx = dx.data_ptr()
-    _call(dev, lib().rfast_lora_backward, C.byref(shape), *ptrs, dy.data_ptr(), p_dx, _vector(da, "da", a.numel(), torch.float32, dev),
-          _vector(db, "db", b.numel(), torch.float32, dev), ws.data_ptr(), ws.numel())
+    elif with_dx:
+        dx = torch.empty_strided((T, d), (shape.ld_x, 1), dtype=torch.bfloat16, device=dev)
+    da = torch.empty(a.shape, dtype=torch.float32, device=dev) if da is None else da
+    db = torch.empty(b.shape, dtype=torch.float32, device=dev) if db is None else db
+    _call(dev, lib().rfast_lora_backward, C.byref(shape), *ptrs, dy.data_ptr(), None if dx is None else dx.data_ptr(),
+          _vector(da, "da", a.numel(), torch.float32, dev), _vector(db, "db", b.numel(), torch.float32, dev), ws.data_ptr(), ws.numel())
     return dx, da, db
 
 
@@ -166,6 +169,7 @@ def rfast_adamw_workspace_bytes(tensors):
 
 
 def rfast_adamw_create(tensors, options, workspace):
+    _t()
     h = C.c_void_p()
     _call(workspace.device, lambda stream: lib().rfast_adamw_create(C.byref(h), len(tensors), tensors, C.byref(options),
                                                                     workspace.data_ptr(), workspace.numel(), stream))
@@ -253,7 +257,7 @@ class RFastAdamW:
     def step(self, gamma, active=None):
         """One step with step size gamma; active: uint8 [tensors] on the device, zero for tensors that stay as they are."""
         if active is not None:
-            _vector(active, "active", len(self.params), _t().uint8, self.device)
+            _vector(active, "active", len(self.params), _torch.uint8, self.device)
         rfast_adamw_step(self.handle, gamma, active, self.device)
 
     def steps(self):
