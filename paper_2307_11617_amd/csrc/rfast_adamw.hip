@@ -2,8 +2,7 @@
 //
 // Elementwise; a coordinate in 32 bits moves 28 bytes (parameter, gradient, two moments in; all but the gradient out) for some 60
 // vector instructions, so the kernel is bound by memory where the tensors are large and by latency where they are small.
-//  - One launch for all tensors: the coordinates of every tensor are cut into chunks, and a table says whose a chunk is.  A
-//    workgroup takes chunks in strides of the grid.
+//  - One launch for all tensors: the coordinates of every tensor are cut into chunks, a workgroup each, and a table says whose a chunk is.
 //  - 8 bits: a block of 256 coordinates, which share a scale, is one wavefront's four coordinates per lane, so the largest magnitude is
 //    found in registers and every byte is still moved once.
 //  - Counters of steps are on the device (a replayed graph has to count).  Every workgroup reads them, and the last one to finish moves
@@ -22,7 +21,7 @@ constexpr int kThreads = 256;
 constexpr int kBlock = 256;                    // coordinates per scale
 constexpr int kSlice = kThreads / 64 * kBlock; // coordinates that the wavefronts of a workgroup take at a time
 constexpr int kGroups = 64;                    // words for workgroups that are through
-constexpr int kMostWorkgroups = 2048;          // eight per compute unit
+constexpr int kMostWorkgroups = 1 << 23;       // a launch has fewer than 2^32 lanes
 constexpr float kCodeMost = 448.f;             // largest finite e4m3
 constexpr float kCodeLeast = 0.001953125f;     // smallest e4m3 above zero, 2^-9
 constexpr size_t kAlign = 256;
@@ -221,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
   }
   // The last workgroup moves the counters on.  No workgroup reads them any more: each has used what it read before it counts itself,
   // and nothing else is handed over, so the words need no ordering of memory (a release across the eight L2s writes them back:
-  // with it, 256 small tensors took 48 us instead of XX).
+  // with it, 256 small tensors took 48 us instead of 8).
   __shared__ bool last;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -300,7 +299,7 @@ bool count_chunks(int32_t tensors, const rfast_adamw_tensor* t, int64_t slices, 
   for (int32_t i = 0; i < tensors; ++i) {
     if (t[i].count < 0 || t[i].count > (int64_t)1 << 46) return false;
     *chunks += (t[i].count + slices * kSlice - 1) / (slices * kSlice);
-    if (*chunks > 0x7fffffff - kMostWorkgroups) return false;
+    if (*chunks > 0x7fffffff - kMostWorkgroups) return false;  // (a workgroup's next chunk is still an int)
   }
   return true;
 }
@@ -313,11 +312,14 @@ Layout layout_of(int32_t tensors, int64_t chunks) {
   l.total = up(l.through + (kGroups * 16 + 1) * 4);
   return l;
 }
-// Slices per chunk: four keep enough bytes under way per wavefront, one spreads small tensors over the card.
-int64_t slices_for(int32_t tensors, const rfast_adamw_tensor* t, int64_t* chunks) {
-  if (!count_chunks(tensors, t, 4, chunks)) return 0;
-  if (*chunks >= 2 * kMostWorkgroups) return 4;
-  return count_chunks(tensors, t, 1, chunks) ? 1 : 0;
+// Slices per chunk.  32 bits: one (four loads per lane under way; 16 x 11.2 M coordinates 807 us, with two 875, with four 885).  8 bits,
+// whose loads of the moments are short: four where there are chunks enough (525; 564 with two, 635 with one; 75 tensors of 200000 on
+// average 43 / 44 / 50), else two (40 of 100000: 16.1; 17.6 with four, 17.7 with one).
+int64_t slices_for(int32_t tensors, const rfast_adamw_tensor* t, int32_t bits, int64_t* chunks) {
+  const int64_t most = bits == 32 ? 1 : 4;
+  if (!count_chunks(tensors, t, most, chunks)) return 0;
+  if (most == 1 || *chunks >= 2048) return most;
+  return count_chunks(tensors, t, 2, chunks) ? 2 : 0;
 }
 
 }  // namespace
@@ -332,9 +334,15 @@ namespace {
 
 template <class P, class G, int BITS> hipError_t launch(const rfast_adamw* h, const Args& a, hipStream_t s) {
   const dim3 grid((unsigned)std::min(std::max(a.chunks, 1), kMostWorkgroups)), block(kThreads);
-  if (h->slices == 1) hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 1, false>), grid, block, 0, s, a);
-  else if (h->stream) hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 4, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 4, false>), grid, block, 0, s, a);
+  constexpr int MOST = BITS == 32 ? 1 : 4;
+  if constexpr (MOST > 1) {
+    if (h->slices == 2) {
+      hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, 2, false>), grid, block, 0, s, a);
+      return hipGetLastError();
+    }
+  }
+  if (h->stream) hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, MOST, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rfast_adamw_kernel<P, G, BITS, MOST, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 template <class P, class G> hipError_t launch(const rfast_adamw* h, const Args& a, hipStream_t s) {
@@ -354,7 +362,7 @@ int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, cons
   if (!(o->eps > 0 && o->eps < 1e30)) return rfast_refuse(RFAST_ERANGE, "eps must be positive and finite");
   if (!aligned(d_workspace, kAlign)) return rfast_refuse(RFAST_EINVAL, "workspace must be 256-byte aligned");
   int64_t chunks;
-  const int64_t slices = slices_for(tensors, t, &chunks);
+  const int64_t slices = slices_for(tensors, t, o->state_bits, &chunks);
   if (slices == 0) return rfast_refuse(RFAST_EINVAL, "a tensor's count is out of range");
   const Layout l = layout_of(tensors, chunks);
   if (workspace_bytes < l.total) return rfast_refuse(RFAST_ENOMEM, "workspace too small");
@@ -410,7 +418,9 @@ int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, cons
   h->grad_type = o->grad_type;
   h->bits = o->state_bits;
   h->slices = (int)slices;
-  h->stream = bytes > (int64_t)256 << 20;  // more than the caches hold from one step to the next
+  // What is read once a step streams past the caches where they would not hold it until the next: 16 x 11.2 M coordinates 910 -> 807 us,
+  // 100 tensors of 200000 in 16 bits (240 MB) 81 -> 74; 20 tensors of 200000 (64 MB) 19.1 -> 20.7 with it, 90 MB with moments in 8 bits 47 -> 56.
+  h->stream = bytes > (int64_t)160 << 20;
   h->a = {(const Row*)(base + l.rows), (const int32_t*)(base + l.whose), (int32_t*)(base + l.steps), (unsigned*)(base + l.through),
           nullptr, tensors, (int32_t)chunks, 0.0, std::log(o->beta1), std::log(o->beta2),
           (float)o->beta1, (float)o->beta2, (float)(1.0 - o->beta1), (float)(1.0 - o->beta2), (float)o->eps};
@@ -438,9 +448,9 @@ hipError_t rfast_launch_adamw_round(rfast_ctx* c, bool sync, int parity) {
 extern "C" {
 
 size_t rfast_adamw_workspace_bytes(int32_t tensors, const rfast_adamw_tensor* t) {
-  int64_t chunks;
-  if (tensors < 1 || !t || slices_for(tensors, t, &chunks) == 0) return 0;
-  return layout_of(tensors, chunks).total;
+  int64_t with32, with8;  // chunks
+  if (tensors < 1 || !t || slices_for(tensors, t, 32, &with32) == 0 || slices_for(tensors, t, 8, &with8) == 0) return 0;
+  return layout_of(tensors, std::max(with32, with8)).total;
 }
 
 int rfast_adamw_create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, const rfast_adamw_options* o,

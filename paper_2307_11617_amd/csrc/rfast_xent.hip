@@ -99,11 +99,12 @@ template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane,
 }
 
 // LANES lanes hold a row, GROUPS groups of logits each.  LANES <= 64: 256 / LANES rows per workgroup.
-// The last group of a row whose length is no multiple of a group begins earlier, so that every load is a whole group without a condition
-// (a condition per load would have each of them waited for before the next is sent): the overlap is in the sum once, and its
-// gradient is written twice alike.
+// Every load is a whole group without a condition (a condition per load would have each of them waited for before the next is sent), so groups
+// overlap at the ends of a row: group h begins at 8 h - m, moved into [0, K - 8] (4 instead of 8 in 32 bits), where m is how far a row of
+// a workgroup's begins behind a multiple of 16 bytes, so that all but the first and last group are aligned (K 50001: 205 us with m = 0,
+// 171 so).  What a group shares with the one before is left out of its sum, and its gradient is written twice alike.
 template <class IN, class OUT, int LANES, int GROUPS>
-__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 1) rfast_xent_kernel(Args a) {
+__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 1) rfast_xent_kernel(Args a) {
   constexpr int N = Group<IN>::N, ROWS = LANES <= 64 ? 256 / LANES : 1, SPAN = LANES * N;
   __shared__ float box[2][16];
   const int lane = threadIdx.x % LANES;
@@ -113,16 +114,18 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 
   const IN* l = (const IN*)a.logits + row * a.ld_logits;
   OUT* grad = a.grad ? (OUT*)a.grad + row * a.ld_grad : nullptr;
   const int label = a.labels[row], last = a.K - N;  // last: where the last group begins (below 0: a row shorter than a group)
+  const int m = LANES > 64 ? (int)((uintptr_t)l / sizeof(IN) % N) : 0;
   const bool counts = label >= 0 && label < a.K;
   if (!counts && !a.lse) {
     if (lane == 0 && a.loss) a.loss[row] = 0.f;
     if (grad) zero_row(grad, a.K, lane, LANES);
     return;
   }
+  auto begin = [&](int h) { return max(min(h * N - m, last), 0); };
   Group<IN> v[GROUPS];
   if (LANES > 8 || GROUPS > 1 || last >= 0) {
 #pragma unroll
-    for (int q = 0; q < GROUPS; ++q) v[q].load(l + min(q * SPAN + lane * N, last));
+    for (int q = 0; q < GROUPS; ++q) v[q].load(l + begin(q * LANES + lane));
   } else {
     v[0].load(l, a.K);
   }
@@ -143,11 +146,11 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 
   float sum = 0.f;
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q) {
-    if ((q + 1) * SPAN <= a.K) {
+    if ((q + 1) * SPAN - m <= a.K && (q > 0 || m == 0)) {
 #pragma unroll
       for (int j = 0; j < N; ++j) sum += power(v[q].at(j), shift);
     } else {
-      const int again = q * SPAN + lane * N - max(min(q * SPAN + lane * N, last), 0);  // what lanes before have
+      const int h = q * LANES + lane, again = h > 0 ? begin(h - 1) + N - begin(h) : 0;  // what the group before has too
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float e = power(v[q].at(j), shift);
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 
   forget();
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q) {
-    const int k = q * SPAN + lane * N, at = max(min(k, last), 0);
+    const int h = q * LANES + lane, at = begin(h);
     float g[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) g[j] = power(v[q].at(j), shift) * c;
@@ -174,7 +177,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 16 ? 4 : 
 #pragma unroll
       for (int j = 0; j < N; ++j) g[j] -= j == label - at ? a.scale : 0.f;
     }
-    if (k >= a.K) continue;
+    if (h * N - m >= a.K) continue;
     if (LANES > 8 || GROUPS > 1 || last >= 0) {
       store_group<N>(grad + at, g);
     } else {
@@ -261,7 +264,7 @@ template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
     return hipGetLastError();
   };
   using std::integral_constant;
-  const auto fits = [&](int lanes, int groups) { return (int64_t)a.K <= (int64_t)lanes * groups * N; };
+  const auto fits = [&](int lanes, int groups) { return a.K + (lanes > 64 ? N - 1 : 0) <= (int64_t)lanes * groups * N; };
 #define RFAST_TRY(L, G) \
   if (fits(L, G)) return go(integral_constant<int, L>(), integral_constant<int, G>())
   RFAST_TRY(8, 1);
@@ -273,7 +276,10 @@ template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
   RFAST_TRY(256, 2);
   RFAST_TRY(256, 4);
   RFAST_TRY(256, 8);
+  RFAST_TRY(512, 6);
   RFAST_TRY(512, 8);
+  RFAST_TRY(512, 10);
+  RFAST_TRY(512, 13);
   RFAST_TRY(512, 16);
   if constexpr (N == 4) {
     RFAST_TRY(1024, 16);
