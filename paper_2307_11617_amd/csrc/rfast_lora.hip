@@ -14,6 +14,7 @@
 // Operand layout of the 16x16x32 instruction (lane l of 64): A: row l%16, contraction indices 8(l/16) .. +7;  B: column l%16, the
 // same indices;  C/D: column l%16, rows 4(l/16) + v for v = 0..3.
 #include <algorithm>
+#include <type_traits>
 
 #include "rfast_operators.h"
 
@@ -21,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kMostRank = 64;
-constexpr int kTileRows = 128, kTileOuts = 128, kStep = 64;  // of `up`
+constexpr int kStep = 64;                 // contraction indices of a stage of `up`
 constexpr int kNone = -1, kBehind = -2;  // row without an adapter, row behind the last segment
 constexpr size_t kAlign = 256;
 size_t up(size_t b) { return (b + kAlign - 1) / kAlign * kAlign; }
@@ -30,12 +31,15 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Eight neighbours from p on, of which `left` exist (any number); zeros for the others.
+// Eight neighbours from p on.
+__device__ inline u32x4 load_eight(const u16* p) {
+  const any_u32x4 t = *reinterpret_cast<const any_u32x4*>(p);
+  return u32x4{t.x, t.y, t.z, t.w};
+}
+// ... of which `left` exist (any number); zeros for the others.  For the ends of rows: a condition per load has it waited for before the next
+// is sent, so wherever all of them exist the loads go out without one.
 __device__ inline u32x4 load_eight(const u16* p, int64_t left) {
-  if (left >= 8) {
-    const any_u32x4 t = *reinterpret_cast<const any_u32x4*>(p);
-    return u32x4{t.x, t.y, t.z, t.w};
-  }
+  if (left >= 8) return load_eight(p);
   u32x4 t = {0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < 7; ++j)
@@ -73,8 +77,9 @@ constexpr int kPieces = 3;  // bf16 that a value of u or e is held as
 // out = scale * (rows of z) x (adapter's matrix m [rank][cols]) in kPieces bf16:
 //   out_rows [rows][kPieces][RP]    what `up` reads
 //   out_cols [kPieces][RP][pitch]   what `sums` reads: the same by columns
-// One workgroup per 16 rows, its wavefronts share the contraction; rows of several segments are taken one segment after the other, or
-// by several workgroups (gridDim.y) where there are so few rows that a segment is one or two of them.
+// A workgroup has 16 RT rows, its WAVES wavefronts share the contraction; rows of several segments are taken one segment after the other,
+// or by several workgroups (gridDim.y) where there are so few rows that a segment is one or two of them.  Rows and ranks that do not
+// exist or belong to another segment are read as the nearest that do, and what comes of them is left out.
 struct Down {
   const u16* z;
   const u16* m;
@@ -87,12 +92,12 @@ struct Down {
   float scale;
 };
 
-template <int RP>
-__global__ void __launch_bounds__(kThreads) rfast_lora_down(Down a) {
-  constexpr int NT = tiles_of(RP);
-  __shared__ f32x4 part[kWaves][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int row0 = blockIdx.x * 16, end = min(row0 + 16, a.seg.rows), behind = a.seg.end_of_all();
+template <int RP, int RT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
+  constexpr int NT = tiles_of(RP), CHUNK = 128;
+  __shared__ f32x4 part[WAVES][RT * NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int row0 = blockIdx.x * (16 * RT), end = min(row0 + 16 * RT, a.seg.rows), behind = a.seg.end_of_all();
   int run = 0;
   for (int r0 = row0, r1; r0 < end; r0 = r1, ++run) {
     int id = kBehind;
@@ -106,40 +111,54 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_down(Down a) {
     if (run % gridDim.y != blockIdx.y) continue;
     if (a.ids && threadIdx.x < r1 - r0) a.ids[r0 + threadIdx.x] = id;
     if (id == kBehind) break;
-    f32x4 acc[NT];
+    f32x4 acc[RT][NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     if (id >= 0) {
-      const bool mine = row0 + n >= r0 && row0 + n < r1;
-      const u16* z = a.z + (int64_t)(row0 + n) * a.ld;
-      const u16* m = a.m + (int64_t)id * a.rank * a.cols;
-      for (int c = wave * 128 + g * 8; c < a.cols + g * 8; c += kWaves * 128) {
+      const u16 *z[RT], *m[NT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) z[i] = a.z + (int64_t)min(max(row0 + 16 * i + n, r0), r1 - 1) * a.ld + g * 8;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) m[t] = a.m + ((int64_t)id * a.rank + min(t * 16 + n, a.rank - 1)) * a.cols + g * 8;
+      const int whole = a.cols / CHUNK * CHUNK;
+      auto chunk = [&](int c, auto load) {
+        u32x4 zf[4][RT], mf[4][NT];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int left = a.cols - (c + 32 * q);
-          const u32x4 zf = load_eight(z + c + 32 * q, mine ? left : 0);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const int k = t * 16 + n;
-            acc[t] = mfma(zf, load_eight(m + (int64_t)k * a.cols + c + 32 * q, k < a.rank ? left : 0), acc[t]);
-          }
+          for (int i = 0; i < RT; ++i) zf[q][i] = load(z[i], c + 32 * q);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mf[q][t] = load(m[t], c + 32 * q);
         }
-      }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[i][t] = mfma(zf[q][i], mf[q][t], acc[i][t]);
+      };
+      for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) chunk(c, [&](const u16* p, int at) { return load_eight(p + at); });
+      if (whole < a.cols && wave == whole / CHUNK % WAVES)
+        chunk(whole, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
     }
     __syncthreads();  // the sums of the run before have been read
 #pragma unroll
-    for (int t = 0; t < NT; ++t) part[wave][t][lane] = acc[t];
-    __syncthreads();
-    if (wave < NT) {
-      f32x4 v = part[0][wave][lane];
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v += part[w][wave][lane];
-      const int k = wave * 16 + n;
+      for (int t = 0; t < NT; ++t) part[wave][i * NT + t][lane] = acc[i][t];
+    __syncthreads();
+    for (int u = wave; u < RT * NT; u += WAVES) {
+      f32x4 v = part[0][u][lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) v += part[w][u][lane];
+      const int k = u % NT * 16 + n, first = row0 + u / NT * 16 + 4 * g;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = row0 + 4 * g + q;
+        const int row = first + q;
         if (k >= RP || row < r0 || row >= r1) continue;
-        float f = v[q] * a.scale;
+        float f = k < a.rank ? v[q] * a.scale : 0.f;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
           const u16 piece = to_bf16(f);
@@ -166,144 +185,295 @@ struct Up {
   int32_t rows, cols, outs, rank;
 };
 
-// The adapters' part for 16 rows from row0 on (B operand) and 16 outputs from out0 on (A operand): one step per adapter that
-// the rows have.  A column of the result is one row's, so that the others of a step are left out there and nothing of an adapter
-// (an infinity, say) reaches rows that have another.
-template <int RP> __device__ inline f32x4 add_adapters(const Up& a, int row0, int out0, f32x4 acc) {
-  constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int row = row0 + n, out = out0 + n;
-  const int id = row < a.rows ? a.ids[row] : kNone;
-  uint64_t pending = __ballot(id >= 0) & 0xFFFF;
-  u32x4 u[STEPS];
+template <int RP> struct Pieces {  // of u for 16 rows, as B operand
+  static constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
+  u32x4 f[STEPS];
+  __device__ void load(const Up& a, int row) {
+    const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int q = 0; q < STEPS; ++q) {
-    const int k = 32 * q + 8 * g;
-    u[q] = load_eight(a.u + (int64_t)row * WIDE + k, id >= 0 && k < WIDE ? 8 : 0);
+    for (int q = 0; q < STEPS; ++q) {
+      const int k = 32 * q + 8 * g;
+      f[q] = load_eight(a.u + (int64_t)row * WIDE + min(k, WIDE - 8));
+      if (k >= WIDE) f[q] = u32x4{0, 0, 0, 0};
+    }
   }
+};
+template <int RP> struct Factor {  // b of adapter `who` for 16 outputs from out0 on, as A operand
+  static constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
+  u32x4 f[STEPS];
+  __device__ void load(const Up& a, int who, int out0) {
+    const int lane = threadIdx.x & 63, out = min(out0 + (lane & 15), a.outs - 1);
+    const u16* b = a.b + ((int64_t)who * a.outs + out) * a.rank;
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) {
+      const int k = 32 * q + 8 * (lane >> 4);
+      if (a.rank == RP) f[q] = k < WIDE ? load_eight(b + k % RP) : u32x4{0, 0, 0, 0};
+      else f[q] = load_eight(b + k % RP, k < WIDE ? a.rank - k % RP : 0);
+    }
+  }
+};
+
+// The adapters' part for 16 rows (their pieces u, their adapters id: lane n has row n's) and 16 outputs from out0 on: one step per adapter
+// that the rows have.  A column of the result is one row's, so that the others of a step are left out there and nothing of an adapter (an
+// infinity, say) reaches rows that have another.
+template <int RP> __device__ inline f32x4 add_adapters(const Up& a, const Pieces<RP>& u, int id, int out0, f32x4 acc) {
+  uint64_t pending = __ballot(id >= 0) & 0xFFFF;
   while (pending) {
     const int who = __builtin_amdgcn_readlane(id, __builtin_ctzll(pending));
     const bool mine = id == who;
     pending &= ~__ballot(mine);
-    const u16* b = a.b + ((int64_t)who * a.outs + out) * a.rank;
+    Factor<RP> b;
+    b.load(a, who, out0);
     f32x4 own = {0, 0, 0, 0};
 #pragma unroll
-    for (int q = 0; q < STEPS; ++q) {
-      const int k = (32 * q + 8 * g) % RP;
-      const u32x4 bf = load_eight(b + k, out < a.outs && 32 * q + 8 * g < WIDE ? a.rank - k : 0);
-      own = mfma(bf, u[q], own);
-    }
+    for (int q = 0; q < Factor<RP>::STEPS; ++q) own = mfma(b.f[q], u.f[q], own);
     if (mine) acc += own;
   }
   return acc;
 }
 
 // Four outputs from `out` on of one row
-template <class Y> __device__ inline void store_outs(const Up& a, int row, int out, f32x4 v) {
-  if (row >= a.rows || out >= a.outs || a.ids[row] == kBehind) return;
+template <class Y> __device__ inline void store_outs(const Up& a, int row, int id, int out, f32x4 v) {
+  if (row >= a.rows || out >= a.outs || id == kBehind) return;
   const float f[4] = {v.x, v.y, v.z, v.w};
   store_four<false>((Y*)a.y + (int64_t)row * a.ld_y + out, a.outs - out, f);
 }
 
+// Many rows: a workgroup's tile of TO outputs x TR rows, shared by WO x WR wavefronts, both operands through two buffers in LDS.  A row of a
+// stage is eight chunks of 16 bytes; chunk c is put at place c ^ row % 8, so that the 16 rows of an operand fall on all banks.
+// DIRECT: rows begin at multiples of 16 bytes, and stages go from memory to LDS without passing through registers (a wavefront's load
+// fills 1 KB, eight rows, in the order of its lanes, so each lane fetches the chunk that belongs to its place); else, and for a last stage
+// that is not whole, through registers.
+// TURNED: w is [cols][outs] instead, as the gradient of the rows reads it.  A lane fetches eight rows of four outputs and turns that block
+// over in registers, one byte permutation per pair of elements.
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT, bool TURNED>
+__global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tiles, int out_tiles) {
+  constexpr int WAVES = WO * WR, THREADS = 64 * WAVES, OI = TO / WO / 16, RJ = TR / WR / 16;
+  constexpr int WL = TO / 8 / WAVES, ZL = TR / 8 / WAVES;  // loads of 16 bytes per lane and stage
+  static_assert(WL * 8 * WAVES == TO && ZL * 8 * WAVES == TR && TO * kStep / 32 == THREADS * (TO * kStep / 32 / THREADS), "tile");
+  constexpr int TL = TURNED ? TO * kStep / 32 / THREADS : 1;  // blocks of 8 x 4 per lane
+  __shared__ u32x4 w_tile[2][TO * 8], z_tile[2][TR * 8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  // Workgroups are dealt to the eight XCDs by turns: one XCD gets consecutive tiles, which share rows and outputs in its L2.
+  const int tiles = row_tiles * out_tiles;
+  int t = blockIdx.x;
+  if (tiles % 8 == 0) t = t % 8 * (tiles / 8) + t / 8;
+  // bands of eight tiles of rows, within a band output by output
+  const int band = t / (8 * out_tiles), in_band = t - band * 8 * out_tiles, high = min(8, row_tiles - 8 * band);
+  const int row0 = (band * 8 + in_band % high) * TR, out0 = in_band / high * TO;
+  const int wo = wave / WR * (TO / WO), wr = wave % WR * (TR / WR);
 
-// Many rows: a workgroup's tile of 128 outputs x 128 rows, 64 x 64 per wavefront, both operands through two buffers in LDS.  Chunks of
-// 16 bytes are put at (chunk ^ row % 8) of their row, so that the 16 rows of an operand fall on all banks.
-template <int RP, class Y>
-__global__ void __launch_bounds__(kThreads) rfast_lora_up(Up a, int row_tiles) {
-  __shared__ u32x4 tile[2][2][128 * kStep / 8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int row0 = (blockIdx.x % row_tiles) * kTileRows, out0 = (blockIdx.x / row_tiles) * kTileOuts;
-  const int wo = (wave >> 1) * 64, wr = (wave & 1) * 64;
-  f32x4 acc[4][4];
+  f32x4 acc[OI][RJ];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < OI; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-  u32x4 next[2][4];
-  auto fetch = [&](int c0) {
+    for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+  // this lane's place of a load: row lane / 8 of eight, and the chunk that goes there
+  const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 8;
+  const u16* zp[ZL];
+  const u16* wp[WL];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int r = (threadIdx.x >> 3) + 32 * q, c = c0 + (threadIdx.x & 7) * 8;
-      next[0][q] = load_eight(a.w + (int64_t)(out0 + r) * a.cols + c, out0 + r < a.outs ? a.cols - c : 0);
-      next[1][q] = load_eight(a.z + (int64_t)(row0 + r) * a.ld_z + c, row0 + r < a.rows ? a.cols - c : 0);
+  for (int q = 0; q < ZL; ++q) zp[q] = a.z + (int64_t)min(row0 + (q * WAVES + wave) * 8 + lr, a.rows - 1) * a.ld_z + lc;
+#pragma unroll
+  for (int q = 0; q < WL; ++q) wp[q] = a.w + (int64_t)min(out0 + (q * WAVES + wave) * 8 + lr, a.outs - 1) * a.cols + lc;
+  u32x4 zr[ZL], wr_[WL];
+  any_u32x2 tr[TL][8];
+  const bool outs_whole = out0 + TO <= a.outs;
+
+  auto send = [&](u32x4* to, const u16* from) {
+    __builtin_amdgcn_global_load_lds((const RFAST_GLOBAL void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  };
+  auto fetch = [&](int c0, int buf) {  // stage from c0 on: into LDS, or into registers for `put`
+    const bool whole = c0 + kStep <= a.cols;
+    if (DIRECT && whole) {
+#pragma unroll
+      for (int q = 0; q < ZL; ++q) send(&z_tile[buf][(q * WAVES + wave) * 64], zp[q] + c0);
+      if constexpr (!TURNED) {
+#pragma unroll
+        for (int q = 0; q < WL; ++q) send(&w_tile[buf][(q * WAVES + wave) * 64], wp[q] + c0);
+      }
+    } else if (whole) {
+#pragma unroll
+      for (int q = 0; q < ZL; ++q) zr[q] = load_eight(zp[q] + c0);
+      if constexpr (!TURNED) {
+#pragma unroll
+        for (int q = 0; q < WL; ++q) wr_[q] = load_eight(wp[q] + c0);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < ZL; ++q) zr[q] = load_eight(zp[q] + c0, a.cols - c0 - lc);
+      if constexpr (!TURNED) {
+#pragma unroll
+        for (int q = 0; q < WL; ++q) wr_[q] = load_eight(wp[q] + c0, a.cols - c0 - lc);
+      }
+    }
+    if constexpr (TURNED) {
+#pragma unroll
+      for (int q = 0; q < TL; ++q) {
+        const int b = q * THREADS + threadIdx.x, k = c0 + b / (TO / 4) * 8, o = out0 + b % (TO / 4) * 4;
+        const u16* p = a.w + (int64_t)k * a.outs + o;
+        if (whole && outs_whole) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) tr[q][i] = *reinterpret_cast<const any_u32x2*>(p + (int64_t)i * a.outs);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const u32x4 v = load_eight(p + (int64_t)i * a.outs, k + i < a.cols ? min(a.outs - o, 4) : 0);
+            tr[q][i] = any_u32x2{v.x, v.y};
+          }
+        }
+      }
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int c0, int buf) {
+    if (!DIRECT || c0 + kStep > a.cols) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int r = (threadIdx.x >> 3) + 32 * q, at = r * 8 + ((threadIdx.x & 7) ^ (r & 7));
-      tile[buf][0][at] = next[0][q];
-      tile[buf][1][at] = next[1][q];
+      for (int q = 0; q < ZL; ++q) z_tile[buf][(q * WAVES + wave) * 64 + lane] = zr[q];
+      if constexpr (!TURNED) {
+#pragma unroll
+        for (int q = 0; q < WL; ++q) w_tile[buf][(q * WAVES + wave) * 64 + lane] = wr_[q];
+      }
+    }
+    if constexpr (TURNED) {
+#pragma unroll
+      for (int q = 0; q < TL; ++q) {
+        const int b = q * THREADS + threadIdx.x, c = b / (TO / 4), o = b % (TO / 4) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          u32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(tr[q][2 * i + 1][j >> 1], tr[q][2 * i][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+          w_tile[buf][(o + j) * 8 + (c ^ ((o + j) & 7))] = v;
+        }
+      }
     }
   };
-  fetch(0);
-  put(0);
-  __syncthreads();
+  // (all of a wavefront's loads into LDS have arrived, then all wavefronts')
+  auto meet = [&] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+
+  fetch(0, 0);
+  put(0, 0);
+  meet();
   for (int c0 = 0, buf = 0; c0 < a.cols; c0 += kStep, buf ^= 1) {
     const bool more = c0 + kStep < a.cols;
-    if (more) fetch(c0 + kStep);
+    if (more) fetch(c0 + kStep, buf ^ 1);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      u32x4 wf[4], zf[4];
+      u32x4 wf[OI], zf[RJ];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ro = wo + 16 * i + n, rr = wr + 16 * i + n;
-        wf[i] = tile[buf][0][ro * 8 + ((4 * q + g) ^ (ro & 7))];
-        zf[i] = tile[buf][1][rr * 8 + ((4 * q + g) ^ (rr & 7))];
-      }
+      for (int j = 0; j < RJ; ++j) zf[j] = z_tile[buf][(wr + 16 * j + n) * 8 + ((4 * q + g) ^ (n & 7))];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < OI; ++i) wf[i] = w_tile[buf][(wo + 16 * i + n) * 8 + ((4 * q + g) ^ (n & 7))];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mfma(wf[i], zf[j], acc[i][j]);
+      for (int i = 0; i < OI; ++i)
+#pragma unroll
+        for (int j = 0; j < RJ; ++j) acc[i][j] = mfma(wf[i], zf[j], acc[i][j]);
     }
-    if (more) put(buf ^ 1);
-    __syncthreads();
+    if (more) put(c0 + kStep, buf ^ 1);
+    meet();
   }
+
+  // The adapters' part.  Usually all rows of a wavefront have the same adapter, whose factors are then fetched once for all of them.
+  int id[RJ];
+  Pieces<RP> u[RJ];
+  bool alike = true;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < RJ; ++j) {
+    const int row = row0 + wr + 16 * j + n;
+    id[j] = row < a.rows ? a.ids[row] : kBehind;
+    u[j].load(a, min(row, a.rows - 1));
+  }
+  const int who = __builtin_amdgcn_readfirstlane(id[0]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = row0 + wr + 16 * j, o = out0 + wo + 16 * i;
-      if (r >= a.rows || o >= a.outs) continue;
-      store_outs<Y>(a, r + n, o + 4 * g, add_adapters<RP>(a, r, o, acc[i][j]));
+  for (int j = 0; j < RJ; ++j) alike = alike && __all(id[j] == who);
+#pragma unroll
+  for (int i = 0; i < OI; ++i) {
+    const int o = out0 + wo + 16 * i;
+    if (o >= a.outs) break;
+    if (alike) {
+      if (who >= 0) {
+        Factor<RP> b;
+        b.load(a, who, o);
+#pragma unroll
+        for (int j = 0; j < RJ; ++j)
+#pragma unroll
+          for (int q = 0; q < Factor<RP>::STEPS; ++q) acc[i][j] = mfma(b.f[q], u[j].f[q], acc[i][j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) acc[i][j] = add_adapters<RP>(a, u[j], id[j], o, acc[i][j]);
     }
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) store_outs<Y>(a, row0 + wr + 16 * j + n, id[j], o + 4 * g, acc[i][j]);
+  }
 }
 
-// Up to 64 rows: bound by one read of W, which goes from memory to the registers of one wavefront and no further.  A workgroup has 16
-// outputs, its wavefronts share the contraction.
+// Up to 64 rows: bound by one read of W, which goes from memory to the registers of one wavefront and no further.  A workgroup has 16 OT
+// outputs, its WAVES wavefronts share the contraction.
 constexpr int kFewRows = 64;
-template <int RP, class Y, int RT>
-__global__ void __launch_bounds__(kThreads) rfast_lora_up_few(Up a) {
-  __shared__ f32x4 part[kWaves][RT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int out0 = blockIdx.x * 16;
-  f32x4 acc[RT];
+template <int RP, class Y, int OT, int RT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
+  constexpr int CHUNK = 128;
+  __shared__ f32x4 part[WAVES][OT * RT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int out0 = blockIdx.x * (16 * OT);
+  f32x4 acc[OT][RT];
+  const u16 *w[OT], *z[RT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0, 0, 0, 0};
-  const u16* w = a.w + (int64_t)(out0 + n) * a.cols;
-  for (int c = wave * 128 + g * 8; c < a.cols + g * 8; c += kWaves * 128) {
+  for (int o = 0; o < OT; ++o) {
+    w[o] = a.w + (int64_t)min(out0 + 16 * o + n, a.outs - 1) * a.cols + g * 8;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int left = a.cols - (c + 32 * q);
-      const u32x4 wf = load_eight(w + c + 32 * q, out0 + n < a.outs ? left : 0);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const int row = 16 * t + n;
-        acc[t] = mfma(wf, load_eight(a.z + (int64_t)row * a.ld_z + c + 32 * q, row < a.rows ? left : 0), acc[t]);
-      }
-    }
+    for (int t = 0; t < RT; ++t) acc[o][t] = f32x4{0, 0, 0, 0};
   }
 #pragma unroll
+  for (int t = 0; t < RT; ++t) z[t] = a.z + (int64_t)min(16 * t + n, a.rows - 1) * a.ld_z + g * 8;
+  const int whole = a.cols / CHUNK * CHUNK;
+  auto chunk = [&](int c, auto load) {
+    u32x4 wf[4][OT], zf[4][RT];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int o = 0; o < OT; ++o) wf[q][o] = load(w[o], c + 32 * q);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) zf[q][t] = load(z[t], c + 32 * q);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int o = 0; o < OT; ++o)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[o][t] = mfma(wf[q][o], zf[q][t], acc[o][t]);
+  };
+  for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) chunk(c, [&](const u16* p, int at) { return load_eight(p + at); });
+  if (whole < a.cols && wave == whole / CHUNK % WAVES)
+    chunk(whole, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+  // the adapters' part of a tile is one wavefront's, so that the tiles' go on beside each other
+#pragma unroll
   for (int t = 0; t < RT; ++t)
-    if (wave == t) acc[t] = add_adapters<RP>(a, 16 * t, out0, acc[t]);
 #pragma unroll
-  for (int t = 0; t < RT; ++t) part[wave][t][lane] = acc[t];
+    for (int o = 0; o < OT; ++o)
+      if (wave == (t * OT + o) % WAVES && out0 + 16 * o < a.outs) {
+        const int row = 16 * t + n;
+        Pieces<RP> u;
+        u.load(a, min(row, a.rows - 1));
+        acc[o][t] = add_adapters<RP>(a, u, row < a.rows ? a.ids[row] : kBehind, out0 + 16 * o, acc[o][t]);
+      }
+#pragma unroll
+  for (int o = 0; o < OT; ++o)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) part[wave][o * RT + t][lane] = acc[o][t];
   __syncthreads();
-  if (wave < RT) {
-    f32x4 v = part[0][wave][lane];
+  for (int u = wave; u < OT * RT; u += WAVES) {
+    f32x4 v = part[0][u][lane];
 #pragma unroll
-    for (int q = 1; q < kWaves; ++q) v += part[q][wave][lane];
-    store_outs<Y>(a, 16 * wave + n, out0 + 4 * g, v);
+    for (int q = 1; q < WAVES; ++q) v += part[q][u][lane];
+    const int row = 16 * (u % RT) + n;
+    store_outs<Y>(a, row, row < a.rows ? a.ids[row] : kBehind, out0 + 16 * (u / RT) + 4 * g, v);
   }
 }
 
@@ -328,38 +498,50 @@ template <int RP, bool RANK_MAJOR>
 __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
   constexpr int NT = tiles_of(RP);
   __shared__ f32x4 part[2][8][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int who = blockIdx.y, c0 = blockIdx.x * 128;
   f32x4 acc[8][NT];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[j][t] = f32x4{0, 0, 0, 0};
-  auto segment = [&](int s) {
-    const int end = a.seg.begin(s + 1);
-    for (int t0 = a.seg.begin(s) + wave * 32; t0 < end; t0 += kWaves * 32) {
-      const int r = t0 + 8 * g, c = c0 + 8 * n;
-      u32x4 z[8];
+  // A lane's first column, moved back where a tile ends with the row (what it computes twice is written twice alike).
+  const bool wide = a.cols >= 8;
+  const int c = wide ? min(c0 + 8 * n, a.cols - 8) : 0;
+  auto block = [&](int t0, int end, auto whole) {  // 32 rows from t0 on; whole: all of them exist, and rows have eight columns
+    constexpr bool WHOLE = decltype(whole)::value;
+    const int r = t0 + 8 * g;
+    u32x4 z[8], sf[NT][kFrags<RP>];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = load_eight(a.z + (int64_t)(r + i) * a.ld + c, r + i < end ? a.cols - c : 0);
-      u32x4 sf[NT][kFrags<RP>];
+    for (int i = 0; i < 8; ++i) {
+      const u16* p = a.z + (int64_t)(r + i) * a.ld + c;
+      z[i] = WHOLE ? load_eight(p) : load_eight(p, r + i < end ? min(a.cols - c, 8) : 0);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < kFrags<RP>; ++i) {
+        const int k = (RP == 8 ? 16 * i : RP * i + 16 * t) + n;
+        const u16* p = a.s + (int64_t)min(k, kPieces * RP - 1) * a.pitch + r;
+        sf[t][i] = WHOLE ? load_eight(p) : load_eight(p, end - r);
+        if (k >= kPieces * RP) sf[t][i] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      u32x4 zf;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) zf[q] = __builtin_amdgcn_perm(z[2 * q + 1][j >> 1], z[2 * q][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < kFrags<RP>; ++i) {
-          const int k = (RP == 8 ? 16 * i : RP * i + 16 * t) + n;
-          sf[t][i] = load_eight(a.s + (int64_t)k * a.pitch + r, k < kPieces * RP ? end - r : 0);
-        }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        u32x4 zf;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) zf[q] = __builtin_amdgcn_perm(z[2 * q + 1][j >> 1], z[2 * q][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < kFrags<RP>; ++i) acc[j][t] = RANK_MAJOR ? mfma(sf[t][i], zf, acc[j][t]) : mfma(zf, sf[t][i], acc[j][t]);
-      }
+        for (int i = 0; i < kFrags<RP>; ++i) acc[j][t] = RANK_MAJOR ? mfma(sf[t][i], zf, acc[j][t]) : mfma(zf, sf[t][i], acc[j][t]);
+    }
+  };
+  auto segment = [&](int s) {
+    const int end = a.seg.begin(s + 1);
+    for (int t0 = a.seg.begin(s) + wave * 32; t0 < end; t0 += kWaves * 32) {
+      if (wide && t0 + 32 <= end) block(t0, end, std::true_type());
+      else block(t0, end, std::false_type());
     }
   };
   if (!a.seg.adapter) {
@@ -396,11 +578,10 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (RANK_MAJOR) {
-      const int c = c0 + 8 * n;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const int k = t * 16 + 4 * g + v;
-        if (k >= a.rank || c >= a.cols) continue;
+        if (k >= a.rank) continue;
         float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = acc[j][t][v] * a.scale;
@@ -415,31 +596,43 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
       for (int v = 0; v < 4; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int c = c0 + 8 * (4 * g + v) + j;
-          if (c < a.cols) a.out[((int64_t)who * a.cols + c) * a.rank + k] = acc[j][t][v] * a.scale;
+          const int at = (wide ? min(c0 + 8 * (4 * g + v), a.cols - 8) : 0) + j;
+          if (at < a.cols) a.out[((int64_t)who * a.cols + at) * a.rank + k] = acc[j][t][v] * a.scale;
         }
     }
   }
 }
 
 // -------------------------------------------------------------------------------------------------------- transposes
-// out [batch][cols][rows] = in [batch][rows][cols]
-__global__ void __launch_bounds__(kThreads) rfast_lora_transpose(const u16* in, u16* out, int rows, int cols) {
+// out [batch][cols][rows] = in [batch][rows][cols], of one adapter's matrix or both
+struct Transpose {
+  const u16* in;
+  u16* out;
+  int32_t rows, cols, tiles_x, tiles;  // tiles of 64 x 64 per matrix
+};
+__global__ void __launch_bounds__(kThreads) rfast_lora_transpose(Transpose a, Transpose b) {
   __shared__ u16 t[64][66];
-  const int64_t at = (int64_t)blockIdx.z * rows * cols;
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, x = threadIdx.x & 63;
-  for (int q = threadIdx.x >> 6; q < 64; q += 4)
-    if (r0 + q < rows && c0 + x < cols) t[q][x] = in[at + (int64_t)(r0 + q) * cols + c0 + x];
+  const bool second = (int)blockIdx.x >= a.tiles;
+  const Transpose q = second ? b : a;
+  const int tile = blockIdx.x - (second ? a.tiles : 0);
+  const int64_t at = (int64_t)blockIdx.y * q.rows * q.cols;
+  const int r0 = tile / q.tiles_x * 64, c0 = tile % q.tiles_x * 64, x = threadIdx.x & 63, high = min(64, q.rows - r0), wide = min(64, q.cols - c0);
+  if (q.cols < 64) {  // (rows are shorter than a wavefront: their elements follow each other)
+    for (int i = threadIdx.x; i < high * wide; i += kThreads) t[i / wide][i % wide] = q.in[at + (int64_t)r0 * q.cols + i];
+  } else {
+    for (int i = threadIdx.x >> 6; i < high; i += 4)
+      if (x < wide) t[i][x] = q.in[at + (int64_t)(r0 + i) * q.cols + c0 + x];
+  }
   __syncthreads();
-  for (int q = threadIdx.x >> 6; q < 64; q += 4)
-    if (c0 + q < cols && r0 + x < rows) out[at + (int64_t)(c0 + q) * rows + r0 + x] = t[x][q];
+  for (int i = threadIdx.x >> 6; i < wide; i += 4)
+    if (x < high) q.out[at + (int64_t)(c0 + i) * q.rows + r0 + x] = t[x][i];
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
 int padded_rank(int rank) { return rank <= 8 ? 8 : rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
 struct Layout {
-  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, wt, total;
+  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, total;
   int64_t pitch;
 };
 Layout layout_of(const rfast_lora_shape& s, int pass) {
@@ -455,7 +648,6 @@ Layout layout_of(const rfast_lora_shape& s, int pass) {
   l.bt = take(pass != 0 ? n * K * r * 2 : 0);
   l.e_rows = take(pass == 2 ? T * wide * 2 : 0);
   l.at = take(pass == 2 ? n * d * r * 2 : 0);
-  l.wt = take(pass == 2 ? d * K * 2 : 0);
   l.total = off;
   return l;
 }
@@ -464,7 +656,7 @@ bool shape_ok(const rfast_lora_shape* s) {
   if (!s || s->rows < 0 || s->segments < 1 || s->adapters < 1 || s->d < 1 || s->K < 1 || s->rank < 1 || s->rank > kMostRank) return false;
   if (s->rows > 1 << 27 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535 || s->segments == 0x7fffffff) return false;
   // a launch has fewer than 2^32 lanes
-  return ((int64_t)s->rows / kTileRows + 1) * (std::max(s->d, s->K) / kTileOuts + 1) < (int64_t)1 << 24;
+  return ((int64_t)s->rows / 128 + 1) * (std::max(s->d, s->K) / 64 + 1) < (int64_t)1 << 23;
 }
 
 template <class F> hipError_t by_rank(int rank, F f) {
@@ -477,27 +669,46 @@ template <class F> hipError_t by_rank(int rank, F f) {
 }
 
 hipError_t launch_down(const Down& a, hipStream_t st) {
-  // with few rows the segments of 16 of them go to workgroups of their own
-  const int spread = a.seg.rows <= 1024 ? std::min(16, a.seg.count) : 1;
   return by_rank(a.rank, [&](auto rp) {
-    hipLaunchKernelGGL((rfast_lora_down<decltype(rp)::value>), dim3((a.seg.rows + 15) / 16, spread), dim3(kThreads), 0, st, a);
-    return hipGetLastError();
+    constexpr int RP = decltype(rp)::value;
+    const auto go = [&](auto rt, auto waves, int spread) {
+      constexpr int RT = decltype(rt)::value, W = decltype(waves)::value;
+      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), spread), dim3(64 * W), 0, st, a);
+      return hipGetLastError();
+    };
+    using std::integral_constant;
+    // with few rows the segments of 16 of them go to workgroups of their own
+    if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::min(16, a.seg.count));
+    if (a.seg.rows <= 8192) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), 1);
+    return go(integral_constant<int, 2>(), integral_constant<int, 4>(), 1);
   });
 }
 
-template <class Y> hipError_t launch_up(const Up& a, hipStream_t st) {
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool TURNED> hipError_t launch_up_tiles(const Up& a, hipStream_t st) {
+  const int row_tiles = (a.rows + TR - 1) / TR, out_tiles = (a.outs + TO - 1) / TO;
+  const dim3 grid((unsigned)row_tiles * out_tiles), block(64 * WO * WR);
+  const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && (TURNED || (a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0));
+  if (direct) hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, true, TURNED>), grid, block, 0, st, a, row_tiles, out_tiles);
+  else hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, false, TURNED>), grid, block, 0, st, a, row_tiles, out_tiles);
+  return hipGetLastError();
+}
+
+// turned: w is [cols][outs]
+template <class Y, bool TURNED> hipError_t launch_up(const Up& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    if (a.rows <= kFewRows) {
-      const dim3 grid((unsigned)((a.outs + 15) / 16));
-      if (a.rows <= 16) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1>), grid, dim3(kThreads), 0, st, a);
-      else if (a.rows <= 32) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 2>), grid, dim3(kThreads), 0, st, a);
-      else hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 4>), grid, dim3(kThreads), 0, st, a);
-    } else {
-      const int row_tiles = (a.rows + kTileRows - 1) / kTileRows, out_tiles = (a.outs + kTileOuts - 1) / kTileOuts;
-      hipLaunchKernelGGL((rfast_lora_up<RP, Y>), dim3((unsigned)row_tiles * out_tiles), dim3(kThreads), 0, st, a, row_tiles);
+    if constexpr (!TURNED) {
+      if (a.rows <= kFewRows) {
+        const dim3 grid((unsigned)((a.outs + 15) / 16));
+        if (a.rows <= 16) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 1, 8>), grid, dim3(512), 0, st, a);
+        else if (a.rows <= 32) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 2, 8>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 4, 8>), grid, dim3(512), 0, st, a);
+        return hipGetLastError();
+      }
     }
-    return hipGetLastError();
+    const int64_t large = ((int64_t)a.rows + 255) / 256 * ((a.outs + 255) / 256);
+    if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, TURNED>(a, st);
+    return launch_up_tiles<RP, Y, 128, 128, 2, 2, TURNED>(a, st);
   });
 }
 
@@ -508,9 +719,9 @@ template <bool RANK_MAJOR> hipError_t launch_sums(const Sums& a, hipStream_t st)
   });
 }
 
-hipError_t launch_transpose(const u16* in, u16* out, int batch, int rows, int cols, hipStream_t st) {
-  hipLaunchKernelGGL(rfast_lora_transpose, dim3((cols + 63) / 64, (rows + 63) / 64, batch), dim3(kThreads), 0, st, in, out, rows, cols);
-  return hipGetLastError();
+Transpose transpose_of(const u16* in, u16* out, int rows, int cols) {
+  const int x = (cols + 63) / 64;
+  return {in, out, rows, cols, x, x * ((rows + 63) / 64)};
 }
 
 bool at_multiple(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
@@ -550,7 +761,7 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   hipError_t e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale}, st);
   if (e != hipSuccess) return rfast_refuse_hip(e, "adapter launch");
   const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank};
-  e = s->y_type == RFAST_F32 ? launch_up<float>(u, st) : launch_up<u16>(u, st);
+  e = s->y_type == RFAST_F32 ? launch_up<float, false>(u, st) : launch_up<u16, false>(u, st);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "projection launch");
 }
 
@@ -571,18 +782,19 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
   int32_t* ids = (int32_t*)(ws + l.ids);
   hipError_t e = hipSuccess;
   if (s->rows > 0) {
-    e = launch_transpose((const u16*)B, bt, s->adapters, s->K, s->rank, st);
+    u16* at = (u16*)(ws + l.at);
+    const Transpose tb = transpose_of((const u16*)B, bt, s->K, s->rank);
+    Transpose ta = transpose_of((const u16*)A, at, s->rank, s->d);
+    if (!dx) ta.tiles = 0;
+    hipLaunchKernelGGL(rfast_lora_transpose, dim3(tb.tiles + ta.tiles, s->adapters), dim3(kThreads), 0, st, tb, ta);
+    e = hipGetLastError();
     if (e == hipSuccess) e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
     if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
+    if (e == hipSuccess && dx)
+      e = launch_up<u16, true>({(const u16*)dy, (const u16*)W, at, e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank}, st);
   }
   if (e == hipSuccess) e = launch_sums<true>({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
   if (e == hipSuccess) e = launch_sums<false>({(const u16*)dy, u_cols, dB, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
-  if (e == hipSuccess && dx && s->rows > 0) {
-    u16 *wt = (u16*)(ws + l.wt), *at = (u16*)(ws + l.at);
-    e = launch_transpose((const u16*)W, wt, 1, s->K, s->d, st);
-    if (e == hipSuccess) e = launch_transpose((const u16*)A, at, s->adapters, s->rank, s->d, st);
-    if (e == hipSuccess) e = launch_up<u16>({(const u16*)dy, wt, at, e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank}, st);
-  }
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "adapter gradient launch");
 }
 
