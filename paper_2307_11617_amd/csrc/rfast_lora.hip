@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kMostRank = 64;
-constexpr int kStep = 64;                 // contraction indices of a stage of `up`
 constexpr int kNone = -1, kBehind = -2;  // row without an adapter, row behind the last segment
 constexpr size_t kAlign = 256;
 size_t up(size_t b) { return (b + kAlign - 1) / kAlign * kAlign; }
@@ -78,7 +77,7 @@ constexpr int kPieces = 3;  // bf16 that a value of u or e is held as
 //   out_rows [rows][kPieces][RP]    what `up` reads
 //   out_cols [kPieces][RP][pitch]   what `sums` reads: the same by columns
 // A workgroup has 16 RT rows, its WAVES wavefronts share the contraction; rows of several segments are taken one segment after the other,
-// or by several workgroups (gridDim.y) where there are so few rows that a segment is one or two of them.  Rows and ranks that do not
+// or (SPREAD) by a workgroup each where there are so few rows that a segment is one or two of them.  Rows and ranks that do not
 // exist or belong to another segment are read as the nearest that do, and what comes of them is left out.
 struct Down {
   const u16* z;
@@ -92,23 +91,25 @@ struct Down {
   float scale;
 };
 
-template <int RP, int RT, int WAVES>
+template <int RP, int RT, int WAVES, bool SPREAD>
 __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
   constexpr int NT = tiles_of(RP), CHUNK = 128;
   __shared__ f32x4 part[WAVES][RT * NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int row0 = blockIdx.x * (16 * RT), end = min(row0 + 16 * RT, a.seg.rows), behind = a.seg.end_of_all();
-  int run = 0;
-  for (int r0 = row0, r1; r0 < end; r0 = r1, ++run) {
+  // SPREAD: workgroup y of sixteen has the run of rows that begins at row y, if one does
+  for (int r0 = SPREAD ? row0 + (int)blockIdx.y : row0, r1; r0 < end; r0 = r1) {
     int id = kBehind;
     r1 = end;
     if (r0 < behind) {
       const int s = a.seg.find(r0);
-      const int stop = a.seg.begin(s + 1);
+      const int start = a.seg.begin(s), stop = a.seg.begin(s + 1);
+      if (SPREAD && r0 != row0 && start != r0 && stop > r0) return;
       id = stop > r0 ? a.seg.adapter_of(s) : kNone;
       r1 = min(stop > r0 ? stop : r0 + 1, end);
+    } else if (SPREAD && r0 != row0 && r0 != behind) {
+      return;
     }
-    if (run % gridDim.y != blockIdx.y) continue;
     if (a.ids && threadIdx.x < r1 - r0) a.ids[r0 + threadIdx.x] = id;
     if (id == kBehind) break;
     f32x4 acc[RT][NT];
@@ -169,6 +170,7 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
         }
       }
     }
+    if (SPREAD) return;
   }
 }
 
@@ -182,8 +184,16 @@ struct Up {
   const int32_t* ids;
   void* y;
   int64_t ld_z, ld_y;
-  int32_t rows, cols, outs, rank;
+  int32_t rows, cols, outs, rank, adapters;
+  // (where row numbers are out of order a row's may never have been written)
+  __device__ int id(int row) const {
+    const int i = row < rows ? ids[row] : kBehind;
+    return i < adapters ? i : kNone;
+  }
 };
+
+// Where chunk c of row o of a matrix of CH chunks a row is put in LDS: at c ^ swizzle.
+template <int CH> __device__ inline int swizzle(int o) { return CH == 4 ? o >> 1 & 3 : CH == 8 ? o & 7 : CH == 2 ? o >> 2 & 1 : 0; }
 
 template <int RP> struct Pieces {  // of u for 16 rows, as B operand
   static constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
@@ -213,21 +223,36 @@ template <int RP> struct Factor {  // b of adapter `who` for 16 outputs from out
   }
 };
 
-// The adapters' part for 16 rows (their pieces u, their adapters id: lane n has row n's) and 16 outputs from out0 on: one step per adapter
-// that the rows have.  A column of the result is one row's, so that the others of a step are left out there and nothing of an adapter (an
-// infinity, say) reaches rows that have another.
-template <int RP> __device__ inline f32x4 add_adapters(const Up& a, const Pieces<RP>& u, int id, int out0, f32x4 acc) {
+// The adapters' part for 16 rows (their pieces u, their adapters id: lane n has row n's) and 16 outputs from out0 on, as far as it is
+// wavefront `share` of SHARES'; four adapters' factors are under way at a time.  A column of the result is one row's, so that the others of a step are
+// left out there and nothing of an adapter (an infinity, say) reaches rows that have another.
+template <int RP, int SHARES> __device__ inline f32x4 add_adapters(const Up& a, const Pieces<RP>& u, int id, int out0, int share, f32x4 acc) {
   uint64_t pending = __ballot(id >= 0) & 0xFFFF;
-  while (pending) {
-    const int who = __builtin_amdgcn_readlane(id, __builtin_ctzll(pending));
-    const bool mine = id == who;
-    pending &= ~__ballot(mine);
-    Factor<RP> b;
-    b.load(a, who, out0);
-    f32x4 own = {0, 0, 0, 0};
+  for (int turn = 0; pending;) {
+    int who[4], found = 0;
+    for (; pending && found < 4; ++turn) {
+      const int w = __builtin_amdgcn_readlane(id, __builtin_ctzll(pending));
+      pending &= ~__ballot(id == w);
+      if (turn % SHARES != share) continue;
+      if (found == 0) who[0] = who[1] = who[2] = who[3] = w;
+      else if (found == 1) who[1] = w;
+      else if (found == 2) who[2] = w;
+      else who[3] = w;
+      ++found;
+    }
+    if (!found) break;
+    Factor<RP> b[4];
 #pragma unroll
-    for (int q = 0; q < Factor<RP>::STEPS; ++q) own = mfma(b.f[q], u.f[q], own);
-    if (mine) acc += own;
+    for (int q = 0; q < 4; ++q)
+      if (q < found) b[q].load(a, who[q], out0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q >= found) break;
+      f32x4 own = {0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < Factor<RP>::STEPS; ++s) own = mfma(b[q].f[s], u.f[s], own);
+      if (id == who[q]) acc += own;
+    }
   }
   return acc;
 }
@@ -239,20 +264,24 @@ template <class Y> __device__ inline void store_outs(const Up& a, int row, int i
   store_four<false>((Y*)a.y + (int64_t)row * a.ld_y + out, a.outs - out, f);
 }
 
-// Many rows: a workgroup's tile of TO outputs x TR rows, shared by WO x WR wavefronts, both operands through two buffers in LDS.  A row of a
-// stage is eight chunks of 16 bytes; chunk c is put at place c ^ row % 8, so that the 16 rows of an operand fall on all banks.
+// Many rows: a workgroup's tile of TO outputs x TR rows, shared by WO x WR wavefronts, both operands staged in LDS, kStep contraction indices
+// at a time, kStages of them in turn.  A row of a stage is four chunks of 16 bytes; chunk c is put at place c ^ row / 2 % 4, so that the
+// 16 rows of an operand fall on all banks.
+// What bounds it is how far ahead the stages are sent for: with two buffers of 64 indices (the next one under way while one is
+// multiplied) the matrix cores were busy for 38 % of the time, XX.  So stage s + 4 is sent for when the operands of stage s are in
+// registers, and the operands of stage s + 1 are read from LDS while those of stage s are multiplied; one barrier per stage says both that stage s + 1
+// has arrived and that nobody reads stage s any more.  A contraction that is no multiple of kStep begins with what is over.
 // DIRECT: rows begin at multiples of 16 bytes, and stages go from memory to LDS without passing through registers (a wavefront's load
-// fills 1 KB, eight rows, in the order of its lanes, so each lane fetches the chunk that belongs to its place); else, and for a last stage
-// that is not whole, through registers.
-// TURNED: w is [cols][outs] instead, as the gradient of the rows reads it.  A lane fetches eight rows of four outputs and turns that block
-// over in registers, one byte permutation per pair of elements.
-template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT, bool TURNED>
+// fills 1 KB, sixteen rows, in the order of its lanes, so each lane fetches the chunk that belongs to its place).  Else they go through
+// registers, one stage ahead.
+constexpr int kStep = 32, kStages = 4;
+
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT>
 __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tiles, int out_tiles) {
-  constexpr int WAVES = WO * WR, THREADS = 64 * WAVES, OI = TO / WO / 16, RJ = TR / WR / 16;
-  constexpr int WL = TO / 8 / WAVES, ZL = TR / 8 / WAVES;  // loads of 16 bytes per lane and stage
-  static_assert(WL * 8 * WAVES == TO && ZL * 8 * WAVES == TR && TO * kStep / 32 == THREADS * (TO * kStep / 32 / THREADS), "tile");
-  constexpr int TL = TURNED ? TO * kStep / 32 / THREADS : 1;  // blocks of 8 x 4 per lane
-  __shared__ u32x4 w_tile[2][TO * 8], z_tile[2][TR * 8];
+  constexpr int WAVES = WO * WR, OI = TO / WO / 16, RJ = TR / WR / 16;
+  constexpr int WL = TO / 16 / WAVES, ZL = TR / 16 / WAVES, L = WL + ZL;  // loads of 16 bytes per lane and stage
+  static_assert(WL * 16 * WAVES == TO && ZL * 16 * WAVES == TR, "every wavefront fetches the same number of rows");
+  __shared__ u32x4 w_tile[kStages][TO * 4], z_tile[kStages][TR * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // Workgroups are dealt to the eight XCDs by turns: one XCD gets consecutive tiles, which share rows and outputs in its L2.
   const int tiles = row_tiles * out_tiles;
@@ -269,147 +298,194 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
 #pragma unroll
     for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-  // this lane's place of a load: row lane / 8 of eight, and the chunk that goes there
-  const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 8;
-  const u16* zp[ZL];
-  const u16* wp[WL];
+  // this lane's place of a load: row lane / 4 of sixteen, and the chunk that goes there; rows that do not exist are the last one
+  const int lr = lane >> 2, lc = ((lane & 3) ^ (lr >> 1 & 3)) * 8;
+  const char* z0 = (const char*)(a.z + (int64_t)row0 * a.ld_z);
+  const char* w0 = (const char*)(a.w + (int64_t)out0 * a.cols);
+  uint32_t zo[ZL], wofs[WL];  // bytes behind these (the launcher sees to it that they fit)
 #pragma unroll
-  for (int q = 0; q < ZL; ++q) zp[q] = a.z + (int64_t)min(row0 + (q * WAVES + wave) * 8 + lr, a.rows - 1) * a.ld_z + lc;
+  for (int q = 0; q < ZL; ++q) zo[q] = (uint32_t)(min((q * WAVES + wave) * 16 + lr, a.rows - 1 - row0) * (uint32_t)a.ld_z + lc) * 2;
 #pragma unroll
-  for (int q = 0; q < WL; ++q) wp[q] = a.w + (int64_t)min(out0 + (q * WAVES + wave) * 8 + lr, a.outs - 1) * a.cols + lc;
-  u32x4 zr[ZL], wr_[WL];
-  any_u32x2 tr[TL][8];
-  const bool outs_whole = out0 + TO <= a.outs;
-
-  auto send = [&](u32x4* to, const u16* from) {
+  for (int q = 0; q < WL; ++q) wofs[q] = (uint32_t)(min((q * WAVES + wave) * 16 + lr, a.outs - 1 - out0) * (uint32_t)a.cols + lc) * 2;
+  auto send = [&](u32x4* to, const char* from) {
     __builtin_amdgcn_global_load_lds((const RFAST_GLOBAL void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
-  auto fetch = [&](int c0, int buf) {  // stage from c0 on: into LDS, or into registers for `put`
-    const bool whole = c0 + kStep <= a.cols;
-    if (DIRECT && whole) {
+  const int over = a.cols % kStep, stages = a.cols / kStep + (over ? 1 : 0);
+  auto begin = [&](int s) { return over ? (s == 0 ? a.cols - over : (s - 1) * kStep) : s * kStep; };
+  auto fetch = [&](int s) {
+    const int64_t c = (int64_t)begin(s) * 2;
 #pragma unroll
-      for (int q = 0; q < ZL; ++q) send(&z_tile[buf][(q * WAVES + wave) * 64], zp[q] + c0);
-      if constexpr (!TURNED) {
+    for (int q = 0; q < ZL; ++q) send(&z_tile[s % kStages][(q * WAVES + wave) * 64], z0 + c + zo[q]);
 #pragma unroll
-        for (int q = 0; q < WL; ++q) send(&w_tile[buf][(q * WAVES + wave) * 64], wp[q] + c0);
-      }
-    } else if (whole) {
+    for (int q = 0; q < WL; ++q) send(&w_tile[s % kStages][(q * WAVES + wave) * 64], w0 + c + wofs[q]);
+  };
+  u32x4 zr[ZL], wg[WL];
+  auto take = [&](int s) {
+    const int64_t c = (int64_t)begin(s) * 2;
+    if (s > 0 || !over) {
 #pragma unroll
-      for (int q = 0; q < ZL; ++q) zr[q] = load_eight(zp[q] + c0);
-      if constexpr (!TURNED) {
+      for (int q = 0; q < ZL; ++q) zr[q] = load_eight((const u16*)(z0 + c + zo[q]));
 #pragma unroll
-        for (int q = 0; q < WL; ++q) wr_[q] = load_eight(wp[q] + c0);
-      }
+      for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]));
     } else {
 #pragma unroll
-      for (int q = 0; q < ZL; ++q) zr[q] = load_eight(zp[q] + c0, a.cols - c0 - lc);
-      if constexpr (!TURNED) {
+      for (int q = 0; q < ZL; ++q) zr[q] = load_eight((const u16*)(z0 + c + zo[q]), over - lc);
 #pragma unroll
-        for (int q = 0; q < WL; ++q) wr_[q] = load_eight(wp[q] + c0, a.cols - c0 - lc);
-      }
-    }
-    if constexpr (TURNED) {
-#pragma unroll
-      for (int q = 0; q < TL; ++q) {
-        const int b = q * THREADS + threadIdx.x, k = c0 + b / (TO / 4) * 8, o = out0 + b % (TO / 4) * 4;
-        const u16* p = a.w + (int64_t)k * a.outs + o;
-        if (whole && outs_whole) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) tr[q][i] = *reinterpret_cast<const any_u32x2*>(p + (int64_t)i * a.outs);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const u32x4 v = load_eight(p + (int64_t)i * a.outs, k + i < a.cols ? min(a.outs - o, 4) : 0);
-            tr[q][i] = any_u32x2{v.x, v.y};
-          }
-        }
-      }
+      for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]), over - lc);
     }
   };
-  auto put = [&](int c0, int buf) {
-    if (!DIRECT || c0 + kStep > a.cols) {
+  auto put = [&](int s) {
 #pragma unroll
-      for (int q = 0; q < ZL; ++q) z_tile[buf][(q * WAVES + wave) * 64 + lane] = zr[q];
-      if constexpr (!TURNED) {
+    for (int q = 0; q < ZL; ++q) z_tile[s % kStages][(q * WAVES + wave) * 64 + lane] = zr[q];
 #pragma unroll
-        for (int q = 0; q < WL; ++q) w_tile[buf][(q * WAVES + wave) * 64 + lane] = wr_[q];
-      }
+    for (int q = 0; q < WL; ++q) w_tile[s % kStages][(q * WAVES + wave) * 64 + lane] = wg[q];
+  };
+  // Stage s + 1 has arrived, for all wavefronts (stages s + 2 and s + 3 may be under way; loads return in order), and what was read
+  // from LDS or written there before is done.
+  auto meet = [&](int s) {
+    if (!DIRECT) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (s + 3 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * L) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
+  const int place = g ^ (n >> 1 & 3);
+  auto z_of = [&](int s, int j) { return z_tile[s % kStages][(wr + 16 * j + n) * 4 + place]; };
+  auto w_of = [&](int s, int i) { return w_tile[s % kStages][(wo + 16 * i + n) * 4 + place]; };
+  struct Operands {
+    u32x4 w[OI], z[RJ];
+  } x, y;
+  // (what is read ahead of the last stage is whatever is there, and not used)
+  auto stage = [&](int s, const Operands& now, Operands& next) {
+    meet(s);
+    if (DIRECT) {
+      if (s + kStages < stages) fetch(s + kStages);
+    } else {
+      if (s + 2 < stages) put(s + 2);
+      if (s + 3 < stages) take(s + 3);
     }
-    if constexpr (TURNED) {
 #pragma unroll
-      for (int q = 0; q < TL; ++q) {
-        const int b = q * THREADS + threadIdx.x, c = b / (TO / 4), o = b % (TO / 4) * 4;
+    for (int j = 0; j < RJ; ++j) next.z[j] = z_of(s + 1, j);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          u32x4 v;
+    for (int i = 0; i < OI; ++i) next.w[i] = w_of(s + 1, i);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(tr[q][2 * i + 1][j >> 1], tr[q][2 * i][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-          w_tile[buf][(o + j) * 8 + (c ^ ((o + j) & 7))] = v;
-        }
-      }
+    for (int i = 0; i < OI; ++i)
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) acc[i][j] = mfma(now.w[i], now.z[j], acc[i][j]);
+    // reads and products by turns, so that the reads are through before the products are
+#pragma unroll
+    for (int i = 0; i < OI + RJ; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, OI * RJ / (OI + RJ + 2), 0);
     }
   };
-  // (all of a wavefront's loads into LDS have arrived, then all wavefronts')
-  auto meet = [&] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
-
-  fetch(0, 0);
-  put(0, 0);
-  meet();
-  for (int c0 = 0, buf = 0; c0 < a.cols; c0 += kStep, buf ^= 1) {
-    const bool more = c0 + kStep < a.cols;
-    if (more) fetch(c0 + kStep, buf ^ 1);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      u32x4 wf[OI], zf[RJ];
-#pragma unroll
-      for (int j = 0; j < RJ; ++j) zf[j] = z_tile[buf][(wr + 16 * j + n) * 8 + ((4 * q + g) ^ (n & 7))];
-#pragma unroll
-      for (int i = 0; i < OI; ++i) wf[i] = w_tile[buf][(wo + 16 * i + n) * 8 + ((4 * q + g) ^ (n & 7))];
-#pragma unroll
-      for (int i = 0; i < OI; ++i)
-#pragma unroll
-        for (int j = 0; j < RJ; ++j) acc[i][j] = mfma(wf[i], zf[j], acc[i][j]);
+  if (DIRECT) {
+    if (over) {
+      take(0);
+      put(0);
+    } else {
+      fetch(0);
     }
-    if (more) put(c0 + kStep, buf ^ 1);
-    meet();
+    for (int s = 1; s < kStages; ++s)
+      if (s < stages) fetch(s);
+  } else {
+    take(0);
+    put(0);
+    if (stages > 1) {
+      take(1);
+      put(1);
+    }
+    if (stages > 2) take(2);
   }
+  meet(-1);
+#pragma unroll
+  for (int j = 0; j < RJ; ++j) x.z[j] = z_of(0, j);
+#pragma unroll
+  for (int i = 0; i < OI; ++i) x.w[i] = w_of(0, i);
+  int s = 0;
+  for (; s + 1 < stages; s += 2) {
+    stage(s, x, y);
+    stage(s + 1, y, x);
+  }
+  if (s < stages) stage(s, x, y);
 
-  // The adapters' part.  Usually all rows of a wavefront have the same adapter, whose factors are then fetched once for all of them.
+  // The adapters' part, one run of rows with the same adapter after the other: its factors for the tile's outputs come through LDS (those of
+  // the next run are under way meanwhile), and every wavefront that has rows of the run takes them up.  A column of a product is one
+  // row's, so that the others are left out there and nothing of an adapter (an infinity, say) reaches rows that have another.
+  // (Every wavefront fetching the factors of its own outputs from memory took 100 us of 340 for 8001 x 4096 x 4096, rank 32.)
+  constexpr int CH = RP / 8, MINE = (TO * CH + 64 * WAVES - 1) / (64 * WAVES);  // chunks of an output's factors; chunks of a lane
+  u32x4* factors = &w_tile[0][0];                                              // [TO][CH]
+  int* tile_ids = (int*)&z_tile[0][0];                                         // [TR]
+  static_assert(TO * CH <= kStages * TO * 4, "the factors fit the stages they take the place of");
   int id[RJ];
-  Pieces<RP> u[RJ];
-  bool alike = true;
 #pragma unroll
   for (int j = 0; j < RJ; ++j) {
-    const int row = row0 + wr + 16 * j + n;
-    id[j] = row < a.rows ? a.ids[row] : kBehind;
-    u[j].load(a, min(row, a.rows - 1));
+    id[j] = a.id(row0 + wr + 16 * j + n);
   }
-  const int who = __builtin_amdgcn_readfirstlane(id[0]);
+  Pieces<RP> u[RJ];
+  if (RP <= 32) {
 #pragma unroll
-  for (int j = 0; j < RJ; ++j) alike = alike && __all(id[j] == who);
-#pragma unroll
-  for (int i = 0; i < OI; ++i) {
-    const int o = out0 + wo + 16 * i;
-    if (o >= a.outs) break;
-    if (alike) {
-      if (who >= 0) {
-        Factor<RP> b;
-        b.load(a, who, o);
-#pragma unroll
-        for (int j = 0; j < RJ; ++j)
-#pragma unroll
-          for (int q = 0; q < Factor<RP>::STEPS; ++q) acc[i][j] = mfma(b.f[q], u[j].f[q], acc[i][j]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < RJ; ++j) acc[i][j] = add_adapters<RP>(a, u[j], id[j], o, acc[i][j]);
+    for (int j = 0; j < RJ; ++j) u[j].load(a, min(row0 + wr + 16 * j + n, a.rows - 1));
+  }
+  __syncthreads();  // nobody reads the stages any more
+  for (int r = threadIdx.x; r < TR; r += 64 * WAVES) tile_ids[r] = a.id(row0 + r);
+  __syncthreads();
+  auto run_end = [&](int r) {  // where the run that begins at r ends
+    const int who = tile_ids[r];
+    for (int q = r; q < TR; q += 64) {
+      const uint64_t other = __ballot(q + lane < TR && tile_ids[min(q + lane, TR - 1)] != who);
+      if (other) return q + __builtin_ctzll(other);
     }
+    return TR;
+  };
+  u32x4 mine[MINE];
+  auto take_factors = [&](int who) {
 #pragma unroll
-    for (int j = 0; j < RJ; ++j) store_outs<Y>(a, row0 + wr + 16 * j + n, id[j], o + 4 * g, acc[i][j]);
+    for (int q = 0; q < MINE; ++q) {
+      const int c = q * 64 * WAVES + threadIdx.x, out = min(out0 + c / CH, a.outs - 1), k = c % CH * 8;
+      const u16* b = a.b + ((int64_t)who * a.outs + out) * a.rank + k;
+      mine[q] = a.rank == RP ? load_eight(b) : load_eight(b, a.rank - k);
+    }
+  };
+  int r = 0, who = tile_ids[0], stop = run_end(0);
+  if (who >= 0) take_factors(who);
+  while (r < TR) {
+    if (who >= 0) {
+#pragma unroll
+      for (int q = 0; q < MINE; ++q) {
+        const int c = q * 64 * WAVES + threadIdx.x, o = c / CH;
+        if (c < TO * CH) factors[o * CH + (c % CH ^ swizzle<CH>(o))] = mine[q];
+      }
+    }
+    const int next = stop < TR ? tile_ids[stop] : kNone, next_stop = stop < TR ? run_end(stop) : TR;
+    __syncthreads();
+    if (next >= 0) take_factors(next);
+    if (who >= 0 && r < wr + 16 * RJ && stop > wr) {
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) {
+        const int first = wr + 16 * j;
+        if (r >= first + 16 || stop <= first) continue;
+        if (RP > 32) u[j].load(a, min(row0 + first + n, a.rows - 1));
+        const bool in = first + n >= r && first + n < stop;
+#pragma unroll
+        for (int i = 0; i < OI; ++i) {
+          f32x4 own = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < Pieces<RP>::STEPS; ++q) {
+            const int o = wo + 16 * i + n, k = (32 * q + 8 * g) % RP / 8;
+            own = mfma(factors[o * CH + (k ^ swizzle<CH>(o))], u[j].f[q], own);
+          }
+          if (in) acc[i][j] += own;
+        }
+      }
+    }
+    __syncthreads();
+    r = stop;
+    who = next;
+    stop = next_stop;
   }
+#pragma unroll
+  for (int i = 0; i < OI; ++i)
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) store_outs<Y>(a, row0 + wr + 16 * j + n, id[j], out0 + wo + 16 * i + 4 * g, acc[i][j]);
 }
 
 // Up to 64 rows: bound by one read of W, which goes from memory to the registers of one wavefront and no further.  A workgroup has 16 OT
@@ -452,17 +528,16 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
   for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) chunk(c, [&](const u16* p, int at) { return load_eight(p + at); });
   if (whole < a.cols && wave == whole / CHUNK % WAVES)
     chunk(whole, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
-  // the adapters' part of a tile is one wavefront's, so that the tiles' go on beside each other
+  // (the adapters of a tile are dealt to the wavefronts)
 #pragma unroll
-  for (int t = 0; t < RT; ++t)
+  for (int t = 0; t < RT; ++t) {
+    const int row = 16 * t + n, id = a.id(row);
+    Pieces<RP> u;
+    u.load(a, min(row, a.rows - 1));
 #pragma unroll
     for (int o = 0; o < OT; ++o)
-      if (wave == (t * OT + o) % WAVES && out0 + 16 * o < a.outs) {
-        const int row = 16 * t + n;
-        Pieces<RP> u;
-        u.load(a, min(row, a.rows - 1));
-        acc[o][t] = add_adapters<RP>(a, u, row < a.rows ? a.ids[row] : kBehind, out0 + 16 * o, acc[o][t]);
-      }
+      if (out0 + 16 * o < a.outs) acc[o][t] = add_adapters<RP, WAVES>(a, u, id, out0 + 16 * o, (wave + t) % WAVES, acc[o][t]);
+  }
 #pragma unroll
   for (int o = 0; o < OT; ++o)
 #pragma unroll
@@ -473,7 +548,7 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
 #pragma unroll
     for (int q = 1; q < WAVES; ++q) v += part[q][u][lane];
     const int row = 16 * (u % RT) + n;
-    store_outs<Y>(a, row, row < a.rows ? a.ids[row] : kBehind, out0 + 16 * (u / RT) + 4 * g, v);
+    store_outs<Y>(a, row, a.id(row), out0 + 16 * (u / RT) + 4 * g, v);
   }
 }
 
@@ -604,35 +679,61 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
 }
 
 // -------------------------------------------------------------------------------------------------------- transposes
-// out [batch][cols][rows] = in [batch][rows][cols], of one adapter's matrix or both
+// out [batch][cols][rows] = in [batch][rows][cols], up to three at once.  A wavefront turns 64 x 64 over: a lane reads eight neighbours of
+// eight rows and writes eight neighbours of eight columns, turned over in registers, so that eight lanes cover a line both ways.
 struct Transpose {
   const u16* in;
   u16* out;
   int32_t rows, cols, tiles_x, tiles;  // tiles of 64 x 64 per matrix
+  int32_t batch;
 };
-__global__ void __launch_bounds__(kThreads) rfast_lora_transpose(Transpose a, Transpose b) {
-  __shared__ u16 t[64][66];
-  const bool second = (int)blockIdx.x >= a.tiles;
-  const Transpose q = second ? b : a;
-  const int tile = blockIdx.x - (second ? a.tiles : 0);
-  const int64_t at = (int64_t)blockIdx.y * q.rows * q.cols;
-  const int r0 = tile / q.tiles_x * 64, c0 = tile % q.tiles_x * 64, x = threadIdx.x & 63, high = min(64, q.rows - r0), wide = min(64, q.cols - c0);
-  if (q.cols < 64) {  // (rows are shorter than a wavefront: their elements follow each other)
-    for (int i = threadIdx.x; i < high * wide; i += kThreads) t[i / wide][i % wide] = q.in[at + (int64_t)r0 * q.cols + i];
+struct Transposes {
+  Transpose t[3];
+};
+__global__ void __launch_bounds__(kThreads) rfast_lora_transpose(Transposes a) {
+  int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  Transpose q = a.t[0];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (tile >= (int64_t)q.tiles * q.batch) {
+      tile -= (int64_t)q.tiles * q.batch;
+      q = a.t[i + 1];
+    }
+  if (tile >= (int64_t)q.tiles * q.batch) return;
+  const int lane = threadIdx.x & 63, in_matrix = (int)(tile % q.tiles);
+  const int64_t at = tile / q.tiles * q.rows * q.cols;
+  const int r = in_matrix / q.tiles_x * 64 + lane / 8 * 8, c = in_matrix % q.tiles_x * 64 + lane % 8 * 8;
+  const u16* from = q.in + at + (int64_t)r * q.cols + c;
+  u16* to = q.out + at + (int64_t)c * q.rows + r;
+  u32x4 v[8];
+  const bool whole = r + 8 <= q.rows && c + 8 <= q.cols;
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols);
   } else {
-    for (int i = threadIdx.x >> 6; i < high; i += 4)
-      if (x < wide) t[i][x] = q.in[at + (int64_t)(r0 + i) * q.cols + c0 + x];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols, r + i < q.rows ? q.cols - c : 0);
   }
-  __syncthreads();
-  for (int i = threadIdx.x >> 6; i < wide; i += 4)
-    if (x < high) q.out[at + (int64_t)(c0 + i) * q.rows + r0 + x] = t[x][i];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    any_u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+    if (whole) {
+      *reinterpret_cast<any_u32x4*>(to + (int64_t)j * q.rows) = w;
+    } else if (c + j < q.cols) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + i < q.rows) to[(int64_t)j * q.rows + i] = (u16)(w[i >> 1] >> (16 * (i & 1)));
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
 int padded_rank(int rank) { return rank <= 8 ? 8 : rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
 struct Layout {
-  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, total;
+  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, wt, total;
   int64_t pitch;
 };
 Layout layout_of(const rfast_lora_shape& s, int pass) {
@@ -648,14 +749,16 @@ Layout layout_of(const rfast_lora_shape& s, int pass) {
   l.bt = take(pass != 0 ? n * K * r * 2 : 0);
   l.e_rows = take(pass == 2 ? T * wide * 2 : 0);
   l.at = take(pass == 2 ? n * d * r * 2 : 0);
+  l.wt = take(pass == 2 ? d * K * 2 : 0);
   l.total = off;
   return l;
 }
 
 bool shape_ok(const rfast_lora_shape* s) {
   if (!s || s->rows < 0 || s->segments < 1 || s->adapters < 1 || s->d < 1 || s->K < 1 || s->rank < 1 || s->rank > kMostRank) return false;
-  if (s->rows > 1 << 27 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535 || s->segments == 0x7fffffff) return false;
-  // a launch has fewer than 2^32 lanes
+  if (s->rows > 1 << 27 || s->ld_x > 1 << 22 || s->ld_y > 1 << 22 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535 || s->segments == 0x7fffffff) return false;
+  // a launch has fewer than 2^32 lanes, also one that turns the matrices over
+  if ((int64_t)s->adapters * ((s->K + 63) / 64 + (s->d + 63) / 64) + (int64_t)((s->K + 63) / 64) * ((s->d + 63) / 64) >= (int64_t)1 << 25) return false;
   return ((int64_t)s->rows / 128 + 1) * (std::max(s->d, s->K) / 64 + 1) < (int64_t)1 << 23;
 }
 
@@ -671,44 +774,49 @@ template <class F> hipError_t by_rank(int rank, F f) {
 hipError_t launch_down(const Down& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    const auto go = [&](auto rt, auto waves, int spread) {
+    const auto go = [&](auto rt, auto waves, auto spread) {
       constexpr int RT = decltype(rt)::value, W = decltype(waves)::value;
-      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), spread), dim3(64 * W), 0, st, a);
+      constexpr bool SPREAD = decltype(spread)::value;
+      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W, SPREAD>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), SPREAD ? 16 : 1), dim3(64 * W), 0, st, a);
       return hipGetLastError();
     };
     using std::integral_constant;
-    // with few rows the segments of 16 of them go to workgroups of their own
-    if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::min(16, a.seg.count));
-    if (a.seg.rows <= 8192) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), 1);
-    return go(integral_constant<int, 2>(), integral_constant<int, 4>(), 1);
+    if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::true_type());
+    if (a.seg.rows <= 4096) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::false_type());
+    if (a.seg.rows <= 16384) return go(integral_constant<int, 2>(), integral_constant<int, 8>(), std::false_type());
+    return go(integral_constant<int, 2>(), integral_constant<int, 4>(), std::false_type());
   });
 }
 
-template <int RP, class Y, int TO, int TR, int WO, int WR, bool TURNED> hipError_t launch_up_tiles(const Up& a, hipStream_t st) {
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT> hipError_t launch_up_tiles(const Up& a, hipStream_t st) {
   const int row_tiles = (a.rows + TR - 1) / TR, out_tiles = (a.outs + TO - 1) / TO;
   const dim3 grid((unsigned)row_tiles * out_tiles), block(64 * WO * WR);
-  const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && (TURNED || (a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0));
-  if (direct) hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, true, TURNED>), grid, block, 0, st, a, row_tiles, out_tiles);
-  else hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, false, TURNED>), grid, block, 0, st, a, row_tiles, out_tiles);
+  hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, DIRECT>), grid, block, 0, st, a, row_tiles, out_tiles);
   return hipGetLastError();
 }
 
-// turned: w is [cols][outs]
-template <class Y, bool TURNED> hipError_t launch_up(const Up& a, hipStream_t st) {
+template <class Y> hipError_t launch_up(const Up& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    if constexpr (!TURNED) {
-      if (a.rows <= kFewRows) {
-        const dim3 grid((unsigned)((a.outs + 15) / 16));
-        if (a.rows <= 16) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 1, 8>), grid, dim3(512), 0, st, a);
-        else if (a.rows <= 32) hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 2, 8>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, 1, 4, 8>), grid, dim3(512), 0, st, a);
+    if (a.rows <= kFewRows) {
+      const auto few = [&](auto ot, auto rt) {
+        constexpr int OT = decltype(ot)::value, RT = decltype(rt)::value;
+        hipLaunchKernelGGL((rfast_lora_up_few<RP, Y, OT, RT, 8>), dim3((unsigned)((a.outs + 16 * OT - 1) / (16 * OT))), dim3(512), 0, st, a);
         return hipGetLastError();
-      }
+      };
+      using std::integral_constant;
+      // two blocks of outputs per workgroup read the rows half as often
+      const bool pairs = a.outs >= 32 * 256;
+      if (a.rows <= 16) return few(integral_constant<int, 1>(), integral_constant<int, 1>());
+      if (a.rows <= 32) return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 2>()) : few(integral_constant<int, 1>(), integral_constant<int, 2>());
+      if (a.rows <= 48) return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 3>()) : few(integral_constant<int, 1>(), integral_constant<int, 3>());
+      return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 4>()) : few(integral_constant<int, 1>(), integral_constant<int, 4>());
     }
     const int64_t large = ((int64_t)a.rows + 255) / 256 * ((a.outs + 255) / 256);
-    if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, TURNED>(a, st);
-    return launch_up_tiles<RP, Y, 128, 128, 2, 2, TURNED>(a, st);
+    const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0;
+    if (!direct) return launch_up_tiles<RP, Y, 128, 128, 2, 2, false>(a, st);
+    if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, true>(a, st);
+    return launch_up_tiles<RP, Y, 128, 128, 2, 2, true>(a, st);
   });
 }
 
@@ -719,10 +827,11 @@ template <bool RANK_MAJOR> hipError_t launch_sums(const Sums& a, hipStream_t st)
   });
 }
 
-Transpose transpose_of(const u16* in, u16* out, int rows, int cols) {
+Transpose transpose_of(const void* in, void* out, int rows, int cols, int batch) {
   const int x = (cols + 63) / 64;
-  return {in, out, rows, cols, x, x * ((rows + 63) / 64)};
+  return {(const u16*)in, (u16*)out, rows, cols, x, x * ((rows + 63) / 64), batch};
 }
+int64_t tiles_of(const Transpose& t) { return (int64_t)t.tiles * t.batch; }
 
 bool at_multiple(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 
@@ -760,8 +869,8 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   const Segments seg = {row_ptr, adapter, s->segments, s->adapters, s->rows};
   hipError_t e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale}, st);
   if (e != hipSuccess) return rfast_refuse_hip(e, "adapter launch");
-  const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank};
-  e = s->y_type == RFAST_F32 ? launch_up<float, false>(u, st) : launch_up<u16, false>(u, st);
+  const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank, s->adapters};
+  e = s->y_type == RFAST_F32 ? launch_up<float>(u, st) : launch_up<u16>(u, st);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "projection launch");
 }
 
@@ -782,16 +891,18 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
   int32_t* ids = (int32_t*)(ws + l.ids);
   hipError_t e = hipSuccess;
   if (s->rows > 0) {
-    u16* at = (u16*)(ws + l.at);
-    const Transpose tb = transpose_of((const u16*)B, bt, s->K, s->rank);
-    Transpose ta = transpose_of((const u16*)A, at, s->rank, s->d);
-    if (!dx) ta.tiles = 0;
-    hipLaunchKernelGGL(rfast_lora_transpose, dim3(tb.tiles + ta.tiles, s->adapters), dim3(kThreads), 0, st, tb, ta);
+    Transposes t = {{transpose_of(B, bt, s->K, s->rank, s->adapters), {}, {}}};
+    if (dx) {
+      t.t[1] = transpose_of(A, ws + l.at, s->rank, s->d, s->adapters);
+      t.t[2] = transpose_of(W, ws + l.wt, s->K, s->d, 1);
+    }
+    const int64_t tiles = tiles_of(t.t[0]) + tiles_of(t.t[1]) + tiles_of(t.t[2]);
+    hipLaunchKernelGGL(rfast_lora_transpose, dim3((unsigned)((tiles + 3) / 4)), dim3(kThreads), 0, st, t);
     e = hipGetLastError();
     if (e == hipSuccess) e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
     if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
     if (e == hipSuccess && dx)
-      e = launch_up<u16, true>({(const u16*)dy, (const u16*)W, at, e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank}, st);
+      e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters}, st);
   }
   if (e == hipSuccess) e = launch_sums<true>({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
   if (e == hipSuccess) e = launch_sums<false>({(const u16*)dy, u_cols, dB, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
