@@ -46,6 +46,23 @@ __device__ inline u32x4 load_eight(const u16* p, int64_t left) {
   return t;
 }
 
+// Takes chunks first, first + step, .. below end through load(chunk, operands) and use(operands), the loads of one chunk under way while
+// the one before is used.  (Left to itself the compiler reuses a load's registers as soon as it can, and has a third of a chunk under way:
+// adapters of rank 32 for 8001 rows of 4096 took 51 us so.)
+template <class Operands, class Load, class Use> __device__ inline void pipelined(int first, int end, int step, Load load, Use use) {
+  Operands x, y;
+  if (first < end) load(first, x);
+  for (int c = first; c < end; c += 2 * step) {
+    if (c + step < end) load(c + step, y);
+    __builtin_amdgcn_sched_barrier(0);
+    use(x);
+    if (c + step >= end) break;
+    if (c + 2 * step < end) load(c + 2 * step, x);
+    __builtin_amdgcn_sched_barrier(0);
+    use(y);
+  }
+}
+
 struct Segments {
   const int32_t* row_ptr;
   const int32_t* adapter;
@@ -77,7 +94,9 @@ constexpr int kPieces = 3;  // bf16 that a value of u or e is held as
 //   out_rows [rows][kPieces][RP]    what `up` reads
 //   out_cols [kPieces][RP][pitch]   what `sums` reads: the same by columns
 // A workgroup has 16 RT rows, its WAVES wavefronts share the contraction; rows of several segments are taken one segment after the other,
-// or (SPREAD) by a workgroup each where there are so few rows that a segment is one or two of them.  Rows and ranks that do not
+// or (SPREAD) by a workgroup each where there are so few rows that a segment is one or two of them.  (Without SPREAD two workgroups
+// share them, the first run and the others: one for both took twice as long where a segment ended, and with one workgroup per compute unit the launch
+// with it.)  Rows and ranks that do not
 // exist or belong to another segment are read as the nearest that do, and what comes of them is left out.
 struct Down {
   const u16* z;
@@ -97,8 +116,14 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
   __shared__ f32x4 part[WAVES][RT * NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int row0 = blockIdx.x * (16 * RT), end = min(row0 + 16 * RT, a.seg.rows), behind = a.seg.end_of_all();
-  // SPREAD: workgroup y of sixteen has the run of rows that begins at row y, if one does
-  for (int r0 = SPREAD ? row0 + (int)blockIdx.y : row0, r1; r0 < end; r0 = r1) {
+  int begin = row0;
+  if (SPREAD) {  // workgroup y of sixteen has the run of rows that begins at row y, if one does
+    begin += blockIdx.y;
+  } else if (blockIdx.y > 0) {  // the second of two has all runs but the first
+    begin = row0 < behind ? min(a.seg.begin(a.seg.find(row0) + 1), end) : end;
+    if (begin <= row0) begin = row0 + 1;  // (as the first one has it where the numbers are out of order)
+  }
+  for (int r0 = begin, r1; r0 < end; r0 = r1) {
     int id = kBehind;
     r1 = end;
     if (r0 < behind) {
@@ -124,25 +149,32 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) m[t] = a.m + ((int64_t)id * a.rank + min(t * 16 + n, a.rank - 1)) * a.cols + g * 8;
       const int whole = a.cols / CHUNK * CHUNK;
-      auto chunk = [&](int c, auto load) {
-        u32x4 zf[4][RT], mf[4][NT];
+      struct Operands {
+        u32x4 z[4][RT], m[4][NT];
+      };
+      auto fetch = [&](int c, Operands& o, auto load) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
 #pragma unroll
-          for (int i = 0; i < RT; ++i) zf[q][i] = load(z[i], c + 32 * q);
+          for (int i = 0; i < RT; ++i) o.z[q][i] = load(z[i], c + 32 * q);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mf[q][t] = load(m[t], c + 32 * q);
+          for (int t = 0; t < NT; ++t) o.m[q][t] = load(m[t], c + 32 * q);
         }
+      };
+      auto use = [&](const Operands& o) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) acc[i][t] = mfma(zf[q][i], mf[q][t], acc[i][t]);
+            for (int t = 0; t < NT; ++t) acc[i][t] = mfma(o.z[q][i], o.m[q][t], acc[i][t]);
       };
-      for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) chunk(c, [&](const u16* p, int at) { return load_eight(p + at); });
-      if (whole < a.cols && wave == whole / CHUNK % WAVES)
-        chunk(whole, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+      pipelined<Operands>(wave * CHUNK, whole, WAVES * CHUNK, [&](int c, Operands& o) { fetch(c, o, [&](const u16* p, int at) { return load_eight(p + at); }); }, use);
+      if (whole < a.cols && wave == whole / CHUNK % WAVES) {
+        Operands o;
+        fetch(whole, o, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+        use(o);
+      }
     }
     __syncthreads();  // the sums of the run before have been read
 #pragma unroll
@@ -170,7 +202,7 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
         }
       }
     }
-    if (SPREAD) return;
+    if (SPREAD || blockIdx.y == 0) return;
   }
 }
 
@@ -508,26 +540,33 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) z[t] = a.z + (int64_t)min(16 * t + n, a.rows - 1) * a.ld_z + g * 8;
   const int whole = a.cols / CHUNK * CHUNK;
-  auto chunk = [&](int c, auto load) {
-    u32x4 wf[4][OT], zf[4][RT];
+  struct Operands {
+    u32x4 w[4][OT], z[4][RT];
+  };
+  auto fetch = [&](int c, Operands& f, auto load) {
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int o = 0; o < OT; ++o) wf[q][o] = load(w[o], c + 32 * q);
+      for (int o = 0; o < OT; ++o) f.w[q][o] = load(w[o], c + 32 * q);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) zf[q][t] = load(z[t], c + 32 * q);
+      for (int t = 0; t < RT; ++t) f.z[q][t] = load(z[t], c + 32 * q);
+  };
+  auto use = [&](const Operands& f) {
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
       for (int o = 0; o < OT; ++o)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[o][t] = mfma(wf[q][o], zf[q][t], acc[o][t]);
+        for (int t = 0; t < RT; ++t) acc[o][t] = mfma(f.w[q][o], f.z[q][t], acc[o][t]);
   };
-  for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) chunk(c, [&](const u16* p, int at) { return load_eight(p + at); });
-  if (whole < a.cols && wave == whole / CHUNK % WAVES)
-    chunk(whole, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+  pipelined<Operands>(wave * CHUNK, whole, WAVES * CHUNK, [&](int c, Operands& f) { fetch(c, f, [&](const u16* p, int at) { return load_eight(p + at); }); }, use);
+  if (whole < a.cols && wave == whole / CHUNK % WAVES) {
+    Operands f;
+    fetch(whole, f, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+    use(f);
+  }
   // (the adapters of a tile are dealt to the wavefronts)
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -569,10 +608,10 @@ struct Sums {
 // operands that the pieces of 16 ranks come in: one each, or, of 8 ranks, the first two pieces side by side and the third alone
 template <int RP> constexpr int kFrags = RP == 8 ? 2 : kPieces;
 
-template <int RP, bool RANK_MAJOR>
-__global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
+template <int RP, bool RANK_MAJOR, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rfast_lora_sums(Sums a) {
   constexpr int NT = tiles_of(RP);
-  __shared__ f32x4 part[2][8][NT][64];
+  __shared__ f32x4 part[WAVES / 2][8][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int who = blockIdx.y, c0 = blockIdx.x * 128;
   f32x4 acc[8][NT];
@@ -583,14 +622,16 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
   // A lane's first column, moved back where a tile ends with the row (what it computes twice is written twice alike).
   const bool wide = a.cols >= 8;
   const int c = wide ? min(c0 + 8 * n, a.cols - 8) : 0;
-  auto block = [&](int t0, int end, auto whole) {  // 32 rows from t0 on; whole: all of them exist, and rows have eight columns
+  struct Operands {
+    u32x4 z[8], s[NT][kFrags<RP>];
+  };
+  auto fetch = [&](int t0, int end, Operands& o, auto whole) {  // 32 rows from t0 on; whole: all of them exist, and rows have eight columns
     constexpr bool WHOLE = decltype(whole)::value;
     const int r = t0 + 8 * g;
-    u32x4 z[8], sf[NT][kFrags<RP>];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const u16* p = a.z + (int64_t)(r + i) * a.ld + c;
-      z[i] = WHOLE ? load_eight(p) : load_eight(p, r + i < end ? min(a.cols - c, 8) : 0);
+      o.z[i] = WHOLE ? load_eight(p) : load_eight(p, r + i < end ? min(a.cols - c, 8) : 0);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -598,26 +639,34 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
       for (int i = 0; i < kFrags<RP>; ++i) {
         const int k = (RP == 8 ? 16 * i : RP * i + 16 * t) + n;
         const u16* p = a.s + (int64_t)min(k, kPieces * RP - 1) * a.pitch + r;
-        sf[t][i] = WHOLE ? load_eight(p) : load_eight(p, end - r);
-        if (k >= kPieces * RP) sf[t][i] = u32x4{0, 0, 0, 0};
+        o.s[t][i] = WHOLE ? load_eight(p) : load_eight(p, end - r);
       }
+  };
+  auto use = [&](const Operands& o) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       u32x4 zf;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) zf[q] = __builtin_amdgcn_perm(z[2 * q + 1][j >> 1], z[2 * q][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+      for (int q = 0; q < 4; ++q) zf[q] = __builtin_amdgcn_perm(o.z[2 * q + 1][j >> 1], o.z[2 * q][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < kFrags<RP>; ++i) acc[j][t] = RANK_MAJOR ? mfma(sf[t][i], zf, acc[j][t]) : mfma(zf, sf[t][i], acc[j][t]);
+        for (int i = 0; i < kFrags<RP>; ++i) {
+          u32x4 sf = o.s[t][i];
+          if (RP == 8 && i == 1 && n >= 8) sf = u32x4{0, 0, 0, 0};  // (the third piece has no neighbour)
+          acc[j][t] = RANK_MAJOR ? mfma(sf, zf, acc[j][t]) : mfma(zf, sf, acc[j][t]);
+        }
     }
   };
   auto segment = [&](int s) {
-    const int end = a.seg.begin(s + 1);
-    for (int t0 = a.seg.begin(s) + wave * 32; t0 < end; t0 += kWaves * 32) {
-      if (wide && t0 + 32 <= end) block(t0, end, std::true_type());
-      else block(t0, end, std::false_type());
-    }
+    const int begin = a.seg.begin(s), end = a.seg.begin(s + 1), whole = wide && end > begin ? begin + (end - begin) / 32 * 32 : begin;
+    pipelined<Operands>(begin + wave * 32, whole, WAVES * 32, [&](int t0, Operands& o) { fetch(t0, end, o, std::true_type()); }, use);
+    for (int t0 = whole; t0 < end; t0 += 32)
+      if (wave == (t0 - begin) / 32 % WAVES) {
+        Operands o;
+        fetch(t0, end, o, std::false_type());
+        use(o);
+      }
   };
   if (!a.seg.adapter) {
     if (who < a.seg.count) segment(who);
@@ -629,7 +678,7 @@ __global__ void __launch_bounds__(kThreads) rfast_lora_sums(Sums a) {
   }
   // the wavefronts' sums, two and two
 #pragma unroll
-  for (int half = 2; half >= 1; half >>= 1) {
+  for (int half = WAVES / 2; half >= 1; half >>= 1) {
     __syncthreads();
     if (wave >= half && wave < 2 * half)
 #pragma unroll
@@ -777,13 +826,12 @@ hipError_t launch_down(const Down& a, hipStream_t st) {
     const auto go = [&](auto rt, auto waves, auto spread) {
       constexpr int RT = decltype(rt)::value, W = decltype(waves)::value;
       constexpr bool SPREAD = decltype(spread)::value;
-      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W, SPREAD>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), SPREAD ? 16 : 1), dim3(64 * W), 0, st, a);
+      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W, SPREAD>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), SPREAD ? 16 : 2), dim3(64 * W), 0, st, a);
       return hipGetLastError();
     };
     using std::integral_constant;
     if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::true_type());
-    if (a.seg.rows <= 4096) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::false_type());
-    if (a.seg.rows <= 16384) return go(integral_constant<int, 2>(), integral_constant<int, 8>(), std::false_type());
+    if (a.seg.rows <= 16384) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::false_type());
     return go(integral_constant<int, 2>(), integral_constant<int, 4>(), std::false_type());
   });
 }
@@ -795,7 +843,7 @@ template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT> hipError
   return hipGetLastError();
 }
 
-template <class Y> hipError_t launch_up(const Up& a, hipStream_t st) {
+template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     if (a.rows <= kFewRows) {
@@ -820,9 +868,30 @@ template <class Y> hipError_t launch_up(const Up& a, hipStream_t st) {
   });
 }
 
+template <class Y> hipError_t launch_up(const Up& all, hipStream_t st) {
+  Up a = all;
+  // Where rows over a multiple of 256 would have the card do one more round of tiles that are mostly empty, they are a launch of their own:
+  // 4100 rows, 4096 x 4096, 202 us in 17 x 16 tiles, XX so.
+  const int64_t columns = (a.outs + 255) / 256, units = 256;
+  const int whole = a.rows / 256 * 256;
+  if (whole > 0 && whole < a.rows && (whole / 256 * columns + units - 1) / units < (((int64_t)whole / 256 + 1) * columns + units - 1) / units) {
+    a.rows = whole;
+    Up rest = all;
+    rest.rows -= whole;
+    rest.z += (int64_t)whole * a.ld_z;
+    rest.u += (int64_t)whole * kPieces * padded_rank(a.rank);
+    rest.ids += whole;
+    rest.y = (Y*)a.y + (int64_t)whole * a.ld_y;
+    const hipError_t e = launch_up_rows<Y>(rest, st);
+    if (e != hipSuccess) return e;
+  }
+  return launch_up_rows<Y>(a, st);
+}
+
 template <bool RANK_MAJOR> hipError_t launch_sums(const Sums& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
-    hipLaunchKernelGGL((rfast_lora_sums<decltype(rp)::value, RANK_MAJOR>), dim3((a.cols + 127) / 128, a.seg.adapters), dim3(kThreads), 0, st, a);
+    constexpr int WAVES = 4;
+    hipLaunchKernelGGL((rfast_lora_sums<decltype(rp)::value, RANK_MAJOR, WAVES>), dim3((a.cols + 127) / 128, a.seg.adapters), dim3(64 * WAVES), 0, st, a);
     return hipGetLastError();
   });
 }
