@@ -47,8 +47,7 @@ __device__ inline u32x4 load_eight(const u16* p, int64_t left) {
 }
 
 // Takes chunks first, first + step, .. below end through load(chunk, operands) and use(operands), the loads of one chunk under way while
-// the one before is used.  (Left to itself the compiler reuses a load's registers as soon as it can, and has a third of a chunk under way:
-// adapters of rank 32 for 8001 rows of 4096 took 51 us so.)
+// the one before is used.  (Left to itself the compiler reuses a load's registers as soon as it can, and has a third of a chunk under way.)
 template <class Operands, class Load, class Use> __device__ inline void pipelined(int first, int end, int step, Load load, Use use) {
   Operands x, y;
   if (first < end) load(first, x);
@@ -73,12 +72,15 @@ struct Segments {
     const int a = adapter ? adapter[s] : s;
     return a >= 0 && a < adapters ? a : kNone;
   }
-  // The last segment that does not begin behind `row` (the one that holds it, if any does), found by 64 probes at a time.
-  __device__ int find(int row) const {
-    int lo = 0, hi = count;
+  // Blocks of R rows that no segment shares: segment s has the numbers from begin(s) / R + s on, which is enough for all of its rows before
+  // those of the next one begin (and leaves some numbers without rows).  What is behind the last segment counts as one more.
+  static __host__ __device__ int64_t blocks(int rows, int segments, int R) { return (int64_t)rows / R + segments + 2; }
+  // The segment of block `block`: the last whose numbers do not begin behind it, found by 64 probes at a time.
+  __device__ int find(int block, int R) const {
+    int lo = 0, hi = count + 1;
     while (hi - lo > 1) {
       const int step = (hi - lo + 63) / 64, at = lo + (threadIdx.x & 63) * step;
-      const int before = __popcll(__ballot(at < hi && row_ptr[at] <= row));
+      const int before = __popcll(__ballot(at < hi && begin(min(at, count)) / R + at <= block));
       lo += (before > 0 ? before - 1 : 0) * step;
       hi = min(lo + step, hi);
     }
@@ -89,15 +91,62 @@ struct Segments {
 constexpr int tiles_of(int RP) { return RP < 16 ? 1 : RP / 16; }
 constexpr int kPieces = 3;  // bf16 that a value of u or e is held as
 
+// -------------------------------------------------------------------------------------------------------- transposes
+// out [batch][cols][rows] = in [batch][rows][cols], up to three at once.  A wavefront turns 64 x 64 over: a lane reads eight neighbours of
+// eight rows and writes eight neighbours of eight columns, turned over in registers, so that eight lanes cover a line both ways.
+struct Transpose {
+  const u16* in;
+  u16* out;
+  int32_t rows, cols, tiles_x, tiles;  // tiles of 64 x 64 per matrix
+  int32_t batch;
+};
+struct Transposes {
+  Transpose t[3];
+};
+__device__ inline void turn_over(const Transposes& a, int64_t tile) {
+  Transpose q = a.t[0];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (tile >= (int64_t)q.tiles * q.batch) {
+      tile -= (int64_t)q.tiles * q.batch;
+      q = a.t[i + 1];
+    }
+  if (tile >= (int64_t)q.tiles * q.batch) return;
+  const int lane = threadIdx.x & 63, in_matrix = (int)(tile % q.tiles);
+  const int64_t at = tile / q.tiles * q.rows * q.cols;
+  const int r = in_matrix / q.tiles_x * 64 + lane / 8 * 8, c = in_matrix % q.tiles_x * 64 + lane % 8 * 8;
+  const u16* from = q.in + at + (int64_t)r * q.cols + c;
+  u16* to = q.out + at + (int64_t)c * q.rows + r;
+  u32x4 v[8];
+  const bool whole = r + 8 <= q.rows && c + 8 <= q.cols;
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols, r + i < q.rows ? q.cols - c : 0);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    any_u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+    if (whole) {
+      *reinterpret_cast<any_u32x4*>(to + (int64_t)j * q.rows) = w;
+    } else if (c + j < q.cols) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + i < q.rows) to[(int64_t)j * q.rows + i] = (u16)(w[i >> 1] >> (16 * (i & 1)));
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------------------- down
 // out = scale * (rows of z) x (adapter's matrix m [rank][cols]) in kPieces bf16:
 //   out_rows [rows][kPieces][RP]    what `up` reads
 //   out_cols [kPieces][RP][pitch]   what `sums` reads: the same by columns
-// A workgroup has 16 RT rows, its WAVES wavefronts share the contraction; rows of several segments are taken one segment after the other,
-// or (SPREAD) by a workgroup each where there are so few rows that a segment is one or two of them.  (Without SPREAD two workgroups
-// share them, the first run and the others: one for both took twice as long where a segment ended, and with one workgroup per compute unit the launch
-// with it.)  Rows and ranks that do not
-// exist or belong to another segment are read as the nearest that do, and what comes of them is left out.
+// A workgroup has up to 16 RT rows of one segment, its WAVES wavefronts share the contraction.  Rows and ranks that do not exist are read as
+// the nearest that do, and what comes of them is left out.
 struct Down {
   const u16* z;
   const u16* m;
@@ -108,101 +157,95 @@ struct Down {
   int64_t ld, pitch;
   int32_t cols, rank;
   float scale;
+  int32_t blocks;  // workgroups (in x) for rows; those behind them turn matrices over that the next launch needs
+  Transposes turn;
 };
 
-template <int RP, int RT, int WAVES, bool SPREAD>
+template <int RP, int RT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
   constexpr int NT = tiles_of(RP), CHUNK = 128;
   __shared__ f32x4 part[WAVES][RT * NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  const int row0 = blockIdx.x * (16 * RT), end = min(row0 + 16 * RT, a.seg.rows), behind = a.seg.end_of_all();
-  int begin = row0;
-  if (SPREAD) {  // workgroup y of sixteen has the run of rows that begins at row y, if one does
-    begin += blockIdx.y;
-  } else if (blockIdx.y > 0) {  // the second of two has all runs but the first
-    begin = row0 < behind ? min(a.seg.begin(a.seg.find(row0) + 1), end) : end;
-    if (begin <= row0) begin = row0 + 1;  // (as the first one has it where the numbers are out of order)
+  if ((int)blockIdx.x >= a.blocks) {
+    turn_over(a.turn, (int64_t)((int)blockIdx.x - a.blocks) * WAVES + wave);
+    return;
   }
-  for (int r0 = begin, r1; r0 < end; r0 = r1) {
-    int id = kBehind;
-    r1 = end;
-    if (r0 < behind) {
-      const int s = a.seg.find(r0);
-      const int start = a.seg.begin(s), stop = a.seg.begin(s + 1);
-      if (SPREAD && r0 != row0 && start != r0 && stop > r0) return;
-      id = stop > r0 ? a.seg.adapter_of(s) : kNone;
-      r1 = min(stop > r0 ? stop : r0 + 1, end);
-    } else if (SPREAD && r0 != row0 && r0 != behind) {
-      return;
-    }
-    if (a.ids && threadIdx.x < r1 - r0) a.ids[r0 + threadIdx.x] = id;
-    if (id == kBehind) break;
-    f32x4 acc[RT][NT];
+  constexpr int R = 16 * RT;
+  const int s = a.seg.find(blockIdx.x, R), begin = a.seg.begin(s), stop = s < a.seg.count ? a.seg.begin(s + 1) : a.seg.rows;
+  const int row0 = begin + ((int)blockIdx.x - s - begin / R) * R;
+  if (row0 < begin || row0 >= stop) return;
+  const int r1 = min(row0 + R, stop), id = s < a.seg.count ? a.seg.adapter_of(s) : kBehind;
+  if (a.ids && threadIdx.x < r1 - row0) a.ids[row0 + threadIdx.x] = id;
+  if (id == kBehind) return;
+  f32x4 acc[RT][NT];
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
-    if (id >= 0) {
-      const u16 *z[RT], *m[NT];
+    for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
+  if (id >= 0) {
+    const u16 *z[RT], *m[NT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) z[i] = a.z + (int64_t)min(max(row0 + 16 * i + n, r0), r1 - 1) * a.ld + g * 8;
+    for (int i = 0; i < RT; ++i) z[i] = a.z + (int64_t)min(row0 + 16 * i + n, r1 - 1) * a.ld + g * 8;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) m[t] = a.m + ((int64_t)id * a.rank + min(t * 16 + n, a.rank - 1)) * a.cols + g * 8;
-      const int whole = a.cols / CHUNK * CHUNK;
-      struct Operands {
-        u32x4 z[4][RT], m[4][NT];
-      };
-      auto fetch = [&](int c, Operands& o, auto load) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-#pragma unroll
-          for (int i = 0; i < RT; ++i) o.z[q][i] = load(z[i], c + 32 * q);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) o.m[q][t] = load(m[t], c + 32 * q);
-        }
-      };
-      auto use = [&](const Operands& o) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[i][t] = mfma(o.z[q][i], o.m[q][t], acc[i][t]);
-      };
-      pipelined<Operands>(wave * CHUNK, whole, WAVES * CHUNK, [&](int c, Operands& o) { fetch(c, o, [&](const u16* p, int at) { return load_eight(p + at); }); }, use);
-      if (whole < a.cols && wave == whole / CHUNK % WAVES) {
-        Operands o;
-        fetch(whole, o, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
-        use(o);
-      }
-    }
-    __syncthreads();  // the sums of the run before have been read
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) part[wave][i * NT + t][lane] = acc[i][t];
-    __syncthreads();
-    for (int u = wave; u < RT * NT; u += WAVES) {
-      f32x4 v = part[0][u][lane];
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w) v += part[w][u][lane];
-      const int k = u % NT * 16 + n, first = row0 + u / NT * 16 + 4 * g;
+    for (int t = 0; t < NT; ++t) m[t] = a.m + ((int64_t)id * a.rank + min(t * 16 + n, a.rank - 1)) * a.cols + g * 8;
+    const int whole = a.cols / CHUNK * CHUNK;
+    struct Operands {
+      u32x4 z[4][RT], m[4][NT];
+    };
+    auto fetch = [&](int c, Operands& o, auto load) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = first + q;
-        if (k >= RP || row < r0 || row >= r1) continue;
-        float f = k < a.rank ? v[q] * a.scale : 0.f;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const u16 piece = to_bf16(f);
-          f -= from_bf16(piece);
-          if (!(fabsf(f) < INFINITY)) f = 0.f;  // the value is not finite: the first piece says so, and the others must not undo it
-          if (a.out_rows) a.out_rows[((int64_t)row * kPieces + i) * RP + k] = piece;
-          if (a.out_cols) a.out_cols[(int64_t)(i * RP + k) * a.pitch + row] = piece;
-        }
+        for (int i = 0; i < RT; ++i) o.z[q][i] = load(z[i], c + 32 * q);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o.m[q][t] = load(m[t], c + 32 * q);
+      }
+    };
+    auto use = [&](const Operands& o) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[i][t] = mfma(o.z[q][i], o.m[q][t], acc[i][t]);
+    };
+    // (several workgroups are on a compute unit: what waits in one, another does, and a chunk ahead in registers is none the faster)
+    for (int c = wave * CHUNK; c < whole; c += WAVES * CHUNK) {
+      Operands o;
+      fetch(c, o, [&](const u16* p, int at) { return load_eight(p + at); });
+      __builtin_amdgcn_sched_barrier(0);
+      use(o);
+    }
+    if (whole < a.cols && wave == whole / CHUNK % WAVES) {
+      Operands o;
+      fetch(whole, o, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+      use(o);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) part[wave][i * NT + t][lane] = acc[i][t];
+  __syncthreads();
+  for (int u = wave; u < RT * NT; u += WAVES) {
+    f32x4 v = part[0][u][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += part[w][u][lane];
+    const int k = u % NT * 16 + n, first = row0 + u / NT * 16 + 4 * g;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = first + q;
+      if (k >= RP || row >= r1) continue;
+      float f = k < a.rank ? v[q] * a.scale : 0.f;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const u16 piece = to_bf16(f);
+        f -= from_bf16(piece);
+        if (!(fabsf(f) < INFINITY)) f = 0.f;  // the value is not finite: the first piece says so, and the others must not undo it
+        if (a.out_rows) a.out_rows[((int64_t)row * kPieces + i) * RP + k] = piece;
+        if (a.out_cols) a.out_cols[(int64_t)(i * RP + k) * a.pitch + row] = piece;
       }
     }
-    if (SPREAD || blockIdx.y == 0) return;
   }
 }
 
@@ -525,7 +568,7 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
 constexpr int kFewRows = 64;
 template <int RP, class Y, int OT, int RT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
-  constexpr int CHUNK = 128;
+  constexpr int Q = 4, CHUNK = 32 * Q;
   __shared__ f32x4 part[WAVES][OT * RT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int out0 = blockIdx.x * (16 * OT);
@@ -541,21 +584,21 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
   for (int t = 0; t < RT; ++t) z[t] = a.z + (int64_t)min(16 * t + n, a.rows - 1) * a.ld_z + g * 8;
   const int whole = a.cols / CHUNK * CHUNK;
   struct Operands {
-    u32x4 w[4][OT], z[4][RT];
+    u32x4 w[Q][OT], z[Q][RT];
   };
   auto fetch = [&](int c, Operands& f, auto load) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int o = 0; o < OT; ++o) f.w[q][o] = load(w[o], c + 32 * q);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int t = 0; t < RT; ++t) f.z[q][t] = load(z[t], c + 32 * q);
   };
   auto use = [&](const Operands& f) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int o = 0; o < OT; ++o)
 #pragma unroll
@@ -609,11 +652,10 @@ struct Sums {
 template <int RP> constexpr int kFrags = RP == 8 ? 2 : kPieces;
 
 template <int RP, bool RANK_MAJOR, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) rfast_lora_sums(Sums a) {
+__device__ inline void sums_of(const Sums& a, int tile, f32x4 (*part)[8][tiles_of(RP)][64]) {
   constexpr int NT = tiles_of(RP);
-  __shared__ f32x4 part[WAVES / 2][8][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  const int who = blockIdx.y, c0 = blockIdx.x * 128;
+  const int who = blockIdx.y, c0 = tile * 128;
   f32x4 acc[8][NT];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
@@ -727,55 +769,12 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_sums(Sums a) {
   }
 }
 
-// -------------------------------------------------------------------------------------------------------- transposes
-// out [batch][cols][rows] = in [batch][rows][cols], up to three at once.  A wavefront turns 64 x 64 over: a lane reads eight neighbours of
-// eight rows and writes eight neighbours of eight columns, turned over in registers, so that eight lanes cover a line both ways.
-struct Transpose {
-  const u16* in;
-  u16* out;
-  int32_t rows, cols, tiles_x, tiles;  // tiles of 64 x 64 per matrix
-  int32_t batch;
-};
-struct Transposes {
-  Transpose t[3];
-};
-__global__ void __launch_bounds__(kThreads) rfast_lora_transpose(Transposes a) {
-  int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  Transpose q = a.t[0];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (tile >= (int64_t)q.tiles * q.batch) {
-      tile -= (int64_t)q.tiles * q.batch;
-      q = a.t[i + 1];
-    }
-  if (tile >= (int64_t)q.tiles * q.batch) return;
-  const int lane = threadIdx.x & 63, in_matrix = (int)(tile % q.tiles);
-  const int64_t at = tile / q.tiles * q.rows * q.cols;
-  const int r = in_matrix / q.tiles_x * 64 + lane / 8 * 8, c = in_matrix % q.tiles_x * 64 + lane % 8 * 8;
-  const u16* from = q.in + at + (int64_t)r * q.cols + c;
-  u16* to = q.out + at + (int64_t)c * q.rows + r;
-  u32x4 v[8];
-  const bool whole = r + 8 <= q.rows && c + 8 <= q.cols;
-  if (whole) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols, r + i < q.rows ? q.cols - c : 0);
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    any_u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-    if (whole) {
-      *reinterpret_cast<any_u32x4*>(to + (int64_t)j * q.rows) = w;
-    } else if (c + j < q.cols) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (r + i < q.rows) to[(int64_t)j * q.rows + i] = (u16)(w[i >> 1] >> (16 * (i & 1)));
-    }
-  }
+// dA and dB in one launch: the first `tiles_a` tiles of columns are dA's
+template <int RP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rfast_lora_sums(Sums a, Sums b, int tiles_a) {
+  __shared__ f32x4 part[WAVES / 2][8][tiles_of(RP)][64];
+  if ((int)blockIdx.x < tiles_a) sums_of<RP, true, WAVES>(a, blockIdx.x, part);
+  else sums_of<RP, false, WAVES>(b, blockIdx.x - tiles_a, part);
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -805,7 +804,7 @@ Layout layout_of(const rfast_lora_shape& s, int pass) {
 
 bool shape_ok(const rfast_lora_shape* s) {
   if (!s || s->rows < 0 || s->segments < 1 || s->adapters < 1 || s->d < 1 || s->K < 1 || s->rank < 1 || s->rank > kMostRank) return false;
-  if (s->rows > 1 << 27 || s->ld_x > 1 << 22 || s->ld_y > 1 << 22 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535 || s->segments == 0x7fffffff) return false;
+  if (s->segments > 1 << 22 || s->rows > 1 << 26 || s->ld_x > 1 << 22 || s->ld_y > 1 << 22 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535 || s->segments == 0x7fffffff) return false;
   // a launch has fewer than 2^32 lanes, also one that turns the matrices over
   if ((int64_t)s->adapters * ((s->K + 63) / 64 + (s->d + 63) / 64) + (int64_t)((s->K + 63) / 64) * ((s->d + 63) / 64) >= (int64_t)1 << 25) return false;
   return ((int64_t)s->rows / 128 + 1) * (std::max(s->d, s->K) / 64 + 1) < (int64_t)1 << 23;
@@ -820,19 +819,26 @@ template <class F> hipError_t by_rank(int rank, F f) {
   }
 }
 
+Transpose transpose_of(const void* in, void* out, int rows, int cols, int batch) {
+  const int x = (cols + 63) / 64;
+  return {(const u16*)in, (u16*)out, rows, cols, x, x * ((rows + 63) / 64), batch};
+}
+int64_t tiles_of(const Transpose& t) { return (int64_t)t.tiles * t.batch; }
+
 hipError_t launch_down(const Down& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    const auto go = [&](auto rt, auto waves, auto spread) {
+    const auto go = [&](auto rt, auto waves) {
       constexpr int RT = decltype(rt)::value, W = decltype(waves)::value;
-      constexpr bool SPREAD = decltype(spread)::value;
-      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W, SPREAD>), dim3((a.seg.rows + 16 * RT - 1) / (16 * RT), SPREAD ? 16 : 2), dim3(64 * W), 0, st, a);
+      Down b = a;
+      b.blocks = (int32_t)Segments::blocks(a.seg.rows, a.seg.count, 16 * RT);
+      const int64_t tiles = tiles_of(a.turn.t[0]) + tiles_of(a.turn.t[1]) + tiles_of(a.turn.t[2]);
+      hipLaunchKernelGGL((rfast_lora_down<RP, RT, W>), dim3((unsigned)(b.blocks + (tiles + W - 1) / W)), dim3(64 * W), 0, st, b);
       return hipGetLastError();
     };
     using std::integral_constant;
-    if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::true_type());
-    if (a.seg.rows <= 16384) return go(integral_constant<int, 1>(), integral_constant<int, 8>(), std::false_type());
-    return go(integral_constant<int, 2>(), integral_constant<int, 4>(), std::false_type());
+    if (a.seg.rows <= 1024) return go(integral_constant<int, 1>(), integral_constant<int, 8>());
+    return go(integral_constant<int, 2>(), integral_constant<int, 4>());
   });
 }
 
@@ -853,12 +859,14 @@ template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
         return hipGetLastError();
       };
       using std::integral_constant;
-      // two blocks of outputs per workgroup read the rows half as often
-      const bool pairs = a.outs >= 32 * 256;
-      if (a.rows <= 16) return few(integral_constant<int, 1>(), integral_constant<int, 1>());
-      if (a.rows <= 32) return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 2>()) : few(integral_constant<int, 1>(), integral_constant<int, 2>());
-      if (a.rows <= 48) return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 3>()) : few(integral_constant<int, 1>(), integral_constant<int, 3>());
-      return pairs ? few(integral_constant<int, 2>(), integral_constant<int, 4>()) : few(integral_constant<int, 1>(), integral_constant<int, 4>());
+      // Two blocks of outputs per workgroup read the rows, from L2, half as often, but there have to be workgroups enough: 48 rows, 4096 x 8192
+      // (without adapters) 34 us with one, 29 with two, 45 with four (15 without the rows).
+      const auto by_rows = [&](auto ot) {
+        if (a.rows <= 16) return few(ot, integral_constant<int, 1>());
+        if (a.rows <= 32) return few(ot, integral_constant<int, 2>());
+        return a.rows <= 48 ? few(ot, integral_constant<int, 3>()) : few(ot, integral_constant<int, 4>());
+      };
+      return a.outs >= 32 * 256 ? by_rows(integral_constant<int, 2>()) : by_rows(integral_constant<int, 1>());
     }
     const int64_t large = ((int64_t)a.rows + 255) / 256 * ((a.outs + 255) / 256);
     const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0;
@@ -888,19 +896,14 @@ template <class Y> hipError_t launch_up(const Up& all, hipStream_t st) {
   return launch_up_rows<Y>(a, st);
 }
 
-template <bool RANK_MAJOR> hipError_t launch_sums(const Sums& a, hipStream_t st) {
+hipError_t launch_sums(const Sums& a, const Sums& b, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int WAVES = 4;
-    hipLaunchKernelGGL((rfast_lora_sums<decltype(rp)::value, RANK_MAJOR, WAVES>), dim3((a.cols + 127) / 128, a.seg.adapters), dim3(64 * WAVES), 0, st, a);
+    const int tiles_a = (a.cols + 127) / 128, tiles_b = (b.cols + 127) / 128;
+    hipLaunchKernelGGL((rfast_lora_sums<decltype(rp)::value, WAVES>), dim3(tiles_a + tiles_b, a.seg.adapters), dim3(64 * WAVES), 0, st, a, b, tiles_a);
     return hipGetLastError();
   });
 }
-
-Transpose transpose_of(const void* in, void* out, int rows, int cols, int batch) {
-  const int x = (cols + 63) / 64;
-  return {(const u16*)in, (u16*)out, rows, cols, x, x * ((rows + 63) / 64), batch};
-}
-int64_t tiles_of(const Transpose& t) { return (int64_t)t.tiles * t.batch; }
 
 bool at_multiple(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 
@@ -936,7 +939,7 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   const Layout l = layout_of(*s, 0);
   char* ws = (char*)workspace;
   const Segments seg = {row_ptr, adapter, s->segments, s->adapters, s->rows};
-  hipError_t e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale}, st);
+  hipError_t e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale, 0, {}}, st);
   if (e != hipSuccess) return rfast_refuse_hip(e, "adapter launch");
   const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank, s->adapters};
   e = s->y_type == RFAST_F32 ? launch_up<float>(u, st) : launch_up<u16>(u, st);
@@ -965,16 +968,14 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
       t.t[1] = transpose_of(A, ws + l.at, s->rank, s->d, s->adapters);
       t.t[2] = transpose_of(W, ws + l.wt, s->K, s->d, 1);
     }
-    const int64_t tiles = tiles_of(t.t[0]) + tiles_of(t.t[1]) + tiles_of(t.t[2]);
-    hipLaunchKernelGGL(rfast_lora_transpose, dim3((unsigned)((tiles + 3) / 4)), dim3(kThreads), 0, st, t);
-    e = hipGetLastError();
-    if (e == hipSuccess) e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
-    if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
+    e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f, 0, t}, st);
+    if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale, 0, {}}, st);
     if (e == hipSuccess && dx)
       e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters}, st);
   }
-  if (e == hipSuccess) e = launch_sums<true>({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f}, st);
-  if (e == hipSuccess) e = launch_sums<false>({(const u16*)dy, u_cols, dB, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
+  if (e == hipSuccess)
+    e = launch_sums({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f},
+                    {(const u16*)dy, u_cols, dB, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale}, st);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "adapter gradient launch");
 }
 

@@ -52,7 +52,7 @@ def _call(device, f, *args):
 
 def _matrix(t, name, rows, cols, dtype, device):
     """Distance of the rows of a [rows][cols] tensor whose columns are neighbours."""
-    if tuple(t.shape) != (rows, cols) or t.device != device or (dtype is not None and t.dtype != dtype):
+    if t.shape != (rows, cols) or t.device != device or (dtype is not None and t.dtype != dtype):
         raise RFastError(-1, f"{name}: need a tensor of shape ({rows}, {cols}) and type {dtype or t.dtype} on {device}, "
                              f"got {tuple(t.shape)}, {t.dtype} on {t.device}")
     if t.is_contiguous():
@@ -104,6 +104,20 @@ def rfast_lora_workspace_bytes(shape, which):
     return int(lib().rfast_lora_workspace_bytes(C.byref(shape), which))
 
 
+_shapes = {}
+
+
+def _lora_shape(*sizes):
+    """(RfastLoraShape by reference, its workspaces in bytes) of these sizes."""
+    got = _shapes.get(sizes)
+    if got is None:
+        if len(_shapes) >= 4096:
+            _shapes.clear()
+        shape = RfastLoraShape(*sizes)
+        got = _shapes[sizes] = (C.byref(shape), tuple(int(lib().rfast_lora_workspace_bytes(C.byref(shape), k)) for k in range(3)))
+    return got
+
+
 def _lora(x, w, a, b, row_ptr, adapter, y_type, ld_y, scale, which):
     torch = _torch
     bf16, dev = torch.bfloat16, x.device
@@ -112,18 +126,18 @@ def _lora(x, w, a, b, row_ptr, adapter, y_type, ld_y, scale, which):
     T, d = x.shape
     K, (n, r, _) = w.shape[0], a.shape
     for t, name, want in ((w, "w", (K, d)), (a, "a", (n, r, d)), (b, "b", (n, K, r))):
-        if t.dtype != bf16 or t.device != dev or tuple(t.shape) != want or not t.is_contiguous():
+        if t.shape != want or t.dtype != bf16 or t.device != dev or not t.is_contiguous():
             raise RFastError(-1, f"{name}: need a contiguous bfloat16 tensor of shape {want} on {dev}, got {t.dtype}, {tuple(t.shape)} on {t.device}")
     ld_x = _matrix(x, "x", T, d, bf16, dev)
     S = row_ptr.numel() - 1
     p_ptr = _vector(row_ptr, "row_ptr", S + 1, torch.int32, dev)
     p_ad = None if adapter is None else _vector(adapter, "adapter", S, torch.int32, dev)
-    shape = RfastLoraShape(T, S, n, d, K, r, ld_x, ld_y, y_type, scale)
-    nbytes = lib().rfast_lora_workspace_bytes(C.byref(shape), which)
+    shape, nbytes = _lora_shape(T, S, n, d, K, r, ld_x, ld_y, y_type, scale)
+    nbytes = nbytes[which]
     if nbytes == 0 and T > 0:
         raise RFastError(-1, "sizes out of range (at least one segment; rank 1 .. 64)")
     ws = torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)
-    return dev, shape, (x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), p_ptr, p_ad), ws
+    return dev, ld_x, (shape, x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), p_ptr, p_ad), (ws.data_ptr(), nbytes or 256), ws
 
 
 def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, out_dtype=None):
@@ -138,8 +152,8 @@ def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, o
     else:
         _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
         ld_y = _matrix(out, "out", T, K, None, x.device)
-    dev, shape, ptrs, ws = _lora(x, w, a, b, row_ptr, adapter, _type(out, "out"), ld_y, scale, 0)
-    _call(dev, lib().rfast_lora_forward, C.byref(shape), *ptrs, out.data_ptr(), ws.data_ptr(), ws.numel())
+    dev, _, given, work, _keep = _lora(x, w, a, b, row_ptr, adapter, _type(out, "out"), ld_y, scale, 0)
+    _call(dev, lib().rfast_lora_forward, *given, out.data_ptr(), *work)
     return out
 
 
@@ -150,15 +164,15 @@ def rfast_lora_backward(x, w, a, b, row_ptr, adapter, dy, scale=1.0, need_dx=Tru
     T, d = x.shape
     ld_y = _matrix(dy, "dy", T, w.shape[0], torch.bfloat16, x.device)
     with_dx = need_dx or dx is not None
-    dev, shape, ptrs, ws = _lora(x, w, a, b, row_ptr, adapter, BF16, ld_y, scale, 2 if with_dx else 1)
+    dev, ld_x, given, work, _keep = _lora(x, w, a, b, row_ptr, adapter, BF16, ld_y, scale, 2 if with_dx else 1)
     if dx is not None:
-        _need(_matrix(dx, "dx", T, d, torch.bfloat16, dev) == shape.ld_x or T <= 1, "dx: its rows must be as far apart as x's")
+        _need(_matrix(dx, "dx", T, d, torch.bfloat16, dev) == ld_x or T <= 1, "dx: its rows must be as far apart as x's")
     elif with_dx:
-        dx = torch.empty_strided((T, d), (shape.ld_x, 1), dtype=torch.bfloat16, device=dev)
+        dx = torch.empty_strided((T, d), (ld_x, 1), dtype=torch.bfloat16, device=dev)
     da = torch.empty(a.shape, dtype=torch.float32, device=dev) if da is None else da
     db = torch.empty(b.shape, dtype=torch.float32, device=dev) if db is None else db
-    _call(dev, lib().rfast_lora_backward, C.byref(shape), *ptrs, dy.data_ptr(), None if dx is None else dx.data_ptr(),
-          _vector(da, "da", a.numel(), torch.float32, dev), _vector(db, "db", b.numel(), torch.float32, dev), ws.data_ptr(), ws.numel())
+    _call(dev, lib().rfast_lora_backward, *given, dy.data_ptr(), None if dx is None else dx.data_ptr(),
+          _vector(da, "da", a.numel(), torch.float32, dev), _vector(db, "db", b.numel(), torch.float32, dev), *work)
     return dx, da, db
 
 
