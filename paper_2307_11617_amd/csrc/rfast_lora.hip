@@ -260,6 +260,10 @@ struct Up {
   void* y;
   int64_t ld_z, ld_y;
   int32_t rows, cols, outs, rank, adapters;
+  // rfast_lora_up with FUSED: u is formed there, from the first factors
+  const u16* m;  // [adapters][rank][cols]
+  Segments seg;
+  float scale;
   // (where row numbers are out of order a row's may never have been written)
   __device__ int id(int row) const {
     const int i = row < rows ? ids[row] : kBehind;
@@ -273,15 +277,16 @@ template <int CH> __device__ inline int swizzle(int o) { return CH == 4 ? o >> 1
 template <int RP> struct Pieces {  // of u for 16 rows, as B operand
   static constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
   u32x4 f[STEPS];
-  __device__ void load(const Up& a, int row) {
+  __device__ void load(const u16* pieces, int row) {
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int q = 0; q < STEPS; ++q) {
       const int k = 32 * q + 8 * g;
-      f[q] = load_eight(a.u + (int64_t)row * WIDE + min(k, WIDE - 8));
+      f[q] = load_eight(pieces + (int64_t)row * WIDE + min(k, WIDE - 8));
       if (k >= WIDE) f[q] = u32x4{0, 0, 0, 0};
     }
   }
+  __device__ void load(const Up& a, int row) { load(a.u, row); }
 };
 template <int RP> struct Factor {  // b of adapter `who` for 16 outputs from out0 on, as A operand
   static constexpr int WIDE = kPieces * RP, STEPS = (WIDE + 31) / 32;
@@ -349,22 +354,39 @@ template <class Y> __device__ inline void store_outs(const Up& a, int row, int i
 // DIRECT: rows begin at multiples of 16 bytes, and stages go from memory to LDS without passing through registers (a wavefront's load
 // fills 1 KB, sixteen rows, in the order of its lanes, so each lane fetches the chunk that belongs to its place).  Else they go through
 // registers, one stage ahead.
+// FUSED: few outputs (one tile of them), so that the pass of `down` over the rows would cost as much as this one.  A workgroup has rows of one
+// segment only, the first factors of its adapter are some more rows of w, and what they come to is handed on through LDS: 32768 rows of 128 nodes, 1024 x
+// 128, rank 8: 21 + 22 us in two passes, XX so.
 constexpr int kStep = 32, kStages = 4;
 
-template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT>
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT, bool FUSED>
 __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tiles, int out_tiles) {
   constexpr int WAVES = WO * WR, OI = TO / WO / 16, RJ = TR / WR / 16;
-  constexpr int WL = TO / 16 / WAVES, ZL = TR / 16 / WAVES, L = WL + ZL;  // loads of 16 bytes per lane and stage
+  constexpr int UT = FUSED ? tiles_of(RP) : 0, UJ = RJ / WO;                    // blocks of ranks; blocks of rows whose u a wavefront forms
+  constexpr int WL = TO / 16 / WAVES, ZL = TR / 16 / WAVES, L = WL + ZL + UT;  // loads per lane and stage, of 16 bytes (of u: 4)
   static_assert(WL * 16 * WAVES == TO && ZL * 16 * WAVES == TR, "every wavefront fetches the same number of rows");
-  __shared__ u32x4 w_tile[kStages][TO * 4], z_tile[kStages][TR * 4];
+  static_assert(!FUSED || (DIRECT && WAVES == 4 && RJ % WO == 0 && TR * kPieces * RP * 2 <= kStages * TR * 64), "fused");
+  __shared__ u32x4 w_tile[kStages][TO * 4], z_tile[kStages][TR * 4], m_tile[FUSED ? kStages : 1][FUSED ? UT * 64 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  // Workgroups are dealt to the eight XCDs by turns: one XCD gets consecutive tiles, which share rows and outputs in its L2.
-  const int tiles = row_tiles * out_tiles;
-  int t = blockIdx.x;
-  if (tiles % 8 == 0) t = t % 8 * (tiles / 8) + t / 8;
-  // bands of eight tiles of rows, within a band output by output
-  const int band = t / (8 * out_tiles), in_band = t - band * 8 * out_tiles, high = min(8, row_tiles - 8 * band);
-  const int row0 = (band * 8 + in_band % high) * TR, out0 = in_band / high * TO;
+  int row0, out0, rows_end, own = kNone;
+  if (FUSED) {
+    const int q = a.seg.find(blockIdx.x, TR), begin = a.seg.begin(q), stop = q < a.seg.count ? a.seg.begin(q + 1) : begin;
+    row0 = begin + ((int)blockIdx.x - q - begin / TR) * TR;
+    if (row0 < begin || row0 >= stop) return;
+    rows_end = min(row0 + TR, stop);
+    out0 = 0;
+    own = a.seg.adapter_of(q);
+  } else {
+    // Workgroups are dealt to the eight XCDs by turns: one XCD gets consecutive tiles, which share rows and outputs in its L2.
+    const int tiles = row_tiles * out_tiles;
+    int t = blockIdx.x;
+    if (tiles % 8 == 0) t = t % 8 * (tiles / 8) + t / 8;
+    // bands of eight tiles of rows, within a band output by output
+    const int band = t / (8 * out_tiles), in_band = t - band * 8 * out_tiles, high = min(8, row_tiles - 8 * band);
+    row0 = (band * 8 + in_band % high) * TR;
+    out0 = in_band / high * TO;
+    rows_end = a.rows;
+  }
   const int wo = wave / WR * (TO / WO), wr = wave % WR * (TR / WR);
 
   f32x4 acc[OI][RJ];
@@ -379,12 +401,23 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
   const char* w0 = (const char*)(a.w + (int64_t)out0 * a.cols);
   uint32_t zo[ZL], wofs[WL];  // bytes behind these (the launcher sees to it that they fit)
 #pragma unroll
-  for (int q = 0; q < ZL; ++q) zo[q] = (uint32_t)(min((q * WAVES + wave) * 16 + lr, a.rows - 1 - row0) * (uint32_t)a.ld_z + lc) * 2;
+  for (int q = 0; q < ZL; ++q) zo[q] = (uint32_t)(min((q * WAVES + wave) * 16 + lr, rows_end - 1 - row0) * (uint32_t)a.ld_z + lc) * 2;
 #pragma unroll
   for (int q = 0; q < WL; ++q) wofs[q] = (uint32_t)(min((q * WAVES + wave) * 16 + lr, a.outs - 1 - out0) * (uint32_t)a.cols + lc) * 2;
   auto send = [&](u32x4* to, const char* from) {
     __builtin_amdgcn_global_load_lds((const RFAST_GLOBAL void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
+  // of 16 ranks a wavefront fetches four, four bytes per lane
+  const char* m0 = nullptr;
+  uint32_t mo[FUSED ? UT : 1];
+  if (FUSED) {
+    m0 = (const char*)(a.m + (int64_t)max(own, 0) * a.rank * a.cols);
+#pragma unroll
+    for (int q = 0; q < UT; ++q) {
+      const int k = 4 * wave + (lane >> 4), chunk = (lane >> 2 & 3) ^ (k >> 1 & 3);
+      mo[q] = (uint32_t)min(16 * q + k, a.rank - 1) * (uint32_t)a.cols * 2 + chunk * 16 + (lane & 3) * 4;
+    }
+  }
   const int over = a.cols % kStep, stages = a.cols / kStep + (over ? 1 : 0);
   auto begin = [&](int s) { return over ? (s == 0 ? a.cols - over : (s - 1) * kStep) : s * kStep; };
   auto fetch = [&](int s) {
@@ -393,8 +426,12 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
     for (int q = 0; q < ZL; ++q) send(&z_tile[s % kStages][(q * WAVES + wave) * 64], z0 + c + zo[q]);
 #pragma unroll
     for (int q = 0; q < WL; ++q) send(&w_tile[s % kStages][(q * WAVES + wave) * 64], w0 + c + wofs[q]);
+#pragma unroll
+    for (int q = 0; q < UT; ++q)
+      __builtin_amdgcn_global_load_lds((const RFAST_GLOBAL void*)(uintptr_t)(m0 + c + mo[q]),
+                                       (__attribute__((address_space(3))) void*)&m_tile[s % kStages][q * 64 + wave * 16], 4, 0, 0);
   };
-  u32x4 zr[ZL], wg[WL];
+  u32x4 zr[ZL], wg[WL], mg[FUSED ? UT : 1];
   auto take = [&](int s) {
     const int64_t c = (int64_t)begin(s) * 2;
     if (s > 0 || !over) {
@@ -407,6 +444,9 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
       for (int q = 0; q < ZL; ++q) zr[q] = load_eight((const u16*)(z0 + c + zo[q]), over - lc);
 #pragma unroll
       for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]), over - lc);
+#pragma unroll
+      for (int q = 0; q < UT; ++q)  // (every wavefront fetches and puts all sixteen ranks of a block here)
+        mg[q] = load_eight((const u16*)(m0 + c) + (int64_t)min(16 * q + lr, a.rank - 1) * a.cols + lc, over - lc);
     }
   };
   auto put = [&](int s) {
@@ -414,6 +454,8 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
     for (int q = 0; q < ZL; ++q) z_tile[s % kStages][(q * WAVES + wave) * 64 + lane] = zr[q];
 #pragma unroll
     for (int q = 0; q < WL; ++q) w_tile[s % kStages][(q * WAVES + wave) * 64 + lane] = wg[q];
+#pragma unroll
+    for (int q = 0; q < UT; ++q) m_tile[s % kStages][q * 64 + lane] = mg[q];
   };
   // Stage s + 1 has arrived, for all wavefronts (stages s + 2 and s + 3 may be under way; loads return in order), and what was read
   // from LDS or written there before is done.
@@ -426,8 +468,15 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
   auto z_of = [&](int s, int j) { return z_tile[s % kStages][(wr + 16 * j + n) * 4 + place]; };
   auto w_of = [&](int s, int i) { return w_tile[s % kStages][(wo + 16 * i + n) * 4 + place]; };
   struct Operands {
-    u32x4 w[OI], z[RJ];
+    u32x4 w[OI], z[RJ], m[FUSED ? UT : 1];
   } x, y;
+  auto m_of = [&](int s, int t) { return m_tile[s % kStages][(16 * t + n) * 4 + place]; };
+  const int first_j = FUSED ? wave / WR * UJ : 0;  // the blocks of rows whose u this wavefront forms
+  f32x4 form[FUSED ? UT : 1][UJ];
+#pragma unroll
+  for (int t = 0; t < UT; ++t)
+#pragma unroll
+    for (int j = 0; j < UJ; ++j) form[t][j] = f32x4{0, 0, 0, 0};
   // (what is read ahead of the last stage is whatever is there, and not used)
   auto stage = [&](int s, const Operands& now, Operands& next) {
     meet(s);
@@ -442,9 +491,15 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
 #pragma unroll
     for (int i = 0; i < OI; ++i) next.w[i] = w_of(s + 1, i);
 #pragma unroll
+    for (int t = 0; t < UT; ++t) next.m[t] = m_of(s + 1, t);
+#pragma unroll
     for (int i = 0; i < OI; ++i)
 #pragma unroll
       for (int j = 0; j < RJ; ++j) acc[i][j] = mfma(now.w[i], now.z[j], acc[i][j]);
+#pragma unroll
+    for (int t = 0; t < UT; ++t)
+#pragma unroll
+      for (int j = 0; j < UJ; ++j) form[t][j] = mfma(now.m[t], first_j == 0 ? now.z[j] : now.z[UJ + j], form[t][j]);
     // reads and products by turns, so that the reads are through before the products are
 #pragma unroll
     for (int i = 0; i < OI + RJ; ++i) {
@@ -475,6 +530,8 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
   for (int j = 0; j < RJ; ++j) x.z[j] = z_of(0, j);
 #pragma unroll
   for (int i = 0; i < OI; ++i) x.w[i] = w_of(0, i);
+#pragma unroll
+  for (int t = 0; t < UT; ++t) x.m[t] = m_of(0, t);
   int s = 0;
   for (; s + 1 < stages; s += 2) {
     stage(s, x, y);
@@ -493,17 +550,43 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
   int id[RJ];
 #pragma unroll
   for (int j = 0; j < RJ; ++j) {
-    id[j] = a.id(row0 + wr + 16 * j + n);
+    const int row = row0 + wr + 16 * j + n;
+    id[j] = !FUSED ? a.id(row) : row < rows_end ? own : kBehind;
   }
   Pieces<RP> u[RJ];
-  if (RP <= 32) {
+  if (RP <= 32 && !FUSED) {
 #pragma unroll
     for (int j = 0; j < RJ; ++j) u[j].load(a, min(row0 + wr + 16 * j + n, a.rows - 1));
   }
   __syncthreads();  // nobody reads the stages any more
-  for (int r = threadIdx.x; r < TR; r += 64 * WAVES) tile_ids[r] = a.id(row0 + r);
+  if (FUSED) {
+    u16* pieces = (u16*)&z_tile[0][0];  // [TR][kPieces][RP]
+#pragma unroll
+    for (int t = 0; t < UT; ++t)
+#pragma unroll
+      for (int j = 0; j < UJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int k = 16 * t + 4 * g + v;
+          float f = k < a.rank ? form[t][j][v] * a.scale : 0.f;
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            const u16 piece = to_bf16(f);
+            f -= from_bf16(piece);
+            if (!(fabsf(f) < INFINITY)) f = 0.f;
+            if (k < RP) pieces[((wr + 16 * (first_j + j) + n) * kPieces + i) * RP + k] = piece;
+          }
+        }
+  } else {
+    for (int r = threadIdx.x; r < TR; r += 64 * WAVES) tile_ids[r] = a.id(row0 + r);
+  }
   __syncthreads();
+  if (FUSED) {
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) u[j].load((const u16*)&z_tile[0][0], wr + 16 * j + n);
+  }
   auto run_end = [&](int r) {  // where the run that begins at r ends
+    if (FUSED) return TR;
     const int who = tile_ids[r];
     for (int q = r; q < TR; q += 64) {
       const uint64_t other = __ballot(q + lane < TR && tile_ids[min(q + lane, TR - 1)] != who);
@@ -520,7 +603,7 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
       mine[q] = a.rank == RP ? load_eight(b) : load_eight(b, a.rank - k);
     }
   };
-  int r = 0, who = tile_ids[0], stop = run_end(0);
+  int r = 0, who = FUSED ? own : tile_ids[0], stop = run_end(0);
   if (who >= 0) take_factors(who);
   while (r < TR) {
     if (who >= 0) {
@@ -538,7 +621,7 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
       for (int j = 0; j < RJ; ++j) {
         const int first = wr + 16 * j;
         if (r >= first + 16 || stop <= first) continue;
-        if (RP > 32) u[j].load(a, min(row0 + first + n, a.rows - 1));
+        if (RP > 32 && !FUSED) u[j].load(a, min(row0 + first + n, a.rows - 1));
         const bool in = first + n >= r && first + n < stop;
 #pragma unroll
         for (int i = 0; i < OI; ++i) {
@@ -845,7 +928,7 @@ hipError_t launch_down(const Down& a, hipStream_t st) {
 template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT> hipError_t launch_up_tiles(const Up& a, hipStream_t st) {
   const int row_tiles = (a.rows + TR - 1) / TR, out_tiles = (a.outs + TO - 1) / TO;
   const dim3 grid((unsigned)row_tiles * out_tiles), block(64 * WO * WR);
-  hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, DIRECT>), grid, block, 0, st, a, row_tiles, out_tiles);
+  hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, DIRECT, false>), grid, block, 0, st, a, row_tiles, out_tiles);
   return hipGetLastError();
 }
 
@@ -873,6 +956,23 @@ template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
     if (!direct) return launch_up_tiles<RP, Y, 128, 128, 2, 2, false>(a, st);
     if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, true>(a, st);
     return launch_up_tiles<RP, Y, 128, 128, 2, 2, true>(a, st);
+  });
+}
+
+// Few outputs go in one launch, where its workgroups, one or more per segment, are all on the card at once or their tiles are half full at
+// least: 32768 rows, 1024 x 128, rank 8, two launches and one: 128 segments 45 and 32 us, 2048 segments 56 and 106; 4096 rows of 256
+// segments 34 and 25; one segment of 512 rows, 4096 x 128, rank 16, 71 and 59.
+bool fused_pays(const Up& a) {
+  const int64_t segments = a.seg.count;
+  return a.outs <= 128 && a.rank <= 32 && a.rows > kFewRows && (a.rows / 128 + segments <= 512 || a.rows >= 64 * segments) && a.ld_z % 8 == 0 &&
+         (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0 && (uintptr_t)a.m % 16 == 0;
+}
+template <class Y> hipError_t launch_fused(const Up& a, hipStream_t st) {
+  return by_rank(a.rank, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value <= 32 ? decltype(rp)::value : 32;
+    hipLaunchKernelGGL((rfast_lora_up<RP, Y, 128, 128, 2, 2, true, true>), dim3((unsigned)Segments::blocks(a.rows, a.seg.count, 128)), dim3(kThreads), 0,
+                       st, a, 0, 0);
+    return hipGetLastError();
   });
 }
 
@@ -939,9 +1039,15 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   const Layout l = layout_of(*s, 0);
   char* ws = (char*)workspace;
   const Segments seg = {row_ptr, adapter, s->segments, s->adapters, s->rows};
-  hipError_t e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale, 0, {}}, st);
+  const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank,
+                s->adapters, (const u16*)A, seg, s->scale};
+  hipError_t e = hipSuccess;
+  if (fused_pays(u)) {
+    e = s->y_type == RFAST_F32 ? launch_fused<float>(u, st) : launch_fused<u16>(u, st);
+    return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "projection launch");
+  }
+  e = launch_down({(const u16*)x, (const u16*)A, (u16*)(ws + l.u_rows), nullptr, (int32_t*)(ws + l.ids), seg, s->ld_x, 0, s->d, s->rank, s->scale, 0, {}}, st);
   if (e != hipSuccess) return rfast_refuse_hip(e, "adapter launch");
-  const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank, s->adapters};
   e = s->y_type == RFAST_F32 ? launch_up<float>(u, st) : launch_up<u16>(u, st);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "projection launch");
 }
@@ -971,7 +1077,7 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
     e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f, 0, t}, st);
     if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale, 0, {}}, st);
     if (e == hipSuccess && dx)
-      e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters}, st);
+      e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters, nullptr, {}, 1.f}, st);
   }
   if (e == hipSuccess)
     e = launch_sums({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f},

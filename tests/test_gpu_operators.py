@@ -115,6 +115,33 @@ def test_lora_forward(name, dtype):
     assert (y[c.used:].float() == torch.tensor(12345.0).to(dtype).float().item()).all(), "rows behind the last segment"
 
 
+ONE_TILE = {
+    "one_step": dict(lengths=[100, 3, 40], ids=[1, 0, 1], adapters=2, d=24, K=128, r=8),
+    "two_steps": dict(lengths=[65], ids=None, adapters=1, d=64, K=1, r=1),
+    "three_steps": dict(lengths=[70], ids=None, adapters=1, d=96, K=16, r=32),
+    "over_four": dict(lengths=[130, 0, 128], ids=None, adapters=3, d=136, K=127, r=20),
+    "blocks": dict(lengths=[128, 129, 1, 0, 256, 300], ids=[2, -1, 9, 0, 1, 2], adapters=3, d=1032, K=128, r=32, spare=130),
+    "rank_9": dict(lengths=[600, 500], ids=[0, 0], adapters=2, d=520, K=33, r=9),
+    "behind_all": dict(lengths=[0, 0], ids=None, adapters=2, d=64, K=64, r=8, spare=200),
+    "many_short": dict(lengths=[1, 5] * 300, ids=None, adapters=600, d=40, K=24, r=2),
+    "not_aligned": dict(lengths=[200, 90], ids=None, adapters=2, d=68, K=100, r=5),
+}
+
+
+@pytest.mark.parametrize("name", ONE_TILE)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_lora_forward_few_outputs(name, dtype):
+    c = Lora(**ONE_TILE[name])
+    x, w, a, b, ptr, ids = c.dev()
+    out = torch.full((c.T, w.shape[0]), 12345.0, dtype=dtype, device=DEV)
+    y = rf.rfast_lora_forward(x, w, a, b, ptr, ids, scale=c.scale, out=out)
+    want, err = c.exact()["y"]
+    last = (BF if dtype == BF16 else STEP) * want.abs()
+    if c.used:
+        within(y[:c.used], want[:c.used], (err * (1 + BF) + last)[:c.used], "y")
+    assert (y[c.used:].float() == torch.tensor(12345.0).to(dtype).float().item()).all(), "rows behind the last segment"
+
+
 @pytest.mark.parametrize("name", CASES)
 @pytest.mark.parametrize("need_dx", [False, True])
 def test_lora_backward(name, need_dx):
