@@ -264,12 +264,15 @@ struct Up {
   const u16* m;  // [adapters][rank][cols]
   Segments seg;
   float scale;
+  float* partials;  // [splits][rows][pitch_of(outs)], where the contraction is split over workgroups
   // (where row numbers are out of order a row's may never have been written)
   __device__ int id(int row) const {
     const int i = row < rows ? ids[row] : kBehind;
     return i < adapters ? i : kNone;
   }
 };
+
+int64_t __host__ __device__ pitch_of(int outs) { return ((int64_t)outs + 3) / 4 * 4; }
 
 // Where chunk c of row o of a matrix of CH chunks a row is put in LDS: at c ^ swizzle.
 template <int CH> __device__ inline int swizzle(int o) { return CH == 4 ? o >> 1 & 3 : CH == 8 ? o & 7 : CH == 2 ? o >> 2 & 1 : 0; }
@@ -348,7 +351,7 @@ template <class Y> __device__ inline void store_outs(const Up& a, int row, int i
 // at a time, kStages of them in turn.  A row of a stage is four chunks of 16 bytes; chunk c is put at place c ^ row / 2 % 4, so that the
 // 16 rows of an operand fall on all banks.
 // What bounds it is how far ahead the stages are sent for: with two buffers of 64 indices (the next one under way while one is
-// multiplied) the matrix cores were busy for 38 % of the time, XX.  So stage s + 4 is sent for when the operands of stage s are in
+// multiplied) the matrix cores were busy for 38 % of the time.  So stage s + 4 is sent for when the operands of stage s are in
 // registers, and the operands of stage s + 1 are read from LDS while those of stage s are multiplied; one barrier per stage says both that stage s + 1
 // has arrived and that nobody reads stage s any more.  A contraction that is no multiple of kStep begins with what is over.
 // DIRECT: rows begin at multiples of 16 bytes, and stages go from memory to LDS without passing through registers (a wavefront's load
@@ -356,11 +359,15 @@ template <class Y> __device__ inline void store_outs(const Up& a, int row, int i
 // registers, one stage ahead.
 // FUSED: few outputs (one tile of them), so that the pass of `down` over the rows would cost as much as this one.  A workgroup has rows of one
 // segment only, the first factors of its adapter are some more rows of w, and what they come to is handed on through LDS: 32768 rows of 128 nodes, 1024 x
-// 128, rank 8: 21 + 22 us in two passes, XX so.
+// 128, rank 8: 21 + 22 us in two passes, 32 so.
+// SPLIT: few tiles, so that their stages one after the other would be all there is to wait for: workgroups (in y) share the contraction and
+// write what they have; rfast_lora_join adds it up, and the adapters' part.
 constexpr int kStep = 32, kStages = 4;
+enum Mode { kWhole, kFused, kSplit };
 
-template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT, bool FUSED>
+template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT, Mode MODE>
 __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tiles, int out_tiles) {
+  constexpr bool FUSED = MODE == kFused;
   constexpr int WAVES = WO * WR, OI = TO / WO / 16, RJ = TR / WR / 16;
   constexpr int UT = FUSED ? tiles_of(RP) : 0, UJ = RJ / WO;                    // blocks of ranks; blocks of rows whose u a wavefront forms
   constexpr int WL = TO / 16 / WAVES, ZL = TR / 16 / WAVES, L = WL + ZL + UT;  // loads per lane and stage, of 16 bytes (of u: 4)
@@ -418,8 +425,10 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
       mo[q] = (uint32_t)min(16 * q + k, a.rank - 1) * (uint32_t)a.cols * 2 + chunk * 16 + (lane & 3) * 4;
     }
   }
-  const int over = a.cols % kStep, stages = a.cols / kStep + (over ? 1 : 0);
-  auto begin = [&](int s) { return over ? (s == 0 ? a.cols - over : (s - 1) * kStep) : s * kStep; };
+  const int all_stages = (a.cols + kStep - 1) / kStep, splits = MODE == kSplit ? gridDim.y : 1, split = MODE == kSplit ? blockIdx.y : 0;
+  const int first = all_stages * split / splits, stages = all_stages * (split + 1) / splits - first;  // stage s here is first + s of all
+  const int all_over = a.cols % kStep, over = first == 0 ? all_over : 0;                              // (the first of all takes what is over)
+  auto begin = [&](int s) { return all_over ? (first + s == 0 ? a.cols - all_over : (first + s - 1) * kStep) : (first + s) * kStep; };
   auto fetch = [&](int s) {
     const int64_t c = (int64_t)begin(s) * 2;
 #pragma unroll
@@ -538,6 +547,16 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
     stage(s + 1, y, x);
   }
   if (s < stages) stage(s, x, y);
+  if constexpr (MODE == kSplit) {
+#pragma unroll
+    for (int i = 0; i < OI; ++i)
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) {
+        const int row = row0 + wr + 16 * j + n, out = out0 + wo + 16 * i + 4 * g;
+        if (row < a.rows && out < a.outs) *reinterpret_cast<f32x4*>(a.partials + ((int64_t)split * a.rows + row) * pitch_of(a.outs) + out) = acc[i][j];
+      }
+    return;
+  }
 
   // The adapters' part, one run of rows with the same adapter after the other: its factors for the tile's outputs come through LDS (those of
   // the next run are under way meanwhile), and every wavefront that has rows of the run takes them up.  A column of a product is one
@@ -646,9 +665,24 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
     for (int j = 0; j < RJ; ++j) store_outs<Y>(a, row0 + wr + 16 * j + n, id[j], out0 + wo + 16 * i + 4 * g, acc[i][j]);
 }
 
+// y = the sum of the partial products + the adapters' part.  A wavefront has 16 rows and 16 outputs.
+template <int RP, class Y> __global__ void __launch_bounds__(kThreads) rfast_lora_join(Up a, int splits) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int out0 = (blockIdx.x * kWaves + wave) * 16, row = blockIdx.y * 16 + n;
+  if (out0 >= a.outs) return;
+  const int id = a.id(row), out = min(out0 + 4 * g, (int)pitch_of(a.outs) - 4);
+  Pieces<RP> u;
+  u.load(a, min(row, a.rows - 1));
+  const float* p = a.partials + min(row, a.rows - 1) * pitch_of(a.outs) + out;
+  f32x4 acc = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int q = 0; q < splits; ++q) acc += *reinterpret_cast<const f32x4*>(p + q * a.rows * pitch_of(a.outs));
+  acc = add_adapters<RP, 1>(a, u, id, out0, 0, acc);
+  store_outs<Y>(a, row, id, out0 + 4 * g, acc);
+}
+
 // Up to 64 rows: bound by one read of W, which goes from memory to the registers of one wavefront and no further.  A workgroup has 16 OT
 // outputs, its WAVES wavefronts share the contraction.
-constexpr int kFewRows = 64;
 template <int RP, class Y, int OT, int RT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
   constexpr int Q = 4, CHUNK = 32 * Q;
@@ -863,8 +897,31 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_sums(Sums a, Sums b, in
 // ------------------------------------------------------------------------------------------------------------- host
 int padded_rank(int rank) { return rank <= 8 ? 8 : rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
+// Workgroups that share the contraction of one tile of 128 x 128, where there are fewer tiles than compute units: a stage of 32 takes a
+// lone workgroup 0.45 us.  4096 x 4096, rank 16, whole and split: 128 rows 73 and 31 us, 512 rows 72 and 48; 8192 x 512, 1024 rows 130 and
+// 44; 1024 x 1024, 300 rows 29 and 19.
+constexpr int kFewRows = 64;
+int splits_of(int64_t rows, int64_t outs, int64_t cols) {
+  if (rows <= kFewRows) return 1;
+  const int64_t tiles = (rows + 127) / 128 * ((outs + 127) / 128), stages = (cols + kStep - 1) / kStep;
+  return (int)std::max<int64_t>(1, std::min({256 / tiles, stages / 8, (int64_t)16}));
+}
+// Where rows over a multiple of 256 would have the card do one more round of tiles that are mostly empty, they are a launch of their own:
+// 4100 rows, 4096 x 4096, 202 us in 17 x 16 tiles, 125 + 9 so.
+int whole_rows(int64_t rows, int64_t outs) {
+  const int64_t columns = (outs + 255) / 256, units = 256, whole = rows / 256 * 256;
+  return (int)(whole > 0 && (whole / 256 * columns + units - 1) / units < ((rows + 255) / 256 * columns + units - 1) / units ? whole : rows);
+}
+size_t partials_bytes(int64_t rows, int64_t outs, int64_t cols) {
+  const int64_t whole = whole_rows(rows, outs);
+  size_t most = 0;
+  for (const int64_t part : {whole, rows - whole})
+    if (const int splits = splits_of(part, outs, cols); splits > 1) most = std::max(most, (size_t)(splits * part * pitch_of((int)outs) * 4));
+  return most;
+}
+
 struct Layout {
-  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, wt, total;
+  size_t ids, u_rows, u_cols, e_rows, e_cols, bt, at, wt, partials, total;
   int64_t pitch;
 };
 Layout layout_of(const rfast_lora_shape& s, int pass) {
@@ -881,6 +938,7 @@ Layout layout_of(const rfast_lora_shape& s, int pass) {
   l.e_rows = take(pass == 2 ? T * wide * 2 : 0);
   l.at = take(pass == 2 ? n * d * r * 2 : 0);
   l.wt = take(pass == 2 ? d * K * 2 : 0);
+  l.partials = take(pass == 0 ? partials_bytes(s.rows, s.K, s.d) : pass == 2 ? partials_bytes(s.rows, s.d, s.K) : 0);
   l.total = off;
   return l;
 }
@@ -928,7 +986,18 @@ hipError_t launch_down(const Down& a, hipStream_t st) {
 template <int RP, class Y, int TO, int TR, int WO, int WR, bool DIRECT> hipError_t launch_up_tiles(const Up& a, hipStream_t st) {
   const int row_tiles = (a.rows + TR - 1) / TR, out_tiles = (a.outs + TO - 1) / TO;
   const dim3 grid((unsigned)row_tiles * out_tiles), block(64 * WO * WR);
-  hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, DIRECT, false>), grid, block, 0, st, a, row_tiles, out_tiles);
+  hipLaunchKernelGGL((rfast_lora_up<RP, Y, TO, TR, WO, WR, DIRECT, kWhole>), grid, block, 0, st, a, row_tiles, out_tiles);
+  return hipGetLastError();
+}
+template <int RP, class Y> hipError_t launch_up_split(const Up& a, int splits, bool direct, hipStream_t st) {
+  const int row_tiles = (a.rows + 127) / 128, out_tiles = (a.outs + 127) / 128;
+  const dim3 grid((unsigned)row_tiles * out_tiles, splits);
+  if (direct) hipLaunchKernelGGL((rfast_lora_up<8, float, 128, 128, 2, 2, true, kSplit>), grid, dim3(kThreads), 0, st, a, row_tiles, out_tiles);
+  else hipLaunchKernelGGL((rfast_lora_up<8, float, 128, 128, 2, 2, false, kSplit>), grid, dim3(kThreads), 0, st, a, row_tiles, out_tiles);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((rfast_lora_join<RP, Y>), dim3((unsigned)((a.outs + 16 * kWaves - 1) / (16 * kWaves)), (unsigned)((a.rows + 15) / 16)), dim3(kThreads), 0, st,
+                     a, splits);
   return hipGetLastError();
 }
 
@@ -953,6 +1022,8 @@ template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
     }
     const int64_t large = ((int64_t)a.rows + 255) / 256 * ((a.outs + 255) / 256);
     const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0;
+    const int splits = splits_of(a.rows, a.outs, a.cols);
+    if (splits > 1) return launch_up_split<RP, Y>(a, splits, direct, st);
     if (!direct) return launch_up_tiles<RP, Y, 128, 128, 2, 2, false>(a, st);
     if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, true>(a, st);
     return launch_up_tiles<RP, Y, 128, 128, 2, 2, true>(a, st);
@@ -961,16 +1032,18 @@ template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
 
 // Few outputs go in one launch, where its workgroups, one or more per segment, are all on the card at once or their tiles are half full at
 // least: 32768 rows, 1024 x 128, rank 8, two launches and one: 128 segments 45 and 32 us, 2048 segments 56 and 106; 4096 rows of 256
-// segments 34 and 25; one segment of 512 rows, 4096 x 128, rank 16, 71 and 59.
+// segments 34 and 25.  Long rows of few tiles are better split: one segment of 512 rows, 4096 x 128, rank 16, 26 us, and 59 in one launch; 8192
+// rows 53 and 60; but 16384 rows, 2048 x 128, 48 and 36; 1000 rows, 784 x 10, 18.5 and 17.
 bool fused_pays(const Up& a) {
   const int64_t segments = a.seg.count;
   return a.outs <= 128 && a.rank <= 32 && a.rows > kFewRows && (a.rows / 128 + segments <= 512 || a.rows >= 64 * segments) && a.ld_z % 8 == 0 &&
-         (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0 && (uintptr_t)a.m % 16 == 0;
+         (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (a.cols <= 1024 || splits_of(a.rows, a.outs, a.cols) < 4) && (uintptr_t)a.w % 16 == 0 &&
+         (uintptr_t)a.m % 16 == 0;
 }
 template <class Y> hipError_t launch_fused(const Up& a, hipStream_t st) {
   return by_rank(a.rank, [&](auto rp) {
     constexpr int RP = decltype(rp)::value <= 32 ? decltype(rp)::value : 32;
-    hipLaunchKernelGGL((rfast_lora_up<RP, Y, 128, 128, 2, 2, true, true>), dim3((unsigned)Segments::blocks(a.rows, a.seg.count, 128)), dim3(kThreads), 0,
+    hipLaunchKernelGGL((rfast_lora_up<RP, Y, 128, 128, 2, 2, true, kFused>), dim3((unsigned)Segments::blocks(a.rows, a.seg.count, 128)), dim3(kThreads), 0,
                        st, a, 0, 0);
     return hipGetLastError();
   });
@@ -978,11 +1051,8 @@ template <class Y> hipError_t launch_fused(const Up& a, hipStream_t st) {
 
 template <class Y> hipError_t launch_up(const Up& all, hipStream_t st) {
   Up a = all;
-  // Where rows over a multiple of 256 would have the card do one more round of tiles that are mostly empty, they are a launch of their own:
-  // 4100 rows, 4096 x 4096, 202 us in 17 x 16 tiles, XX so.
-  const int64_t columns = (a.outs + 255) / 256, units = 256;
-  const int whole = a.rows / 256 * 256;
-  if (whole > 0 && whole < a.rows && (whole / 256 * columns + units - 1) / units < (((int64_t)whole / 256 + 1) * columns + units - 1) / units) {
+  const int whole = whole_rows(a.rows, a.outs);
+  if (whole < a.rows) {
     a.rows = whole;
     Up rest = all;
     rest.rows -= whole;
@@ -1040,7 +1110,7 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   char* ws = (char*)workspace;
   const Segments seg = {row_ptr, adapter, s->segments, s->adapters, s->rows};
   const Up u = {(const u16*)x, (const u16*)W, (const u16*)B, (const u16*)(ws + l.u_rows), (const int32_t*)(ws + l.ids), y, s->ld_x, s->ld_y, s->rows, s->d, s->K, s->rank,
-                s->adapters, (const u16*)A, seg, s->scale};
+                s->adapters, (const u16*)A, seg, s->scale, (float*)(ws + l.partials)};
   hipError_t e = hipSuccess;
   if (fused_pays(u)) {
     e = s->y_type == RFAST_F32 ? launch_fused<float>(u, st) : launch_fused<u16>(u, st);
@@ -1077,7 +1147,7 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
     e = launch_down({(const u16*)x, (const u16*)A, nullptr, u_cols, nullptr, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f, 0, t}, st);
     if (e == hipSuccess) e = launch_down({(const u16*)dy, bt, e_rows, e_cols, ids, seg, s->ld_y, l.pitch, s->K, s->rank, s->scale, 0, {}}, st);
     if (e == hipSuccess && dx)
-      e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters, nullptr, {}, 1.f}, st);
+      e = launch_up<u16>({(const u16*)dy, (const u16*)(ws + l.wt), (const u16*)(ws + l.at), e_rows, ids, dx, s->ld_y, s->ld_x, s->rows, s->K, s->d, s->rank, s->adapters, nullptr, {}, 1.f, (float*)(ws + l.partials)}, st);
   }
   if (e == hipSuccess)
     e = launch_sums({(const u16*)x, e_cols, dA, seg, s->ld_x, l.pitch, s->d, s->rank, 1.f},

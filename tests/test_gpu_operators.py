@@ -142,6 +142,35 @@ def test_lora_forward_few_outputs(name, dtype):
     assert (y[c.used:].float() == torch.tensor(12345.0).to(dtype).float().item()).all(), "rows behind the last segment"
 
 
+LONG = {  # few outputs or rows and long sums, forward and backward
+    "long_sums": dict(lengths=[40, 0, 30], ids=[1, 1, -1], adapters=2, d=4100, K=10, r=8),
+    "long_sums_odd": dict(lengths=[1, 65, 70], ids=None, adapters=3, d=1031, K=70, r=40, spare=9),
+    "wide_back": dict(lengths=[3] * 30, ids=[i % 7 for i in range(30)], adapters=7, d=100, K=2050, r=33),
+    "wide_back_odd": dict(lengths=[99, 1, 100], ids=[2, 0, 2], adapters=3, d=67, K=1027, r=16),
+    "rows_over": dict(lengths=[2000, 118], ids=None, adapters=2, d=512, K=8192, r=4),
+}
+
+
+@pytest.mark.parametrize("name", LONG)
+def test_lora_long_sums(name):
+    c = Lora(**LONG[name])
+    x, w, a, b, ptr, ids = c.dev()
+    want = c.exact()
+    for dtype in (F32, BF16):
+        out = torch.full((c.T, w.shape[0]), 12345.0, dtype=dtype, device=DEV)
+        y = rf.rfast_lora_forward(x, w, a, b, ptr, ids, scale=c.scale, out=out)
+        v, err = want["y"]
+        within(y[:c.used], v[:c.used], (err * (1 + BF) + (BF if dtype == BF16 else STEP) * v.abs())[:c.used], "y")
+        assert (y[c.used:].float() == torch.tensor(12345.0).to(dtype).float().item()).all(), "rows behind the last segment"
+    dx0 = torch.full_like(x, 77.0)
+    dx, da, db = rf.rfast_lora_backward(x, w, a, b, ptr, ids, c.dy.to(DEV), scale=c.scale, dx=dx0)
+    within(da, *want["da"], "da")
+    within(db, *want["db"], "db")
+    v, err = want["dx"]
+    within(dx[:c.used], v[:c.used], (err * (1 + BF) + BF * v.abs())[:c.used], "dx")
+    assert (dx[c.used:] == 77.0).all(), "rows behind the last segment"
+
+
 @pytest.mark.parametrize("name", CASES)
 @pytest.mark.parametrize("need_dx", [False, True])
 def test_lora_backward(name, need_dx):
