@@ -35,16 +35,34 @@ __device__ inline u32x4 load_eight(const u16* p) {
   const any_u32x4 t = *reinterpret_cast<const any_u32x4*>(p);
   return u32x4{t.x, t.y, t.z, t.w};
 }
-// ... of which `left` exist (any number); zeros for the others.  For the ends of rows: a condition per load has it waited for before the next
-// is sent, so wherever all of them exist the loads go out without one.
-__device__ inline u32x4 load_eight(const u16* p, int64_t left) {
-  if (left >= 8) return load_eight(p);
+// ... of which `left` exist (any number); zeros for the others.  For rows of fewer than eight: a condition per load has it waited for before the
+// next is sent, so everywhere else the loads go out without one.
+__device__ inline u32x4 load_few(const u16* p, int64_t left) {
   u32x4 t = {0, 0, 0, 0};
 #pragma unroll
-  for (int j = 0; j < 7; ++j)
+  for (int j = 0; j < 8; ++j)
     if (j < left) t[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
   return t;
 }
+// v without its first n elements (n >= 0), zeros behind the others
+__device__ inline u32x4 drop_first(u32x4 v, int n) {
+  const uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+  const int b = 16 * n;
+  const uint64_t l = b < 64 ? lo >> b | (b > 0 ? hi << (64 - b) : 0) : b < 128 ? hi >> (b - 64) : 0, h = b < 64 ? hi >> b : 0;
+  return u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+// the first n elements of v (any n), zeros behind them
+__device__ inline u32x4 keep_first(u32x4 v, int n) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = 2 * i + 1 < n ? v[i] : 2 * i < n ? v[i] & 0xFFFF : 0;
+  return v;
+}
+// Eight neighbours from p on in a row of at least eight, of which `left` are in the row: its last eight, moved to their places.
+__device__ inline u32x4 load_eight(const u16* p, int64_t left) {
+  const int there = (int)min(left, (int64_t)8);
+  return drop_first(load_eight(left < 8 ? p + left - 8 : p), 8 - max(there, 0));
+}
+__device__ inline u32x4 load_eight(const u16* p, int64_t left, bool wide) { return wide ? load_eight(p, left) : load_few(p, left); }
 
 // Takes chunks first, first + step, .. below end through load(chunk, operands) and use(operands), the loads of one chunk under way while
 // the one before is used.  (Left to itself the compiler reuses a load's registers as soon as it can, and has a third of a chunk under way.)
@@ -124,7 +142,7 @@ __device__ inline void turn_over(const Transposes& a, int64_t tile) {
     for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load_eight(from + (int64_t)i * q.cols, r + i < q.rows ? q.cols - c : 0);
+    for (int i = 0; i < 8; ++i) v[i] = load_few(from + (int64_t)i * q.cols, r + i < q.rows ? q.cols - c : 0);
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -218,7 +236,8 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_down(Down a) {
     }
     if (whole < a.cols && wave == whole / CHUNK % WAVES) {
       Operands o;
-      fetch(whole, o, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+      if (a.cols >= 8) fetch(whole, o, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+      else fetch(whole, o, [&](const u16* p, int at) { return load_few(p + at, a.cols - at - g * 8); });
       use(o);
     }
   }
@@ -301,7 +320,7 @@ template <int RP> struct Factor {  // b of adapter `who` for 16 outputs from out
     for (int q = 0; q < STEPS; ++q) {
       const int k = 32 * q + 8 * (lane >> 4);
       if (a.rank == RP) f[q] = k < WIDE ? load_eight(b + k % RP) : u32x4{0, 0, 0, 0};
-      else f[q] = load_eight(b + k % RP, k < WIDE ? a.rank - k % RP : 0);
+      else f[q] = load_eight(b + k % RP, k < WIDE ? a.rank - k % RP : 0, a.rank >= 8);
     }
   }
 };
@@ -450,12 +469,12 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
       for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]));
     } else {
 #pragma unroll
-      for (int q = 0; q < ZL; ++q) zr[q] = load_eight((const u16*)(z0 + c + zo[q]), over - lc);
+      for (int q = 0; q < ZL; ++q) zr[q] = load_eight((const u16*)(z0 + c + zo[q]), over - lc, a.cols >= 8);
 #pragma unroll
-      for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]), over - lc);
+      for (int q = 0; q < WL; ++q) wg[q] = load_eight((const u16*)(w0 + c + wofs[q]), over - lc, a.cols >= 8);
 #pragma unroll
       for (int q = 0; q < UT; ++q)  // (every wavefront fetches and puts all sixteen ranks of a block here)
-        mg[q] = load_eight((const u16*)(m0 + c) + (int64_t)min(16 * q + lr, a.rank - 1) * a.cols + lc, over - lc);
+        mg[q] = load_eight((const u16*)(m0 + c) + (int64_t)min(16 * q + lr, a.rank - 1) * a.cols + lc, over - lc, a.cols >= 8);
     }
   };
   auto put = [&](int s) {
@@ -619,7 +638,7 @@ __global__ void __launch_bounds__(64 * WO * WR) rfast_lora_up(Up a, int row_tile
     for (int q = 0; q < MINE; ++q) {
       const int c = q * 64 * WAVES + threadIdx.x, out = min(out0 + c / CH, a.outs - 1), k = c % CH * 8;
       const u16* b = a.b + ((int64_t)who * a.outs + out) * a.rank + k;
-      mine[q] = a.rank == RP ? load_eight(b) : load_eight(b, a.rank - k);
+      mine[q] = a.rank == RP ? load_eight(b) : load_eight(b, a.rank - k, a.rank >= 8);
     }
   };
   int r = 0, who = FUSED ? own : tile_ids[0], stop = run_end(0);
@@ -724,7 +743,8 @@ __global__ void __launch_bounds__(64 * WAVES) rfast_lora_up_few(Up a) {
   pipelined<Operands>(wave * CHUNK, whole, WAVES * CHUNK, [&](int c, Operands& f) { fetch(c, f, [&](const u16* p, int at) { return load_eight(p + at); }); }, use);
   if (whole < a.cols && wave == whole / CHUNK % WAVES) {
     Operands f;
-    fetch(whole, f, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+    if (a.cols >= 8) fetch(whole, f, [&](const u16* p, int at) { return load_eight(p + at, a.cols - at - g * 8); });
+    else fetch(whole, f, [&](const u16* p, int at) { return load_few(p + at, a.cols - at - g * 8); });
     use(f);
   }
   // (the adapters of a tile are dealt to the wavefronts)
@@ -786,19 +806,20 @@ __device__ inline void sums_of(const Sums& a, int tile, f32x4 (*part)[8][tiles_o
   };
   auto fetch = [&](int t0, int end, Operands& o, auto whole) {  // 32 rows from t0 on; whole: all of them exist, and rows have eight columns
     constexpr bool WHOLE = decltype(whole)::value;
-    const int r = t0 + 8 * g;
+    const int r = t0 + 8 * g, from = WHOLE ? r : min((int64_t)r, a.pitch - 8);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const u16* p = a.z + (int64_t)(r + i) * a.ld + c;
-      o.z[i] = WHOLE ? load_eight(p) : load_eight(p, r + i < end ? min(a.cols - c, 8) : 0);
+      const u16* p = a.z + (int64_t)(WHOLE ? r + i : min(r + i, end - 1)) * a.ld + c;
+      o.z[i] = wide ? load_eight(p) : load_few(p, a.cols - c);
+      if (!WHOLE && r + i >= end) o.z[i] = u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < kFrags<RP>; ++i) {
         const int k = (RP == 8 ? 16 * i : RP * i + 16 * t) + n;
-        const u16* p = a.s + (int64_t)min(k, kPieces * RP - 1) * a.pitch + r;
-        o.s[t][i] = WHOLE ? load_eight(p) : load_eight(p, end - r);
+        o.s[t][i] = load_eight(a.s + (int64_t)min(k, kPieces * RP - 1) * a.pitch + from);
+        if (!WHOLE) o.s[t][i] = keep_first(drop_first(o.s[t][i], r - from), end - r);
       }
   };
   auto use = [&](const Operands& o) {
@@ -817,8 +838,11 @@ __device__ inline void sums_of(const Sums& a, int tile, f32x4 (*part)[8][tiles_o
         }
     }
   };
+  bool shared = false;  // more than the first wavefront have a part
   auto segment = [&](int s) {
-    const int begin = a.seg.begin(s), end = a.seg.begin(s + 1), whole = wide && end > begin ? begin + (end - begin) / 32 * 32 : begin;
+    const int begin = a.seg.begin(s), end = a.seg.begin(s + 1);
+    shared |= end - begin > 32;
+    const int whole = wide && end > begin ? begin + (end - begin) / 32 * 32 : begin;
     pipelined<Operands>(begin + wave * 32, whole, WAVES * 32, [&](int t0, Operands& o) { fetch(t0, end, o, std::true_type()); }, use);
     for (int t0 = whole; t0 < end; t0 += 32)
       if (wave == (t0 - begin) / 32 % WAVES) {
@@ -836,8 +860,9 @@ __device__ inline void sums_of(const Sums& a, int tile, f32x4 (*part)[8][tiles_o
     }
   }
   // the wavefronts' sums, two and two
+  if (!shared && wave != 0) return;
 #pragma unroll
-  for (int half = WAVES / 2; half >= 1; half >>= 1) {
+  for (int half = WAVES / 2; half >= 1 && shared; half >>= 1) {
     __syncthreads();
     if (wave >= half && wave < 2 * half)
 #pragma unroll
@@ -902,8 +927,8 @@ int padded_rank(int rank) { return rank <= 8 ? 8 : rank <= 16 ? 16 : rank <= 32 
 // 44; 1024 x 1024, 300 rows 29 and 19.
 constexpr int kFewRows = 64;
 int splits_of(int64_t rows, int64_t outs, int64_t cols) {
-  if (rows <= kFewRows) return 1;
   const int64_t tiles = (rows + 127) / 128 * ((outs + 127) / 128), stages = (cols + kStep - 1) / kStep;
+  if (rows <= kFewRows || tiles > 128) return 0;
   return (int)std::max<int64_t>(1, std::min({256 / tiles, stages / 8, (int64_t)16}));
 }
 // Where rows over a multiple of 256 would have the card do one more round of tiles that are mostly empty, they are a launch of their own:
@@ -916,7 +941,7 @@ size_t partials_bytes(int64_t rows, int64_t outs, int64_t cols) {
   const int64_t whole = whole_rows(rows, outs);
   size_t most = 0;
   for (const int64_t part : {whole, rows - whole})
-    if (const int splits = splits_of(part, outs, cols); splits > 1) most = std::max(most, (size_t)(splits * part * pitch_of((int)outs) * 4));
+    if (const int splits = splits_of(part, outs, cols); splits > 0) most = std::max(most, (size_t)(splits * part * pitch_of((int)outs) * 4));
   return most;
 }
 
@@ -1023,7 +1048,7 @@ template <class Y> hipError_t launch_up_rows(const Up& a, hipStream_t st) {
     const int64_t large = ((int64_t)a.rows + 255) / 256 * ((a.outs + 255) / 256);
     const bool direct = a.ld_z % 8 == 0 && (uintptr_t)a.z % 16 == 0 && a.cols % 8 == 0 && (uintptr_t)a.w % 16 == 0;
     const int splits = splits_of(a.rows, a.outs, a.cols);
-    if (splits > 1) return launch_up_split<RP, Y>(a, splits, direct, st);
+    if (splits > 0) return launch_up_split<RP, Y>(a, splits, direct, st);
     if (!direct) return launch_up_tiles<RP, Y, 128, 128, 2, 2, false>(a, st);
     if (large >= 192) return launch_up_tiles<RP, Y, 256, 256, 2, 4, true>(a, st);
     return launch_up_tiles<RP, Y, 128, 128, 2, 2, true>(a, st);
