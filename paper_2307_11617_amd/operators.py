@@ -146,6 +146,7 @@ def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, o
     [0, adapters): no adapter).  Returns y [T][K] in out_dtype (default bfloat16); rows behind the last segment are not
     written: they stay as they are in `out`, and hold anything without one."""
     torch = _t()
+    _need(x.dim() == 2 and w.dim() == 2, "need matrices x [rows][d] and w [K][d]")
     T, K = x.shape[0], w.shape[0]
     if out is None:
         out, ld_y = torch.empty((T, K), dtype=out_dtype or torch.bfloat16, device=x.device), max(K, 1)
@@ -161,6 +162,7 @@ def rfast_lora_backward(x, w, a, b, row_ptr, adapter, dy, scale=1.0, need_dx=Tru
     """(dx, da, db) of rfast_lora_forward for dy bfloat16 [T][K], w frozen: dx bfloat16 [T][d] (None unless need_dx or a tensor to write to
     is given; rows behind the last segment are not written), da float32 [adapters][rank][d], db float32 [adapters][K][rank]."""
     torch = _t()
+    _need(x.dim() == 2 and w.dim() == 2, "need matrices x [rows][d] and w [K][d]")
     T, d = x.shape
     ld_y = _matrix(dy, "dy", T, w.shape[0], torch.bfloat16, x.device)
     with_dx = need_dx or dx is not None
@@ -266,12 +268,15 @@ class RFastAdamW:
         nbytes = rfast_adamw_workspace_bytes(tensors)
         _need(nbytes > 0, "sizes out of range")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self._made_on = torch.cuda.current_stream(self.device)
         self.handle = rfast_adamw_create(tensors, RfastAdamwOptions(pt, gt, state_bits, betas[0], betas[1], eps), self.workspace)
 
     def step(self, gamma, active=None):
         """One step with step size gamma; active: uint8 [tensors] on the device, zero for tensors that stay as they are."""
         if active is not None:
             _vector(active, "active", len(self.params), _torch.uint8, self.device)
+        if _stream_of(self.device.index) != self._made_on.cuda_stream:  # the allocator has to know, or it hands the workspace on too early
+            self.workspace.record_stream(_torch.cuda.current_stream(self.device))
         rfast_adamw_step(self.handle, gamma, active, self.device)
 
     def steps(self):

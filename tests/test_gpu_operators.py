@@ -763,3 +763,102 @@ def test_refusals_on_the_gpu():
     with pytest.raises(RFastError):
         RFastAdamW([p], [g]).step(float("inf"))
     RFastAdamW([p, torch.zeros(100, device=DEV)], [g, g]).step(1e-3)  # gradients may be shared
+
+
+def test_lora_refuses_memory_that_is_written_and_read():
+    """In place is refused; other columns of the same rows are not in place."""
+    c = Lora([40, 60], None, 2, 64, 64, 8, seed=2)
+    x, w, a, b, ptr, _ = c.dev()
+    dy = c.dy.to(DEV)
+    with pytest.raises(RFastError, match="overlaps"):
+        rf.rfast_lora_forward(x, w, a, b, ptr, None, out=x)
+    for dx in (x, dy):
+        with pytest.raises(RFastError, match="overlaps"):
+            rf.rfast_lora_backward(x, w, a, b, ptr, None, dy, dx=dx)
+    both = torch.zeros((2, 2, 64, 8), dtype=F32, device=DEV)
+    with pytest.raises(RFastError, match="overlaps"):
+        rf.rfast_lora_backward(x, w, a, b, ptr, None, dy, da=both[0].view(2, 8, 64), db=both[0])
+    wide = torch.zeros((c.T, 200), dtype=BF16, device=DEV)
+    wide[:, 64:128] = x
+    for at in (0, 128, 136):
+        y = rf.rfast_lora_forward(wide[:, 64:128], w, a, b, ptr, None, scale=c.scale, out=wide[:, at:at + 64])
+        assert torch.equal(y, rf.rfast_lora_forward(x, w, a, b, ptr, None, scale=c.scale)) and torch.equal(wide[:, 64:128], x)
+    for at in (1, 63, 65, 127):
+        with pytest.raises(RFastError, match="overlaps"):
+            rf.rfast_lora_forward(wide[:, 64:128], w, a, b, ptr, None, out=wide[:, at:at + 64])
+    for bad in (x[0], x[None]):
+        with pytest.raises(RFastError):
+            rf.rfast_lora_forward(bad, w, a, b, ptr)
+        with pytest.raises(RFastError):
+            rf.rfast_lora_backward(bad, w, a, b, ptr, None, dy)
+
+
+def test_lora_two_streams_and_graphs_at_once():
+    """Calls on two streams, and two graphs on two streams, share nothing: every result is the one of a call alone."""
+    many = [Lora([300, 84], None, 2, 1024, 96, 16, seed=21), Lora([90, 30], [1, 0], 2, 512, 264, 40, seed=22)]
+    args = []
+    for c in many:
+        x, w, a, b, ptr, ids = c.dev()
+        args.append((x, w, a, b, ptr, ids, c.dy.to(DEV), c.scale))
+
+    def both(x, w, a, b, ptr, ids, dy, scale):
+        return (rf.rfast_lora_forward(x, w, a, b, ptr, ids, scale=scale), *rf.rfast_lora_backward(x, w, a, b, ptr, ids, dy, scale=scale))
+
+    alone = [both(*q) for q in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(10):
+        for k in (0, 1):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(both(*args[k]))
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for k in (0, 1):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(both(*args[k]))
+        graphs.append(g)
+    for turn in range(5):
+        for o in outs:
+            for t in o:
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            with torch.cuda.stream(streams[k]):
+                graphs[k].replay()
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            got[k].append(tuple(t.clone() for t in outs[k]))
+        args[0][0].mul_(1.0)  # the program's own work between replays
+        torch.cuda.synchronize()
+    for k in (0, 1):
+        for one in got[k]:
+            for p, q in zip(one, alone[k]):
+                assert torch.equal(p, q)
+
+
+def test_adamw_steps_on_another_stream_outlive_the_object():
+    """The workspace is not handed on while a step on another stream still reads it."""
+    g = gen(31)
+    params = [normal(g, 70001, dtype=F32).to(DEV) for _ in range(6)]
+    grads = [normal(g, 70001, dtype=F32).to(DEV) for _ in range(6)]
+    want = [p.clone() for p in params]
+    plain = RFastAdamW(want, grads)
+    for _ in range(20):
+        plain.step(1e-2)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    opt = RFastAdamW(params, grads)
+    m, v = opt.m, opt.v  # (theirs to keep)
+    torch.cuda.synchronize()
+    nbytes = opt.workspace.numel()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            opt.step(1e-2)
+    del opt
+    taken = [torch.full((nbytes,), 255, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    for p, q in zip(params, want):
+        assert torch.equal(p, q)
+    assert len(taken) == 4 and len(m) == len(v) == 6
