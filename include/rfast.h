@@ -457,7 +457,7 @@ typedef struct rfast_lora_shape {
   int32_t y_type;            /* forward: rfast_type of y; backward: RFAST_BF16 (dy) */
   float scale;
 } rfast_lora_shape;
-/* Device workspace in bytes (pure function; 0 if a size is out of range).  pass 0: rfast_lora_forward, 1: rfast_lora_backward
+/* Device workspace in bytes (pure function; 0 if a size is out of range; never less for more rows).  pass 0: rfast_lora_forward, 1: rfast_lora_backward
  * without dx, 2: with dx. */
 size_t rfast_lora_workspace_bytes(const rfast_lora_shape* shape, int32_t pass);
 /* y: y_type [rows][ld_y >= K].  Products of bf16 are summed in 32 bits, and A_a x_t, which the second product reads, keeps its

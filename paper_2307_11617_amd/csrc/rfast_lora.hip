@@ -937,12 +937,12 @@ int whole_rows(int64_t rows, int64_t outs) {
   const int64_t columns = (outs + 255) / 256, units = 256, whole = rows / 256 * 256;
   return (int)(whole > 0 && (whole / 256 * columns + units - 1) / units < ((rows + 255) / 256 * columns + units - 1) / units ? whole : rows);
 }
+// What the partial products of `rows` rows, or of any fewer, take at most: a workspace for many rows does for few.  (Tiles of rows times splits
+// are at most 256 / tiles of outputs, as splits_of divides them.)
 size_t partials_bytes(int64_t rows, int64_t outs, int64_t cols) {
-  const int64_t whole = whole_rows(rows, outs);
-  size_t most = 0;
-  for (const int64_t part : {whole, rows - whole})
-    if (const int splits = splits_of(part, outs, cols); splits > 0) most = std::max(most, (size_t)(splits * part * pitch_of((int)outs) * 4));
-  return most;
+  const int64_t columns = (outs + 127) / 128, most = std::max<int64_t>(1, std::min<int64_t>(16, (cols + kStep - 1) / kStep / 8));
+  if (rows <= kFewRows || columns > 128) return 0;
+  return (size_t)(128 * std::min(256 / columns, (rows + 127) / 128 * most) * pitch_of((int)outs) * 4);
 }
 
 struct Layout {
@@ -1147,7 +1147,7 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   if (rc != RFAST_OK || s->rows == 0) return rc;
   {
     const int64_t n = s->adapters, r = s->rank, d = s->d, K = s->K, wide = s->y_type == RFAST_F32 ? 4 : 2;
-    const Area out = {y, s->rows, s->ld_y * wide, K * wide}, work = flat(workspace, workspace_bytes);
+    const Area out = {y, s->rows, s->ld_y * wide, K * wide}, work = flat(workspace, (int64_t)layout_of(*s, 0).total);
     const Area read[] = {{x, s->rows, s->ld_x * 2, d * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
                          flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
     for (const Area& in : read)
@@ -1180,7 +1180,7 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
   if (!dA || !dB) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   {
     const int64_t T = s->rows, n = s->adapters, r = s->rank, d = s->d, K = s->K;
-    const Area written[] = {{dx, T, s->ld_x * 2, d * 2}, flat(dA, n * r * d * 4), flat(dB, n * r * K * 4), flat(workspace, workspace_bytes)};
+    const Area written[] = {{dx, T, s->ld_x * 2, d * 2}, flat(dA, n * r * d * 4), flat(dB, n * r * K * 4), flat(workspace, (int64_t)layout_of(*s, pass).total)};
     const Area read[] = {{x, T, s->ld_x * 2, d * 2}, {dy, T, s->ld_y * 2, K * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
                          flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
     for (int i = 0; i < 4; ++i) {

@@ -333,3 +333,13 @@ def test_adamw_refusals():
             rfast_set_adamw(gpu.ctx, 0.9, 0.9, 1e-8, 0.0, 32, s)
     gpu.init(None, None)  # nothing of the refused calls stays
     gpu.sync_run(1, 0.1)
+
+
+def test_loss_whose_last_rows_are_fewer():
+    """The loss goes over the pools as many rows at a time as a round has, and the last rows of all need no larger workspace."""
+    w, x0 = adapters(n=2, d=1024, K=128, rank=8, samples=9320, batch=8320)
+    orc, gpu = make_oracle(w, x0=x0), harness.make_gpu(w)
+    gpu.init(x0, w.sched.initial_batch())
+    want = orc.diagnostics()["loss_at_xbar"]
+    assert abs(gpu.diagnostics()["loss_at_xbar"] - want) <= 1e-2 * abs(want)
+    gpu.check()

@@ -25,6 +25,16 @@ def test_lora_workspace_is_pure_and_checks_ranges():
     assert rf.rfast_lora_workspace_bytes(shape(), 3) == 0 and rf.rfast_lora_workspace_bytes(shape(), -1) == 0
 
 
+def test_lora_workspace_for_many_rows_does_for_few():
+    for d, K, rank in ((1024, 128, 8), (4096, 4096, 16), (512, 33000, 64), (100, 70, 1), (8192, 8, 3)):
+        for k in (0, 1, 2):
+            last = 0
+            for rows in (1, 64, 65, 128, 129, 300, 512, 1000, 2048, 4100, 8001, 16384, 16385, 40000):
+                now = rf.rfast_lora_workspace_bytes(shape(rows=rows, d=d, K=K, rank=rank, ld_x=d, ld_y=K), k)
+                assert now >= last > -1, (d, K, rows, k)
+                last = now
+
+
 def forward(s, x=DEV, w=DEV, a=DEV, b=DEV, ptr=DEV, ad=None, y=DEV, ws=DEV, nbytes=1 << 40):
     code = rf.lib().rfast_lora_forward(C.byref(s) if s is not None else None, x, w, a, b, ptr, ad, y, ws, nbytes, None)
     return code, rf.rfast_last_error(None)
