@@ -57,7 +57,8 @@ __device__ inline u32x4 keep_first(u32x4 v, int n) {
   for (int i = 0; i < 4; ++i) v[i] = 2 * i + 1 < n ? v[i] : 2 * i < n ? v[i] & 0xFFFF : 0;
   return v;
 }
-// Eight neighbours from p on in a row of at least eight, of which `left` are in the row: its last eight, moved to their places.
+// Eight neighbours from p on in a row of at least eight that ends at p + left, before p or behind it: the row's last eight are read and moved
+// to their places, so p + left has to be the row's end whatever is wanted of it.
 __device__ inline u32x4 load_eight(const u16* p, int64_t left) {
   const int there = (int)min(left, (int64_t)8);
   return drop_first(load_eight(left < 8 ? p + left - 8 : p), 8 - max(there, 0));
@@ -318,9 +319,9 @@ template <int RP> struct Factor {  // b of adapter `who` for 16 outputs from out
     const u16* b = a.b + ((int64_t)who * a.outs + out) * a.rank;
 #pragma unroll
     for (int q = 0; q < STEPS; ++q) {
-      const int k = 32 * q + 8 * (lane >> 4);
-      if (a.rank == RP) f[q] = k < WIDE ? load_eight(b + k % RP) : u32x4{0, 0, 0, 0};
-      else f[q] = load_eight(b + k % RP, k < WIDE ? a.rank - k % RP : 0, a.rank >= 8);
+      const int k = 32 * q + 8 * (lane >> 4), at = k % RP;  // (where k is past the pieces, what it would repeat is read and dropped)
+      f[q] = a.rank == RP ? load_eight(b + at) : load_eight(b + at, a.rank - at, a.rank >= 8);
+      if (k >= WIDE) f[q] = u32x4{0, 0, 0, 0};
     }
   }
 };

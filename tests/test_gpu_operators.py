@@ -862,3 +862,15 @@ def test_adamw_steps_on_another_stream_outlive_the_object():
     for p, q in zip(params, want):
         assert torch.equal(p, q)
     assert len(taken) == 4 and len(m) == len(v) == 6
+
+
+@pytest.mark.parametrize("rank", range(9, 16))
+@pytest.mark.parametrize("rows", [9, 200])
+def test_lora_ranks_between(rank, rows):
+    """Ranks whose factors end inside an operand, by the ways of few rows and of a joined sum: what is read of them stays in their tensor
+    (here at the beginning of memory of its own)."""
+    c = Lora([rows - 4, 4], None, 2, 136, 264, rank, seed=rank)
+    x, w, a, b, ptr, _ = c.dev()
+    want, err = c.exact()["y"]
+    y = rf.rfast_lora_forward(x, w, a, b, ptr, None, scale=c.scale, out_dtype=F32)
+    within(y, want, err * (1 + BF) + STEP * want.abs(), "y")
