@@ -480,7 +480,8 @@ int rfast_lora_backward(const rfast_lora_shape* shape, const void* x, const void
  * state_bits 32: m and v are fp32.  state_bits 8: m and sqrt(v) are held as 8-bit floats (e4m3) with an fp32 scale for every 256
  * coordinates counted from the tensor's first, largest magnitude / 448; the step itself uses the unrounded ones.  The root, whose
  * range is half that of v, is never rounded to zero: one that is not zero is held as the smallest code at least, so that no coordinate with a
- * momentum meets a vanished denominator.  A moment that is not finite is held as NaN and counts for no scale. */
+ * momentum meets a vanished denominator.  A moment that is not finite is held as NaN and counts for no scale.  256 coordinates
+ * whose largest magnitude is below 448 * 2^-126 (5.3e-36) are held as zeros with a scale of zero. */
 typedef struct rfast_adamw rfast_adamw;
 typedef struct rfast_adamw_tensor {
   void* param;             /* device, param_type [count], updated                                              */

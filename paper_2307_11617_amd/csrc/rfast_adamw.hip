@@ -24,6 +24,7 @@ constexpr int kGroups = 64;                    // words for workgroups that are 
 constexpr int kMostWorkgroups = 1 << 23;       // a launch has fewer than 2^32 lanes
 constexpr float kCodeMost = 448.f;             // largest finite e4m3
 constexpr float kCodeLeast = 0.001953125f;     // smallest e4m3 above zero, 2^-9
+constexpr float kTopLeast = 0x1.cp-118f;       // 448 * 2^-126: below it a block's scale is no normal number
 constexpr size_t kAlign = 256;
 size_t up(size_t b) { return (b + kAlign - 1) / kAlign * kAlign; }
 
@@ -68,6 +69,12 @@ __device__ inline float finite_magnitude(float v) {
   const float a = fabsf(v);
   return a < INFINITY ? a : 0.f;  // false for NaN too
 }
+
+// What a block whose largest magnitude is `top` is multiplied by to become codes.  Below kTopLeast the scale would lose its digits and its inverse
+// be infinite (zeros times it NaN), as without a gradient a momentum gets there: by 0.9 a step from 1e-3 in some 700.  Such a block
+// is held as zeros with a scale of zero; a root, whose square was a number of 32 bits, is 2^-75 and more or zero.
+__device__ inline float inverse_of(float top) { return top >= kTopLeast ? 1.f / top * kCodeMost : 0.f; }
+__device__ inline float scale_of(float top) { return top >= kTopLeast ? top * (1.f / kCodeMost) : 0.f; }
 
 // Four values as e4m3 times scale; values that are not finite become NaN.
 __device__ inline uint32_t codes_of(const float* v, float inverse, bool root) {
@@ -164,11 +171,11 @@ template <int BITS, bool STREAM> struct Moments {
       top_m = wave_max(top_m);
       top_v = wave_max(top_v);
       if (left <= 0) return;
-      store_codes<STREAM>((uint8_t*)pm + k, left, codes_of(m, top_m > 0.f ? 1.f / top_m * kCodeMost : 0.f, false));
-      store_codes<STREAM>((uint8_t*)pv + k, left, codes_of(root, top_v > 0.f ? 1.f / top_v * kCodeMost : 0.f, true));
+      store_codes<STREAM>((uint8_t*)pm + k, left, codes_of(m, inverse_of(top_m), false));
+      store_codes<STREAM>((uint8_t*)pv + k, left, codes_of(root, inverse_of(top_v), true));
       if (k % kBlock == 0) {
-        ms[k / kBlock] = top_m * (1.f / kCodeMost);
-        vs[k / kBlock] = top_v * (1.f / kCodeMost);
+        ms[k / kBlock] = scale_of(top_m);
+        vs[k / kBlock] = scale_of(top_v);
       }
     }
   }

@@ -1,0 +1,92 @@
+"""The operators on tensors where their range ends: moments that fade, memory that is handed on, extents of 32 bits.
+
+Tolerances as in test_gpu_operators.py: bounds from the roundings on the way."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import harness  # noqa: E402
+from paper_2307_11617_amd import RFastAdamW  # noqa: E402
+from test_gpu_adapters import quad  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F8 = torch.float32, torch.float8_e4m3fn
+LEAST = 448 * 2.0 ** -126  # a block whose largest magnitude is below this is held as zeros
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def test_adamw_eight_bits_after_the_last_gradient():
+    """Gradients that end, as an adapter's without rows: its moments fade to nothing over a thousand steps, and no parameter is lost."""
+    p = torch.randn(700, generator=gen(1)).to(DEV)
+    g = torch.zeros(700, device=DEV)
+    g[::3] = torch.randn(234, generator=gen(2)).to(DEV) * 1e-3
+    start, touched = p.clone(), g != 0
+    o = RFastAdamW([p], [g], state_bits=8)
+    for _ in range(3):
+        o.step(1e-3)
+    g.zero_()
+    for _ in range(500):
+        o.step(1e-3)
+    after = p.clone()  # from here a step is 0.9^500 of the first ones, nothing beside a parameter
+    for _ in range(500):
+        o.step(1e-3)
+    assert torch.isfinite(p).all() and torch.equal(p, after)
+    assert torch.equal(p[~touched], start[~touched]) and (p[touched] != start[touched]).all()
+    m, v = o.m[0].view(F8).float(), o.v[0].view(F8).float()
+    assert torch.isfinite(v).all() and (v[touched] > 0).all()
+    assert (m == 0).all() and (o.m_scale[0] == 0).all() and (o.steps() == 1003).all()
+
+
+@pytest.mark.parametrize("top", [1e-44, 1e-40, 1e-38, 1.2e-36, 5e-36, 5.9e-36, 1e-34, 1e-30])
+def test_adamw_eight_bits_tiny_moments(top):
+    """A block of moments of every size around what a scale can hold, without a gradient: one step makes 0.9 of them, or zeros."""
+    p = torch.randn(256, generator=gen(3)).to(DEV)
+    start = p.clone()
+    codes = torch.linspace(-448, 448, 257)[:256].to(F8)
+    codes[100:140] = 0
+    scale = torch.tensor([top / 448], dtype=F32)
+    m, s = codes.to(DEV), scale.to(DEV)
+    m0 = (codes.float() * scale).double()
+    o = RFastAdamW([p], [torch.zeros(256, device=DEV)], m=[m], v=[torch.zeros(256, dtype=F8, device=DEV)], m_scale=[s],
+                   v_scale=[torch.zeros(1, device=DEV)], state_bits=8, steps=100)
+    o.step(1e-3)
+    assert torch.equal(p, start)  # at most 1e-3 * 1e-30 / 1e-8
+    want = 0.9 * m0
+    got = (m.float().cpu() * s.cpu()).double()
+    assert torch.isfinite(m.float()).all()
+    if 0.9 * top < LEAST:
+        assert (got == 0).all() and s.item() == 0
+    else:
+        assert abs(s.item() - 0.9 * top / 448) <= 2.0 ** -21 * top / 448
+        # half a step of a code, of the smallest codes half their distance 2^-9; the roundings of 0.9, the products and the scale
+        bound = (2.0 ** -4 + 2.0 ** -20) * want.abs() + 2.0 ** -10 * s.item() * (1 + 2.0 ** -20) + 2.0 ** -148
+        assert ((got - want).abs() <= bound).all()
+
+
+def test_adamw_rounds_eight_bits_tiny_moments():
+    """The same of the rounds' variant: nodes whose moments have faded go on as if they had none."""
+    w = quad(5, 300, 31)
+    gpu = harness.make_gpu(w)
+    gpu.set_adamw(state_bits=8)
+    gpu.init(np.random.default_rng(4).standard_normal((w.n, w.p)).astype(np.float32), None)
+    codes = np.arange(w.n * w.p, dtype=np.int64).reshape(w.n, w.p) % 120  # finite codes, zero among them
+    gpu.write("ADAMW_M", codes.astype(np.uint8))
+    gpu.write("ADAMW_M_SCALE", np.full((w.n, 2), 2e-39, np.float32))
+    gpu.write("Z", np.zeros((w.n, w.p), np.float32))
+    x = gpu.read("X")
+    everyone = torch.ones((1, w.n), dtype=torch.uint8, device=DEV)
+    st, dev = harness.upload_chunk(gpu, w, 0, 1)
+    gpu.run(1, everyone, dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, None)
+    gpu.check()
+    assert (gpu.read("ADAMW_M") == 0).all() and (gpu.read("ADAMW_M_SCALE") == 0).all()
+    st, dev = harness.upload_chunk(gpu, w, 1, 20)
+    gpu.run(19, dev["active"], dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, None)
+    gpu.check()
+    assert np.isfinite(gpu.read("X")).all() and (gpu.read("X") != x).any()
+    assert ((gpu.read("ADAMW_M") & 0x7F) != 0x7F).all() and ((gpu.read("ADAMW_V") & 0x7F) != 0x7F).all()
