@@ -230,8 +230,13 @@ class RFastAdamW:
         self.device = params[0].device
         _need(params[0].is_cuda, "params: need tensors on the GPU")
 
+        made = []  # memory of this object's own
+
         def listed(value, name, make):
-            value = [make(p) for p in params] if value is None else list(value)
+            if value is None:
+                value = [make(p) for p in params]
+                made.extend(value)
+            value = list(value)
             _need(len(value) == n, f"{name}: need one per parameter")
             return value
 
@@ -268,15 +273,19 @@ class RFastAdamW:
         nbytes = rfast_adamw_workspace_bytes(tensors)
         _need(nbytes > 0, "sizes out of range")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self._made_on = torch.cuda.current_stream(self.device)
+        self._made = made + [self.workspace]
+        self._streams = {torch.cuda.current_stream(self.device).cuda_stream}  # those that the allocator knows to use that memory
         self.handle = rfast_adamw_create(tensors, RfastAdamwOptions(pt, gt, state_bits, betas[0], betas[1], eps), self.workspace)
 
     def step(self, gamma, active=None):
         """One step with step size gamma; active: uint8 [tensors] on the device, zero for tensors that stay as they are."""
         if active is not None:
             _vector(active, "active", len(self.params), _torch.uint8, self.device)
-        if _stream_of(self.device.index) != self._made_on.cuda_stream:  # the allocator has to know, or it hands the workspace on too early
-            self.workspace.record_stream(_torch.cuda.current_stream(self.device))
+        if _stream_of(self.device.index) not in self._streams:  # the allocator has to know, or it hands the memory on too early
+            stream = _torch.cuda.current_stream(self.device)
+            for t in self._made:
+                t.record_stream(stream)
+            self._streams.add(stream.cuda_stream)
         rfast_adamw_step(self.handle, gamma, active, self.device)
 
     def steps(self):

@@ -90,3 +90,34 @@ def test_adamw_rounds_eight_bits_tiny_moments():
     gpu.check()
     assert np.isfinite(gpu.read("X")).all() and (gpu.read("X") != x).any()
     assert ((gpu.read("ADAMW_M") & 0x7F) != 0x7F).all() and ((gpu.read("ADAMW_V") & 0x7F) != 0x7F).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_memory_of_its_own_outlives_the_object(bits):
+    """Moments, scales and workspace that the object made are not handed on while steps on other streams still use them."""
+    g = gen(5)
+    first = [torch.randn(700001, generator=g).to(DEV) for _ in range(6)]
+    grads = [torch.randn(700001, generator=g).to(DEV) for _ in range(6)]
+    want = [p.clone() for p in first]
+    plain = RFastAdamW(want, grads, state_bits=bits)
+    for _ in range(40):
+        plain.step(1e-2)
+    torch.cuda.synchronize()
+    for streams in (1, 2):
+        params = [p.clone() for p in first]
+        opt = RFastAdamW(params, grads, state_bits=bits)
+        sizes = [t.numel() * t.element_size() for t in [*opt.m, *opt.v, *(s for s in opt.m_scale + opt.v_scale if s is not None), opt.workspace]]
+        torch.cuda.synchronize()
+        sides = [torch.cuda.Stream() for _ in range(streams)]
+        for k in range(streams):
+            sides[k].wait_stream(sides[k - 1])
+            with torch.cuda.stream(sides[k]):
+                for _ in range(40 // streams):
+                    opt.step(1e-2)
+        del opt
+        taken = [torch.full((b,), 255, dtype=torch.uint8, device=DEV) for b in sizes for _ in (0, 1)]
+        torch.cuda.synchronize()
+        for t in taken:
+            assert (t == 255).all()
+        for p, q in zip(params, want):
+            assert torch.equal(p, q)
