@@ -357,7 +357,8 @@ int rfast_set_optimizer(rfast_ctx* ctx, float momentum, float weight_decay, floa
  *        v_i = x_i - gamma (mhat_i / (sqrt(qhat_i) + eps) + weight_decay x_i)
  * with the tracked direction z_i in the place of the gradient, mhat = m / (1 - beta1^t), qhat = q / (1 - beta2^t) and t = t_i + 1, the
  * number of the node's activation; only an activated node touches its moments.  The same holds for rfast_sync_round.  The weight
- * decay is decoupled: it is part of no gradient and of no loss.  The moments are held as rfast_adamw_create describes (state_bits 32 or 8, the
+ * decay is decoupled: it is part of no gradient and of no loss.  beta1, beta2 and eps have the range of rfast_adamw_options; the moments
+ * are held as rfast_adamw_create describes (state_bits 32 or 8, the
  * scales counted from each node's first coordinate).  d_state: device memory of rfast_adamw_state_bytes(n, p, state_bits), 256-byte aligned,
  * owned by the caller, must outlive the context.  Rounds take the kernels per round (rfast_use_blocks has no effect), with one
  * launch more for the moments.  rfast_init must follow before the next round. */
@@ -497,7 +498,7 @@ typedef struct rfast_adamw_tensor {
 } rfast_adamw_tensor;
 typedef struct rfast_adamw_options {
   int32_t param_type, grad_type, state_bits;
-  double beta1, beta2, eps;  /* [0, 1), [0, 1), > 0; in double, as 1 - beta2 would lose digits */
+  double beta1, beta2, eps;  /* [0, 1), [0, 1), [2^-126, 1e30); in double, as 1 - beta2 would lose digits */
 } rfast_adamw_options;
 /* Device workspace in bytes for these counts (0 if one is out of range).  tensors: HOST array; of it only `count` is read. */
 size_t rfast_adamw_workspace_bytes(int32_t tensors, const rfast_adamw_tensor* host_tensors);

@@ -56,8 +56,8 @@ struct Args {
 __device__ inline double one_less_power(double log_beta, int t) { return -expm1((double)t * log_beta); }
 
 // a / b to about one unit in the last place: the step is not carried on like the moments, whose bits decide codes, and a division that
-// is rounded correctly takes twice the instructions.  (b is at least eps and no denormal for any eps that has a use; where its reciprocal is
-// not finite or zero, so is the quotient to fp32.)
+// is rounded correctly takes twice the instructions.  (b is at least eps, which is no denormal, so its reciprocal is finite; where b is infinite or
+// the quotient is, the correction is no number and is left out.)
 __device__ inline float over(float a, float b) {
   const float r = __builtin_amdgcn_rcpf(b);
   const float q = a * r;
@@ -366,7 +366,7 @@ int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, cons
     return rfast_refuse(RFAST_EINVAL, "param_type and grad_type must be RFAST_F32 or RFAST_BF16");
   if (o->state_bits != 8 && o->state_bits != 32) return rfast_refuse(RFAST_EINVAL, "state_bits must be 8 or 32");
   if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1)) return rfast_refuse(RFAST_ERANGE, "beta1 and beta2 must lie in [0, 1)");
-  if (!(o->eps > 0 && o->eps < 1e30)) return rfast_refuse(RFAST_ERANGE, "eps must be positive and finite");
+  if (!rfast_adamw_eps_ok(o->eps)) return rfast_refuse(RFAST_ERANGE, "eps must lie in [2^-126, 1e30)");
   if (!aligned(d_workspace, kAlign)) return rfast_refuse(RFAST_EINVAL, "workspace must be 256-byte aligned");
   int64_t chunks;
   const int64_t slices = slices_for(tensors, t, o->state_bits, &chunks);

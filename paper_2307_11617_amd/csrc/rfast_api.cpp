@@ -1474,7 +1474,7 @@ int rfast_set_adamw(rfast_ctx* c, double beta1, double beta2, double eps, double
   if (!c) return RFAST_EINVAL;
   if (state_bits != 8 && state_bits != 32) return fail(c, RFAST_EINVAL, "state_bits must be 8 or 32");
   if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return fail(c, RFAST_ERANGE, "beta1 and beta2 must lie in [0, 1)");
-  if (!(eps > 0 && eps < 1e30)) return fail(c, RFAST_ERANGE, "eps must be positive and finite");
+  if (!rfast_adamw_eps_ok(eps)) return fail(c, RFAST_ERANGE, "eps must lie in [2^-126, 1e30)");
   if (!(weight_decay >= 0 && weight_decay < 1e30)) return fail(c, RFAST_ERANGE, "weight_decay must be finite and >= 0");
   if (!d_state || (uintptr_t)d_state % kAlign != 0) return fail(c, RFAST_EINVAL, "the states need memory at a multiple of 256 bytes");
   if (state_bytes < rfast_adamw_state_bytes(c->d.n, c->d.p, state_bits)) return fail(c, RFAST_ENOMEM, "memory for the states too small");

@@ -9,6 +9,8 @@
 
 int rfast_refuse(int code, const std::string& msg);  // text for rfast_last_error(NULL)
 int rfast_refuse_hip(hipError_t e, const char* what);
+// AdamW divides by sqrt(v) + eps in 32 bits: a denormal has no finite reciprocal, and 0 / eps would be no number
+inline bool rfast_adamw_eps_ok(double eps) { return eps >= 0x1p-126 && eps < 1e30; }
 
 typedef unsigned short u16;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

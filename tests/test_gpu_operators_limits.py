@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import harness  # noqa: E402
-from paper_2307_11617_amd import RFastAdamW  # noqa: E402
+from paper_2307_11617_amd import RFastAdamW, RFastError  # noqa: E402
 from test_gpu_adapters import quad  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -121,3 +121,29 @@ def test_adamw_memory_of_its_own_outlives_the_object(bits):
             assert (t == 255).all()
         for p, q in zip(params, want):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_smallest_eps(bits):
+    """The smallest eps that is taken leaves what never had a gradient alone; smaller ones are refused, by the rounds' variant too."""
+    p = torch.ones(300, device=DEV)
+    g = torch.zeros(300, device=DEV)
+    g[::2] = 1e-3
+    o = RFastAdamW([p], [g], state_bits=bits, eps=2.0 ** -126)
+    for _ in range(3):
+        o.step(1e-2)
+    assert torch.equal(p[1::2], torch.ones(150, device=DEV)) and torch.isfinite(p).all() and (p[::2] < 1).all()
+    w = quad(3, 40, 33)
+    gpu = harness.make_gpu(w)
+    for eps in (2.0 ** -127, 1e-60):
+        with pytest.raises(RFastError, match="eps"):
+            RFastAdamW([p], [g], state_bits=bits, eps=eps)
+        with pytest.raises(RFastError, match="eps"):
+            gpu.set_adamw(eps=eps, state_bits=bits)
+    gpu.set_adamw(eps=2.0 ** -126, state_bits=bits)
+    gpu.init(None, None)
+    gpu.write("Z", np.zeros((w.n, w.p), np.float32))
+    st, dev = harness.upload_chunk(gpu, w, 0, 1)
+    gpu.run(1, torch.ones((1, w.n), dtype=torch.uint8, device=DEV), dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, None)
+    gpu.check()
+    assert np.isfinite(gpu.read("X")).all()

@@ -133,3 +133,10 @@ def test_tensors_on_the_host_are_refused(bad):
         rf.rfast_softmax_xent(x, torch.zeros(4, dtype=torch.int32))
     with pytest.raises(rf.RFastError):
         rf.RFastAdamW([torch.zeros(4)], [torch.zeros(4)])
+
+
+@pytest.mark.parametrize("eps", [2.0 ** -127, 1e-40, 1e-60, 5e-324])
+def test_adamw_refuses_an_eps_that_32_bits_do_not_hold(eps):
+    """A coordinate that never had a gradient is divided by eps alone: 0 / 0, or by the infinite reciprocal of a denormal."""
+    code, msg = create(tensors(), eps=eps)
+    assert code == -4 and "eps" in msg
