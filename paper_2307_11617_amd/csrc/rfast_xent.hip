@@ -95,7 +95,7 @@ __device__ inline void finish_row(const Args& a, int64_t row, float shift, float
 }
 
 template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane, int lanes) {
-  for (int k = lane; k < K; k += lanes) grad[k] = (OUT)0;
+  for (int64_t k = lane; k < K; k += lanes) grad[k] = (OUT)0;  // (the last step of a row of nearly 2^31 passes 32 bits)
 }
 
 // LANES lanes hold a row, GROUPS groups of logits each.  LANES <= 64: 256 / LANES rows per workgroup.

@@ -6,12 +6,12 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import harness  # noqa: E402
-from paper_2307_11617_amd import RFastAdamW, RFastError  # noqa: E402
+from paper_2307_11617_amd import RFastAdamW, RFastError, rfast_softmax_xent  # noqa: E402
 from test_gpu_adapters import quad  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
-F32, F8 = torch.float32, torch.float8_e4m3fn
+F32, BF16, F8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
 LEAST = 448 * 2.0 ** -126  # a block whose largest magnitude is below this is held as zeros
 
 
@@ -147,3 +147,26 @@ def test_adamw_smallest_eps(bits):
     gpu.run(1, torch.ones((1, w.n), dtype=torch.uint8, device=DEV), dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, None)
     gpu.check()
     assert np.isfinite(gpu.read("X")).all()
+
+
+@pytest.mark.parametrize("left", [900])
+def test_xent_longest_rows(left):
+    """Rows of nearly 2^31 classes: offsets within a row pass 32 bits.  One that counts, padding, one that is masked out entirely."""
+    K = 2 ** 31 - 1 - left
+    logits = torch.zeros((1, K), dtype=BF16, device=DEV)
+    label = torch.tensor([K - 3], dtype=torch.int32, device=DEV)
+    loss, grad = rfast_softmax_xent(logits, label, grad_scale=2.0 ** 40, grad=logits)
+    # K equal logits: sums of ones are exact in each of 1024 lanes (2^21) and off by 2^-24 of the sum at each of ten joins; log and the division
+    # by four steps; the gradient is rounded to bf16
+    assert abs(loss.item() - np.log(K)) <= 2.0 ** -19 * np.log(K)
+    p = 2.0 ** 40 / K
+    assert abs(grad[0, K - 3].item() - (p - 2.0 ** 40)) <= 2.0 ** -8 * 2.0 ** 40
+    grad[0, K - 3] = grad[0, 0]
+    assert abs(grad[0, 0].item() - p) <= 2.0 ** -7 * p and (grad == grad[0, 0]).all()
+    for lse in (None, torch.zeros(1, device=DEV)):
+        logits.fill_(1.0)
+        loss, grad = rfast_softmax_xent(logits, torch.full_like(label, -1), grad=logits, lse=lse)
+        assert loss.item() == 0 and not grad.any()
+    logits.fill_(float("-inf"))
+    loss, grad = rfast_softmax_xent(logits, label, grad=logits)
+    assert loss.item() == 0 and not grad.any()
