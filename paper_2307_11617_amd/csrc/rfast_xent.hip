@@ -264,7 +264,7 @@ template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
     return hipGetLastError();
   };
   using std::integral_constant;
-  const auto fits = [&](int lanes, int groups) { return a.K + (lanes > 64 ? N - 1 : 0) <= (int64_t)lanes * groups * N; };
+  const auto fits = [&](int lanes, int groups) { return (int64_t)a.K + (lanes > 64 ? N - 1 : 0) <= (int64_t)lanes * groups * N; };
 #define RFAST_TRY(L, G) \
   if (fits(L, G)) return go(integral_constant<int, L>(), integral_constant<int, G>())
   RFAST_TRY(8, 1);

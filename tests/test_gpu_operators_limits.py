@@ -149,7 +149,7 @@ def test_adamw_smallest_eps(bits):
     assert np.isfinite(gpu.read("X")).all()
 
 
-@pytest.mark.parametrize("left", [900])
+@pytest.mark.parametrize("left", [0, 7, 900])
 def test_xent_longest_rows(left):
     """Rows of nearly 2^31 classes: offsets within a row pass 32 bits.  One that counts, padding, one that is masked out entirely."""
     K = 2 ** 31 - 1 - left
