@@ -31,6 +31,12 @@ def _need(ok, msg):
         raise RFastError(-1, msg)
 
 
+def _sizes(*counts):
+    """Counts go to the library in 32 bits, which ctypes would cut to."""
+    if max(counts) > 0x7FFFFFFF:
+        raise RFastError(-1, f"sizes out of range: {max(counts)}")
+
+
 def _type(t, name):
     k = _types.get(t.dtype)
     if k is None:
@@ -77,6 +83,7 @@ def rfast_softmax_xent(logits, labels, grad_scale=1.0, grad_dtype=None, grad=Non
     if logits.dim() != 2 or not logits.is_cuda or logits.shape[1] < 1:
         raise RFastError(-1, "logits: need a matrix on the GPU with at least one class")
     T, K = logits.shape
+    _sizes(T, K)
     dev = logits.device
     ld, lt = _matrix(logits, "logits", T, K, None, dev), _type(logits, "logits")
     p_labels = _vector(labels, "labels", T, torch.int32, dev)
@@ -113,6 +120,7 @@ def _lora_shape(*sizes):
     if got is None:
         if len(_shapes) >= 4096:
             _shapes.clear()
+        _sizes(*sizes[:6])
         shape = RfastLoraShape(*sizes)
         got = _shapes[sizes] = (C.byref(shape), tuple(int(lib().rfast_lora_workspace_bytes(C.byref(shape), k)) for k in range(3)))
     return got

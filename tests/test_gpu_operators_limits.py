@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import harness  # noqa: E402
-from paper_2307_11617_amd import RFastAdamW, RFastError, rfast_softmax_xent  # noqa: E402
+from paper_2307_11617_amd import RFastAdamW, RFastError, rfast_lora_backward, rfast_lora_forward, rfast_softmax_xent  # noqa: E402
 from test_gpu_adapters import quad  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -170,3 +170,18 @@ def test_xent_longest_rows(left):
     logits.fill_(float("-inf"))
     loss, grad = rfast_softmax_xent(logits, label, grad=logits)
     assert loss.item() == 0 and not grad.any()
+
+
+def test_extents_that_32_bits_do_not_hold_are_refused():
+    """Sizes of 2^32 and a little more are not taken for that little."""
+    wide = torch.empty((1, 2 ** 32 + 8), dtype=BF16, device=DEV)
+    label = torch.zeros(1, dtype=torch.int32, device=DEV)
+    with pytest.raises(RFastError, match="range"):
+        rfast_softmax_xent(wide, label, grad=False)
+    x = wide.view(-1, 1)  # rows of one feature
+    w, a, b = (torch.zeros(s, dtype=BF16, device=DEV) for s in ((1, 1), (1, 2, 1), (1, 1, 2)))
+    ptr = torch.tensor([0, 8], dtype=torch.int32, device=DEV)
+    with pytest.raises(RFastError, match="range"):
+        rfast_lora_forward(x, w, a, b, ptr, out=x)
+    with pytest.raises(RFastError, match="range"):
+        rfast_lora_backward(x, w, a, b, ptr, None, x, dx=x)
