@@ -1103,20 +1103,7 @@ hipError_t launch_sums(const Sums& a, const Sums& b, hipStream_t st) {
 
 bool at_multiple(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 
-// Rows of `wide` bytes, `apart` bytes apart
-struct Area {
-  const void* p;
-  int64_t rows, apart, wide;
-};
-bool overlap(const Area& a, const Area& b) {
-  if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return false;
-  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p, a1 = a0 + (a.rows - 1) * a.apart + a.wide, b1 = b0 + (b.rows - 1) * b.apart + b.wide;
-  if (a1 <= b0 || b1 <= a0) return false;
-  if (a.apart != b.apart || a.rows < 2 || b.rows < 2) return true;
-  const int64_t behind = (int64_t)(b0 > a0 ? (b0 - a0) % a.apart : (a.apart - (a0 - b0) % a.apart) % a.apart);  // other columns of the same rows?
-  return behind < a.wide || behind + b.wide > a.apart;
-}
-Area flat(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+RfastArea flat(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
 
 int check(const rfast_lora_shape* s, int pass, const void* x, const void* W, const void* A, const void* B, const int32_t* row_ptr,
           const int32_t* adapter, const void* y, const void* workspace, size_t workspace_bytes) {
@@ -1148,12 +1135,12 @@ int rfast_lora_forward(const rfast_lora_shape* s, const void* x, const void* W, 
   if (rc != RFAST_OK || s->rows == 0) return rc;
   {
     const int64_t n = s->adapters, r = s->rank, d = s->d, K = s->K, wide = s->y_type == RFAST_F32 ? 4 : 2;
-    const Area out = {y, s->rows, s->ld_y * wide, K * wide}, work = flat(workspace, (int64_t)layout_of(*s, 0).total);
-    const Area read[] = {{x, s->rows, s->ld_x * 2, d * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
-                         flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
-    for (const Area& in : read)
-      if (overlap(out, in) || overlap(work, in)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
-    if (overlap(out, work)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
+    const RfastArea out = {y, s->rows, s->ld_y * wide, K * wide}, work = flat(workspace, (int64_t)layout_of(*s, 0).total);
+    const RfastArea read[] = {{x, s->rows, s->ld_x * 2, d * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
+                              flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
+    for (const RfastArea& in : read)
+      if (rfast_overlap(out, in) || rfast_overlap(work, in)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
+    if (rfast_overlap(out, work)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
   }
   const hipStream_t st = (hipStream_t)hip_stream;
   const Layout l = layout_of(*s, 0);
@@ -1181,14 +1168,14 @@ int rfast_lora_backward(const rfast_lora_shape* s, const void* x, const void* W,
   if (!dA || !dB) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   {
     const int64_t T = s->rows, n = s->adapters, r = s->rank, d = s->d, K = s->K;
-    const Area written[] = {{dx, T, s->ld_x * 2, d * 2}, flat(dA, n * r * d * 4), flat(dB, n * r * K * 4), flat(workspace, (int64_t)layout_of(*s, pass).total)};
-    const Area read[] = {{x, T, s->ld_x * 2, d * 2}, {dy, T, s->ld_y * 2, K * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
-                         flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
+    const RfastArea written[] = {{dx, T, s->ld_x * 2, d * 2}, flat(dA, n * r * d * 4), flat(dB, n * r * K * 4), flat(workspace, (int64_t)layout_of(*s, pass).total)};
+    const RfastArea read[] = {{x, T, s->ld_x * 2, d * 2}, {dy, T, s->ld_y * 2, K * 2}, flat(W, K * d * 2), flat(A, n * r * d * 2), flat(B, n * r * K * 2),
+                              flat(row_ptr, ((int64_t)s->segments + 1) * 4), flat(adapter, (int64_t)s->segments * 4)};
     for (int i = 0; i < 4; ++i) {
-      for (const Area& in : read)
-        if (overlap(written[i], in)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
+      for (const RfastArea& in : read)
+        if (rfast_overlap(written[i], in)) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
       for (int j = 0; j < i; ++j)
-        if (overlap(written[i], written[j])) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
+        if (rfast_overlap(written[i], written[j])) return rfast_refuse(RFAST_EINVAL, "memory that is written overlaps an argument");
     }
   }
   if (!at_multiple(dA, 4) || !at_multiple(dB, 4) || !at_multiple(dx, 2)) return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");

@@ -12,6 +12,20 @@ int rfast_refuse_hip(hipError_t e, const char* what);
 // AdamW divides by sqrt(v) + eps in 32 bits: a denormal has no finite reciprocal, and 0 / eps would be no number
 inline bool rfast_adamw_eps_ok(double eps) { return eps >= 0x1p-126 && eps < 1e30; }
 
+// Memory of a call: rows of `wide` bytes, `apart` bytes apart.  Other columns of the same rows are other memory.
+struct RfastArea {
+  const void* p;
+  int64_t rows, apart, wide;
+};
+inline bool rfast_overlap(const RfastArea& a, const RfastArea& b) {
+  if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return false;
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p, a1 = a0 + (a.rows - 1) * a.apart + a.wide, b1 = b0 + (b.rows - 1) * b.apart + b.wide;
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (a.apart != b.apart || a.rows < 2 || b.rows < 2) return true;
+  const int64_t behind = (int64_t)(b0 > a0 ? (b0 - a0) % a.apart : (a.apart - (a0 - b0) % a.apart) % a.apart);  // other columns of the same rows?
+  return behind < a.wide || behind + b.wide > a.apart;
+}
+
 typedef unsigned short u16;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

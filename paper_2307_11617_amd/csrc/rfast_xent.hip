@@ -306,9 +306,8 @@ extern "C" int rfast_softmax_xent(int32_t rows, int32_t K, const void* logits, i
       (uintptr_t)d_rows % 4)
     return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");
   if (grad) {
-    const uintptr_t l0 = (uintptr_t)logits, l1 = l0 + ((size_t)(rows - 1) * ld_logits + K) * lw;
-    const uintptr_t g0 = (uintptr_t)grad, g1 = g0 + ((size_t)(rows - 1) * ld_grad + K) * gw;
-    if (g0 < l1 && l0 < g1 && !(g0 == l0 && lw == gw && ld_logits == ld_grad))
+    const RfastArea in = {logits, rows, ld_logits * lw, (int64_t)K * lw}, out = {grad, rows, ld_grad * gw, (int64_t)K * gw};
+    if (rfast_overlap(in, out) && !(grad == logits && lw == gw && ld_logits == ld_grad))
       return rfast_refuse(RFAST_EINVAL, "the gradient overlaps the logits without being in their place");
   }
   const Args a = {logits, labels, loss, lse, grad, d_rows, ld_logits, ld_grad, rows, K, grad_scale};

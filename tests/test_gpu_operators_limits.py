@@ -185,3 +185,24 @@ def test_extents_that_32_bits_do_not_hold_are_refused():
         rfast_lora_forward(x, w, a, b, ptr, out=x)
     with pytest.raises(RFastError, match="range"):
         rfast_lora_backward(x, w, a, b, ptr, None, x, dx=x)
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("K", [7, 300, 5000])
+def test_xent_gradient_in_other_columns_of_the_logits_rows(types, K):
+    """A buffer whose rows hold logits and gradient side by side is no overlap; columns that both have are one."""
+    T, (lt, gt) = 9, types
+    narrow = 4 // gt.itemsize if lt == F32 else 1  # gradient elements per logit's width
+    logits = torch.randn((T, K), generator=gen(8)).to(lt).to(DEV)
+    label = torch.arange(T, dtype=torch.int32, device=DEV) % K
+    both = torch.full((T, 3 * K + 4), 7.0, dtype=lt, device=DEV)
+    for at in (0, 2 * K, 2 * K + 1):
+        both.fill_(7.0)
+        both[:, K:2 * K] = logits
+        want_loss, want = rfast_softmax_xent(both[:, K:2 * K], label, grad_dtype=gt)  # (the order of a sum goes by the rows' addresses)
+        grad = both.view(gt)[:, at * narrow:at * narrow + K]
+        loss, got = rfast_softmax_xent(both[:, K:2 * K], label, grad=grad)
+        assert torch.equal(got, want) and torch.equal(loss, want_loss) and torch.equal(both[:, K:2 * K], logits)
+    for at in (2 * K - 1, K + 1):
+        with pytest.raises(RFastError, match="overlaps"):
+            rfast_softmax_xent(both[:, K:2 * K], label, grad=both.view(gt)[:, at * narrow:at * narrow + K])
