@@ -494,7 +494,7 @@ typedef struct rfast_adamw_tensor {
   void* copy;              /* device, bf16 [count] that receives the new parameters rounded, or NULL            */
   int64_t count;           /* 0 and more                                                                       */
   double weight_decay;
-  int64_t steps;           /* steps this tensor has taken so far                                               */
+  int64_t steps;           /* steps this tensor has taken so far, 0 .. 2^31 - 1 (where the counter stays)       */
 } rfast_adamw_tensor;
 typedef struct rfast_adamw_options {
   int32_t param_type, grad_type, state_bits;

@@ -21,6 +21,7 @@ constexpr int kThreads = 256;
 constexpr int kBlock = 256;                    // coordinates per scale
 constexpr int kSlice = kThreads / 64 * kBlock; // coordinates that the wavefronts of a workgroup take at a time
 constexpr int kGroups = 64;                    // words for workgroups that are through
+constexpr int kMostSteps = 0x7fffffff;         // where a counter stays
 constexpr int kMostWorkgroups = 1 << 23;       // a launch has fewer than 2^32 lanes
 constexpr float kCodeMost = 448.f;             // largest finite e4m3
 constexpr float kCodeLeast = 0.001953125f;     // smallest e4m3 above zero, 2^-9
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
     const int i = __builtin_amdgcn_readfirstlane(a.whose[chunk]);
     if (a.active && a.active[i] == 0) continue;
     const Row r = a.rows[i];
-    const int t = a.steps[i] + 1;
+    const int t = min(a.steps[i], kMostSteps - 1) + 1;
     const int64_t begin = (chunk - r.first) * (U * kSlice), k0 = begin + threadIdx.x * 4;
     if (begin + U * kSlice <= r.count) step_chunk<P, G, BITS, U, STREAM, true>(a, r, t, k0);
     else step_chunk<P, G, BITS, U, STREAM, false>(a, r, t, k0);
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) rfast_adamw_kernel(Args a) {
   __syncthreads();
   if (!last) return;
   for (int i = threadIdx.x; i < a.tensors; i += kThreads)
-    if (!a.active || a.active[i] != 0) a.steps[i] += 1;
+    if (!a.active || a.active[i] != 0) a.steps[i] = min(a.steps[i], kMostSteps - 1) + 1;
 }
 
 // The AdamW variant of a round: the same moments, of the nodes about to act, from the tracked directions z; what the step would
@@ -383,7 +384,7 @@ int create(rfast_adamw** out, int32_t tensors, const rfast_adamw_tensor* t, cons
     const rfast_adamw_tensor& q = t[i];
     const std::string who = "tensor " + std::to_string(i) + ": ";
     if (!(q.weight_decay >= 0 && q.weight_decay < 1e30)) return rfast_refuse(RFAST_ERANGE, who + "weight_decay must be finite and >= 0");
-    if (q.steps < 0 || q.steps > 0x7ffffffe) return rfast_refuse(RFAST_ERANGE, who + "steps out of range");
+    if (q.steps < 0 || q.steps > kMostSteps) return rfast_refuse(RFAST_ERANGE, who + "steps out of range");
     steps[i] = (int32_t)q.steps;
     rows[i] = {q.param, q.grad, q.m, q.v, q.m_scale, q.v_scale, (u16*)q.copy, q.count, first, q.weight_decay};
     const int64_t n = (q.count + slices * kSlice - 1) / (slices * kSlice);
@@ -494,7 +495,7 @@ int rfast_adamw_steps(rfast_adamw* h, int32_t* host_steps, void* hip_stream) {
 int rfast_adamw_set_steps(rfast_adamw* h, const int32_t* host_steps, void* hip_stream) {
   if (!h || !host_steps) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   for (int32_t i = 0; i < h->a.tensors; ++i)
-    if (host_steps[i] < 0 || host_steps[i] == 0x7fffffff) return rfast_refuse(RFAST_ERANGE, "steps out of range");
+    if (host_steps[i] < 0) return rfast_refuse(RFAST_ERANGE, "steps out of range");
   hipError_t e = hipMemcpyAsync(h->a.steps, host_steps, (size_t)h->a.tensors * 4, hipMemcpyHostToDevice, (hipStream_t)hip_stream);
   if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "write of the counters");

@@ -206,3 +206,19 @@ def test_xent_gradient_in_other_columns_of_the_logits_rows(types, K):
     for at in (2 * K - 1, K + 1):
         with pytest.raises(RFastError, match="overlaps"):
             rfast_softmax_xent(both[:, K:2 * K], label, grad=both.view(gt)[:, at * narrow:at * narrow + K])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_counters_stay_at_their_largest(bits):
+    """Steps behind the 2^31st are like it: both corrections have been one for long."""
+    most, p, g = 2 ** 31 - 1, torch.zeros(100, device=DEV), torch.full((100,), 1e-3, device=DEV)
+    o = RFastAdamW([p], [g], state_bits=bits, steps=most - 1)
+    for _ in range(4):
+        o.step(1e-2)
+    assert list(o.steps()) == [most] and torch.isfinite(p).all() and (p < 0).all()
+    o.set_steps([most])
+    q, h = torch.zeros(100, device=DEV), g.clone()
+    r = RFastAdamW([q], [h], state_bits=bits, steps=most)
+    for _ in range(4):
+        r.step(1e-2)
+    assert torch.equal(p, q)
