@@ -37,6 +37,11 @@ def _sizes(*counts):
         raise RFastError(-1, f"sizes out of range: {max(counts)}")
 
 
+def _counters(steps):
+    if not all(0 <= s <= 0x7FFFFFFF for s in steps):  # (before anything cuts them to their type)
+        raise RFastError(-4, "steps out of range")
+
+
 def _type(t, name):
     k = _types.get(t.dtype)
     if k is None:
@@ -265,6 +270,7 @@ class RFastAdamW:
             self.m_scale = self.v_scale = [None] * n
         self.copies = [None] * n if copies is None else listed(copies, "copies", None)
         decay, steps = numbers(weight_decay, "weight_decay"), numbers(steps, "steps")
+        _counters(steps)
         tensors = (RfastAdamwTensor * n)()
         pt, gt = _type(params[0], "params"), _type(grads[0], "grads")
         states = (torch.float32,) if state_bits == 32 else (torch.uint8, torch.float8_e4m3fn)
@@ -300,8 +306,10 @@ class RFastAdamW:
         return rfast_adamw_steps(self.handle, np.empty(len(self.params), dtype=np.int32), self.device)
 
     def set_steps(self, steps):
-        steps = np.ascontiguousarray(steps, dtype=np.int32)
+        steps = np.asarray(steps)
         _need(steps.shape == (len(self.params),), "need one number per tensor")
+        _counters(steps)
+        steps = np.ascontiguousarray(steps, dtype=np.int32)
         rfast_adamw_set_steps(self.handle, steps, self.device)
 
     def close(self):

@@ -222,3 +222,18 @@ def test_adamw_counters_stay_at_their_largest(bits):
     for _ in range(4):
         r.step(1e-2)
     assert torch.equal(p, q)
+
+
+def test_adamw_counters_out_of_range_are_refused():
+    p, g = torch.zeros(10, device=DEV), torch.zeros(10, device=DEV)
+    o = RFastAdamW([p], [g], steps=7)
+    for bad in (2 ** 32, 2 ** 32 + 5, 2 ** 31, -1, 2 ** 64 + 5):
+        with pytest.raises(RFastError, match="range"):
+            o.set_steps([bad])
+        with pytest.raises(RFastError, match="range"):
+            RFastAdamW([p], [g], steps=bad)
+    with pytest.raises(RFastError, match="range"):
+        o.set_steps(np.array([2 ** 32 + 5]))
+    assert list(o.steps()) == [7]
+    o.set_steps(np.array([9]))
+    assert list(o.steps()) == [9]
