@@ -411,7 +411,7 @@ int rfast_diagnostics_static(rfast_ctx* ctx, const float* d_xstar, double* d_out
  * the gradient kernels of each round (at most 4096 rounds are kept since the
  * last enable).  rfast_kernel_time waits for the stream and returns the summed
  * milliseconds and the number of timed launches of `which`
- * (0 = fused/mix+track state kernels, 1 = gradient kernels, 2 = resolver).
+ * (0 = fused/mix+track state kernels and rfast_set_adamw's, 1 = gradient kernels, 2 = resolver).
  * Rounds that teams of workgroups would take (rfast_use_blocks: least squares, logistic
  * and softmax regression) run as kernels per round while this is on, whose state and
  * gradient kernels can be told apart: the times are those of that form, not of the one

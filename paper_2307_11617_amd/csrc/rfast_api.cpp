@@ -957,7 +957,9 @@ static int float_round(rfast_ctx* c, float gamma, const int32_t* d_batch_idx, bo
   gamma = gamma_now(c, gamma);
   hipError_t e;
   if (c->adamw.bits) {
+    time_begin(c, 0);
     e = rfast_launch_adamw_round(c, false, 0);
+    time_end(c, 0);
     if (e != hipSuccess) return hipfail(c, e, "AdamW launch");
   }
   if (separable) {
@@ -1370,7 +1372,9 @@ int rfast_sync_round(rfast_ctx* c, float gamma, const int32_t* d_batch_idx) {
   gamma = gamma_now(c, gamma);
   hipError_t e;
   if (c->adamw.bits) {
+    time_begin(c, 0);
     e = rfast_launch_adamw_round(c, true, c->sync_parity);
+    time_end(c, 0);
     if (e != hipSuccess) return hipfail(c, e, "AdamW launch");
   }
   time_begin(c, 0);
@@ -1730,7 +1734,7 @@ int rfast_profile_enable(rfast_ctx* c, int32_t on) {
   if (on && c->ev[0][0].empty()) {
     for (int w = 0; w < 3; ++w)
       for (int s = 0; s < 2; ++s) {
-        const size_t cnt = (w == 0 ? 2 : 1) * kMax;
+        const size_t cnt = (w == 0 ? 3 : 1) * kMax;  // mix, track and AdamW
         c->ev[w][s].resize(cnt);
         for (size_t k = 0; k < cnt; ++k)
           if (hipEventCreate(&c->ev[w][s][k]) != hipSuccess) return fail(c, RFAST_EHIP, "hipEventCreate failed");

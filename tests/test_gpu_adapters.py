@@ -343,3 +343,26 @@ def test_loss_whose_last_rows_are_fewer():
     want = orc.diagnostics()["loss_at_xbar"]
     assert abs(gpu.diagnostics()["loss_at_xbar"] - want) <= 1e-2 * abs(want)
     gpu.check()
+
+
+@pytest.mark.parametrize("make,each", [(lambda: quad(5, 300, 41), 1), (lambda: configs.config1(p=256, samples=64, batch=16, rounds=20), 2)])
+def test_adamw_launches_are_timed(make, each):
+    """The launch that moves the moments counts with the state kernels, `each` a round without it."""
+    from paper_2307_11617_amd import rfast_kernel_time, rfast_profile_enable
+    w = make()
+    gpu = harness.make_gpu(w)
+    for adamw in (0, 1):
+        if adamw:
+            gpu.set_adamw()
+        gpu.init(None, w.sched.initial_batch())
+        from paper_2307_11617_amd import rfast_use_blocks
+        rfast_use_blocks(gpu.ctx, False)
+        rfast_profile_enable(gpu.ctx, True)
+        st, dev = harness.upload_chunk(gpu, w, 0, 10)
+        gpu.run(10, dev["active"], dev["delay_R"], dev["delay_C"], dev["drop_R"], dev["drop_C"], w.gamma, dev["batch_idx"])
+        ms, count = rfast_kernel_time(gpu.ctx, 0)
+        assert count == 10 * (each + adamw) and ms > 0
+        rfast_profile_enable(gpu.ctx, True)
+        gpu.sync_run(4, w.gamma, None if dev["batch_idx"] is None else dev["batch_idx"][:4].contiguous())
+        assert rfast_kernel_time(gpu.ctx, 0)[1] == 4 * (each + adamw)
+        rfast_profile_enable(gpu.ctx, False)
