@@ -366,3 +366,23 @@ def test_adamw_launches_are_timed(make, each):
         gpu.sync_run(4, w.gamma, None if dev["batch_idx"] is None else dev["batch_idx"][:4].contiguous())
         assert rfast_kernel_time(gpu.ctx, 0)[1] == 4 * (each + adamw)
         rfast_profile_enable(gpu.ctx, False)
+
+
+@pytest.mark.parametrize("kw", [dict(n=6, d=64, K=24, rank=4, samples=64, batch=0), dict(n=5, d=37, K=150, rank=3, samples=50, batch=0),
+                                dict(n=3, d=96, K=40, rank=40, samples=40, batch=0)])
+def test_adapter_synchronous_steps(kw):
+    """Push-pull steps of all nodes with full gradients, alone and with event-driven iterations of one node between them."""
+    w, x0 = adapters(**kw)
+    plain, gpu = make_oracle(w, x0=x0), harness.make_gpu(w)
+    orc = PushPullOracle(w.R.dense(), w.C.dense(), plain.obj, x0=x0)
+    gpu.init(x0, None)
+    for steps in (1, 1, 7):
+        gpu.sync_run(steps, w.gamma)
+        for _ in range(steps):
+            orc.step(w.gamma)
+        gpu.check()
+        assert harness.rel_l2(gpu.read("X"), orc.x) <= w.tol and harness.rel_l2(gpu.read("Z"), orc.z, 1e-3 * np.linalg.norm(orc.g)) <= 10 * w.tol
+    before = gpu.read("X")
+    gpu.run_events(1, 3, None, 0, 0.0, 1e-2)
+    gpu.check()
+    assert (np.abs(gpu.read("X") - before).max(axis=1) > 0).sum() == 1
