@@ -106,6 +106,3 @@ template <class F> __device__ inline float wave_reduce(float v, F f) {
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
 }
-__device__ inline float wave_sum(float v) {
-  return wave_reduce(v, [](float a, float b) { return a + b; });
-}

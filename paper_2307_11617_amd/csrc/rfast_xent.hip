@@ -3,7 +3,7 @@
 //   lse = log sum exp l_k,  loss = lse - l_label,  grad_k = c (exp(l_k - lse) - [k == label])
 //
 // Some five operations per logit, so the bound is one read of the logits and one write of the gradient.  A row therefore stays in
-// registers between the two: a wavefront's up to kWaveMost logits, a workgroup's of 256 or 1024 lanes beyond.  Rows longer than the registers
+// registers between the two: of 8 to 64 lanes up to 1024 logits (2048 of bf16), of a workgroup of 256 to 1024 lanes beyond.  Rows longer than the registers
 // of a workgroup are read twice, the second time through the caches, with a running maximum and sum per lane in the first pass.
 // A row's maximum is taken out of its exponents before they are formed, so that nothing overflows; sums are in 32 bits,
 // one per lane and then a tree.
