@@ -329,9 +329,10 @@ def main():
     n_state = n_grad = n_res = 0
     # launches of the multi-round kernel (rounds, ms, bytes, rows in, rows out, node-updates) and, of the rounds that ran
     # one pass each, time, bytes and node-updates
-    launches_multi, one_ms, one_bytes, one_updates, one_launches = [], 0.0, 0.0, 0, 0
+    launches_multi, one_ms, one_bytes, one_updates, one_launches, one_rounds = [], 0.0, 0.0, 0, 0, []
     lanes, per_wave = rf.rfast_block_info(gpu.ctx, with_kind=True) if multi else (0, False)
-    for lo, hi in segs:
+    while segs:
+        lo, hi = segs.pop(0)
         before = None if args.sync else read_stamps(gpu)
         rf.rfast_profile_enable(gpu.ctx, True)
         run(cut(lo, hi), hi - lo)
@@ -362,6 +363,10 @@ def main():
             act = (after["t"] != before["t"])
             one_bytes += one_pass_bytes(w, edges, before, after, act) + momentum_words * 4.0 * w.p * float(act.sum())
             one_ms, one_updates, one_launches = one_ms + ms, one_updates + done, one_launches + cnt
+            one_rounds.append(lo)
+        if not segs and not launches_multi and not one_rounds:
+            # fewer rounds than the multi-round kernel takes: those of the call ran one pass each, unseen in between; the next ones call by call
+            segs = [(W + 2 * K + q, W + 2 * K + q + 1) for q in range(K1)]
 
     act_timed = st["active"][W:W + K].astype(np.int64)
     act_prof = st["active"][W + K:W + 2 * K].astype(np.int64)
@@ -431,14 +436,14 @@ def main():
                              "launch when they fit, not counted); flops_per_launch: (4 B + 21) p per node-update"})
     else:
         # One pass over HBM per round (two for the objectives whose gradient runs between them).
-        secs = one_ms * 1e-3
+        secs = one_ms * 1e-3 if one_rounds else float("inf")  # (no round seen alone: rates of zero)
         launches = max(one_launches, 1)
         kernel = "rfast_state_kernel" + ("<FUSED>" if separable else "<MIX> + <TRACK>")
         if w.objective in ("least_squares", "logistic") and not args.no_blocks:
             # this leg runs its rounds in calls of one: a mixing pass, then the kernel that does the column sums and the
             # tracker update (in a longer call it also mixes for the next round and the mixing pass runs once per stretch)
             kernel = "rfast_state_kernel<MIX> + rfast_cols_track_mix_kernel"
-        act1 = act_prof
+        act1 = st["active"][one_rounds].astype(np.int64)
         alg1 = sum(algorithmic_bytes_per_round(w, a) for a in act1)
         lay1 = sum(algorithmic_bytes_per_round(w, a, layout=True) for a in act1)
         counted = counted_traffic(w.name, "state", 1) if headline and separable else None
