@@ -140,3 +140,20 @@ def test_adamw_refuses_an_eps_that_32_bits_do_not_hold(eps):
     """A coordinate that never had a gradient is divided by eps alone: 0 / 0, or by the infinite reciprocal of a denormal."""
     code, msg = create(tensors(), eps=eps)
     assert code == -4 and "eps" in msg
+
+
+def test_lora_most_segments_beside_most_tiles():
+    """Blocks of rows and tiles of matrices turned over, in one launch, are fewer than 2^32 lanes together."""
+    def lanes(s):
+        tiles = s.adapters * ((s.K + 63) // 64 + (s.d + 63) // 64) + (s.K + 63) // 64 * ((s.d + 63) // 64)
+        rows = 16 if s.rows <= 1024 else 32
+        waves = 8 if s.rows <= 1024 else 4
+        return (s.rows // rows + s.segments + 2 + (tiles + waves - 1) // waves) * 64 * waves
+    taken = 0
+    for rows in (1, 1000, 1024, 1025, 1 << 16):
+        for K in range(32704 - 64 * 4, 32704 + 1):
+            s = shape(rows=rows, segments=1 << 22, adapters=65535, d=64, K=K, rank=1, ld_x=64, ld_y=K)
+            if rf.rfast_lora_workspace_bytes(s, 2) > 0:
+                taken += 1
+                assert lanes(s) < 1 << 32, (rows, K)
+    assert taken > 0
