@@ -321,8 +321,8 @@ Layout layout_of(int32_t tensors, int64_t chunks) {
   return l;
 }
 // Slices per chunk.  32 bits: one (four loads per lane under way; 16 x 11.2 M coordinates 807 us, with two 875, with four 885).  8 bits,
-// whose loads of the moments are short: four where there are chunks enough (525; 564 with two, 635 with one; 75 tensors of 200000 on
-// average 43 / 44 / 50), else two (40 of 100000: 16.1; 17.6 with four, 17.7 with one).
+// whose loads of the moments are short: four where there are chunks enough (507; 548 with two, 618 with one; 75 tensors of 200000 on
+// average 41 / 40 / 47), else two (40 of 100000: 16.1; 17.6 with four, 17.7 with one).
 int64_t slices_for(int32_t tensors, const rfast_adamw_tensor* t, int32_t bits, int64_t* chunks) {
   const int64_t most = bits == 32 ? 1 : 4;
   if (!count_chunks(tensors, t, most, chunks)) return 0;

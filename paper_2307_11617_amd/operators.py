@@ -3,7 +3,9 @@ projection, softmax cross-entropy with its gradient, and AdamW over many tensors
 
 Every call runs on the current stream of its tensors' device and neither waits nor reads anything back, so that it can be captured
 into a graph.  Workspaces come from torch's allocator with each call: calls on different streams, and graphs, share none.
-What the library cannot see (extents, types, devices of tensors) is checked here, before any launch."""
+What the library cannot see (extents, types, devices of tensors) is checked here, before any launch.
+None takes part in torch's autograd: inputs that require gradients are read as they are and results require none; gradients are the backward
+calls' own results."""
 from __future__ import annotations
 
 import ctypes as C
@@ -80,7 +82,7 @@ def _vector(t, name, count, dtype, device):
 
 
 def rfast_softmax_xent(logits, labels, grad_scale=1.0, grad_dtype=None, grad=None, loss=None, lse=None, rows=None):
-    """(loss, grad) of rows of logits [T][K] (float32 or bfloat16): loss float32 [T], grad = grad_scale (softmax - onehot) in
+    """(loss, grad) of rows of logits [T][K] (float32 or bfloat16) with labels int32 [T] (outside [0, K): padding): loss float32 [T], grad = grad_scale (softmax - onehot) in
     grad_dtype (default: the logits').  grad: tensor to write to, `logits` itself for its place, or False for no gradient.
     lse: float32 [T] to receive log sum exp.  rows: int32 [1] on the device; only that many rows are taken, the others of the
     outputs are not written."""
@@ -173,7 +175,7 @@ def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, o
 
 def rfast_lora_backward(x, w, a, b, row_ptr, adapter, dy, scale=1.0, need_dx=True, dx=None, da=None, db=None):
     """(dx, da, db) of rfast_lora_forward for dy bfloat16 [T][K], w frozen: dx bfloat16 [T][d] (None unless need_dx or a tensor to write to
-    is given; rows behind the last segment are not written), da float32 [adapters][rank][d], db float32 [adapters][K][rank]."""
+    is given, its rows as far apart as x's; rows behind the last segment are not written), da float32 [adapters][rank][d], db float32 [adapters][K][rank]."""
     torch = _t()
     _need(x.dim() == 2 and w.dim() == 2, "need matrices x [rows][d] and w [K][d]")
     T, d = x.shape
@@ -230,7 +232,8 @@ class RFastAdamW:
     params, grads: contiguous float32 or bfloat16 tensors of one device, the same tensors at every step (gradients are read where they
     were given).  m, v: the moments, made as zeros where not given (state_bits 32: float32; 8: uint8 or float8_e4m3fn codes of m and
     sqrt(v), with m_scale and v_scale float32 [ceil(count / 256)]).  weight_decay: one number or one per tensor.  copies: bfloat16 tensors (or None each) that receive the
-    new parameters rounded.  steps: taken before, one number or one per tensor."""
+    new parameters rounded.  steps: taken before, one number or one per tensor.
+    A graph that holds steps needs the object for as long as it is replayed."""
 
     def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, state_bits=32, betas=(0.9, 0.999), eps=1e-8,
                  weight_decay=0.0, copies=None, steps=0):
