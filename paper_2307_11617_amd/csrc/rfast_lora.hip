@@ -972,8 +972,10 @@ Layout layout_of(const rfast_lora_shape& s, int pass) {
 bool shape_ok(const rfast_lora_shape* s) {
   if (!s || s->rows < 0 || s->segments < 1 || s->adapters < 1 || s->d < 1 || s->K < 1 || s->rank < 1 || s->rank > kMostRank) return false;
   if (s->segments > 1 << 22 || s->rows > 1 << 26 || s->ld_x > 1 << 22 || s->ld_y > 1 << 22 || s->d > 1 << 22 || s->K > 1 << 22 || s->adapters > 65535) return false;
-  // a launch has fewer than 2^32 lanes, also one that turns the matrices over: 512 for each of up to 2^22 + 67 blocks of rows, 64 for a tile
-  if ((int64_t)s->adapters * ((s->K + 63) / 64 + (s->d + 63) / 64) + (int64_t)((s->K + 63) / 64) * ((s->d + 63) / 64) >= ((int64_t)1 << 25) - 1024) return false;
+  // a launch has fewer than 2^32 lanes, also one that turns the matrices over: 64 for each of their tiles beside 512 for a block of rows, of which
+  // there are up to 66 more than segments (with more than 1024 rows 256 lanes, of up to 2^22 + 2^21 + 2)
+  const int64_t tiles = (int64_t)s->adapters * ((s->K + 63) / 64 + (s->d + 63) / 64) + (int64_t)((s->K + 63) / 64) * ((s->d + 63) / 64);
+  if (tiles >= (int64_t)1 << 25 || tiles + 8 * ((int64_t)s->segments + 67) >= (int64_t)1 << 26) return false;
   return ((int64_t)s->rows / 128 + 1) * (std::max(s->d, s->K) / 64 + 1) < (int64_t)1 << 23;
 }
 

@@ -82,8 +82,8 @@ def _vector(t, name, count, dtype, device):
 
 
 def rfast_softmax_xent(logits, labels, grad_scale=1.0, grad_dtype=None, grad=None, loss=None, lse=None, rows=None):
-    """(loss, grad) of rows of logits [T][K] (float32 or bfloat16) with labels int32 [T] (outside [0, K): padding): loss float32 [T], grad = grad_scale (softmax - onehot) in
-    grad_dtype (default: the logits').  grad: tensor to write to, `logits` itself for its place, or False for no gradient.
+    """(loss, grad) of rows of logits [T][K] (float32 or bfloat16) with labels int32 [T] (outside [0, K): padding): loss float32 [T],
+    grad = grad_scale (softmax - onehot) in grad_dtype (default: the logits').  grad: tensor to write to, `logits` itself for its place, or False for no gradient.
     lse: float32 [T] to receive log sum exp.  rows: int32 [1] on the device; only that many rows are taken, the others of the
     outputs are not written."""
     torch = _t()
@@ -175,7 +175,8 @@ def rfast_lora_forward(x, w, a, b, row_ptr, adapter=None, scale=1.0, out=None, o
 
 def rfast_lora_backward(x, w, a, b, row_ptr, adapter, dy, scale=1.0, need_dx=True, dx=None, da=None, db=None):
     """(dx, da, db) of rfast_lora_forward for dy bfloat16 [T][K], w frozen: dx bfloat16 [T][d] (None unless need_dx or a tensor to write to
-    is given, its rows as far apart as x's; rows behind the last segment are not written), da float32 [adapters][rank][d], db float32 [adapters][K][rank]."""
+    is given, its rows as far apart as x's; rows behind the last segment are not written), da float32 [adapters][rank][d], db
+    float32 [adapters][K][rank]."""
     torch = _t()
     _need(x.dim() == 2 and w.dim() == 2, "need matrices x [rows][d] and w [K][d]")
     T, d = x.shape

@@ -157,3 +157,5 @@ def test_lora_most_segments_beside_most_tiles():
                 taken += 1
                 assert lanes(s) < 1 << 32, (rows, K)
     assert taken > 0
+    s = shape(rows=1000, segments=1, adapters=65535, d=64, K=32704 - 64, rank=1, ld_x=64, ld_y=32704)  # few segments beside nearly as many tiles
+    assert rf.rfast_lora_workspace_bytes(s, 2) > 0 and lanes(s) < 1 << 32
