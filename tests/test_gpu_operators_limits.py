@@ -237,3 +237,87 @@ def test_adamw_counters_out_of_range_are_refused():
     assert list(o.steps()) == [7]
     o.set_steps(np.array([9]))
     assert list(o.steps()) == [9]
+
+
+@pytest.mark.parametrize("K", [48, 264])
+def test_lora_offsets_that_pass_32_bits(K):
+    """Rows and outputs 40000 elements apart, 70000 of them: the last lie 2.8e9 elements behind the first, and are what the same rows alone give."""
+    T, d, r, apart, scale = 70000, 64, 8, 40000, 0.5
+    g = gen(9)
+    x, w, a, b, dy = ((torch.randn(s, generator=g) * std).to(BF16).to(DEV) for s, std in
+                      (((T, d), 1), ((K, d), 0.1), ((2, r, d), 0.1), ((2, K, r), 0.5), ((T, K), 0.1)))
+    wide = torch.zeros((T, apart), dtype=BF16, device=DEV)
+    xs, ys, dxs = wide[:, :d], wide[:, 1024:1024 + K], wide[:, 2048:2048 + d]
+    dys = torch.zeros((T, apart), dtype=BF16, device=DEV)[:, 512:512 + K]
+    xs.copy_(x)
+    dys.copy_(dy)
+    ptr = torch.tensor([0, 35001, T], dtype=torch.int32, device=DEV)
+    y = rfast_lora_forward(xs, w, a, b, ptr, scale=scale, out=ys)
+    dx, da, db = rfast_lora_backward(xs, w, a, b, ptr, None, dys, scale=scale, dx=dxs)
+    want = rfast_lora_forward(x, w, a, b, ptr, scale=scale)
+    back = rfast_lora_backward(x, w, a, b, ptr, None, dy, scale=scale)
+    for got, other in ((y, want), (dx, back[0]), (da, back[1]), (db, back[2])):
+        assert torch.isfinite(other).all() and torch.equal(got, other)
+    low = 69900  # and the last rows against the formula: a sum of n exact products of bf16 is off by 2^-23 n of their magnitudes, rounded to bf16
+    x64, w64, a64, b64, dy64 = x[low:].double(), w.double(), a[1].double(), b[1].double(), dy[low:].double()
+    y64 = x64 @ w64.t() + scale * (x64 @ a64.t()) @ b64.t()
+    size = x64.abs() @ w64.abs().t() + scale * (x64.abs() @ a64.abs().t()) @ b64.abs().t()
+    assert ((y[low:].double() - y64).abs() <= 2.0 ** -23 * 2 * (d + 2 * r + 8) * size + 2.0 ** -8 * y64.abs() * 1.01).all()
+    assert not wide[:, 3000:].any()
+
+
+def test_training_step_captured_whole():
+    """Forward, loss, backward and step of adapters in one graph: every replay is the eager step from the same state."""
+    T, d, K, r = 300, 72, 40, 6
+    g = gen(10)
+    w = (torch.randn((K, d), generator=g) * 0.1).to(BF16).to(DEV)
+    ptr = torch.tensor([0, 100, 100, 250], dtype=torch.int32, device=DEV)  # (rows behind the last segment too)
+    start = [torch.randn((3, r, d), generator=g) * 0.1, torch.randn((3, K, r), generator=g) * 0.3]
+    data = [((torch.randn((T, d), generator=g)).to(BF16), torch.randint(-1, K, (T,), generator=g).to(torch.int32)) for _ in range(5)]
+
+    def make():
+        x, label = torch.zeros((T, d), dtype=BF16, device=DEV), torch.zeros(T, dtype=torch.int32, device=DEV)
+        master = [t.to(DEV) for t in start]
+        held = [t.to(BF16) for t in master]
+        grads = [torch.zeros_like(t) for t in master]
+        logits, dy = torch.zeros((T, K), device=DEV), torch.zeros((T, K), dtype=BF16, device=DEV)
+        loss, opt = torch.zeros(T, device=DEV), RFastAdamW(master, grads, copies=held, state_bits=8, weight_decay=0.01)
+
+        def step():
+            rfast_lora_forward(x, w, *held, ptr, scale=0.5, out=logits)
+            rfast_softmax_xent(logits, label, grad_scale=1 / T, grad=dy, loss=loss, rows=ptr[3:])
+            rfast_lora_backward(x, w, *held, ptr, None, dy, scale=0.5, need_dx=False, da=grads[0], db=grads[1])
+            opt.step(1e-2)
+        return x, label, step, [*master, *held, *grads, loss, logits, dy], opt
+
+    (x, label, step, state, opt), (x2, label2, step2, state2, opt2) = make(), make()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k, (rows, classes) in enumerate(data):
+        for to, frm in ((x, rows), (x2, rows), (label, classes), (label2, classes)):
+            to.copy_(frm)
+        graph.replay()
+        step2()
+        torch.cuda.synchronize()
+        for p, q in zip(state, state2):
+            assert torch.equal(p, q) and torch.isfinite(p).all()
+        assert (opt.steps() == k + 1).all() and (opt2.steps() == k + 1).all()
+    assert (state[0][1] != start[0][1].to(DEV)).any() and not state[4][1].any()  # the second adapter has no rows: decay alone
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_tensor_of_more_than_2_to_the_31(bits):
+    """One tensor of 2^31 + 513 coordinates, all alike but for its last ones: offsets pass 32 bits, the last block is short."""
+    count = 2 ** 31 + 513
+    p, g = torch.zeros(count, dtype=BF16, device=DEV), torch.ones(count, dtype=BF16, device=DEV)
+    g[-700:] = -1.0
+    g[-1] = 0.0
+    o = RFastAdamW([p], [g], state_bits=bits)
+    o.step(0.5)  # the first step is gamma times the gradient's sign, to eps
+    assert (p[:-700] == -0.5).all() and (p[-700:-1] == 0.5).all() and p[-1].item() == 0
+    m = o.m[0].view(F8) if bits == 8 else o.m[0]
+    assert (m[-700:-1].float() < 0).all() and m[-1].float().item() == 0 and (o.steps() == 1).all()
+    if bits == 8:
+        scale = o.m_scale[0]  # (the last block is the last coordinate alone)
+        assert scale.numel() == 2 ** 23 + 3 and (scale[:-1] == scale[0]).all() and scale[0] > 0 and scale[-1] == 0
