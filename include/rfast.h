@@ -515,6 +515,73 @@ int rfast_adamw_steps(rfast_adamw* h, int32_t* host_steps, void* hip_stream);
 int rfast_adamw_set_steps(rfast_adamw* h, const int32_t* host_steps, void* hip_stream);
 void rfast_adamw_destroy(rfast_adamw* h);
 
+/* The clipped loss of a policy over K classes with its gradient, in one pass over the logits.  Of a row with action a:
+ *   logp = l_a - log sum_k exp(l_k),   r = exp(logp - old_logp),   q = reference - logp,
+ *   loss = weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + beta (exp(q) - q - 1)),
+ *   s = weight (-[not clipped] r A + beta (1 - exp(q))),   grad_k = grad_scale s ([k == a] - exp(l_k) / sum).
+ * Clipped is a row with A > 0 and r > 1 + clip_high, or A < 0 and r < 1 - clip_low.  logits, actions (as labels), grad, d_rows: as in
+ * rfast_softmax_xent; also what is said there of masked classes, padding (loss, gradient and logp 0; so for a row that is masked out entirely)
+ * and logits that are NaN or +infinity.  old_logp, advantage: device fp32 [rows].  reference: device fp32 [rows] or NULL (no second
+ * term).  weight: device fp32 [rows] or NULL (1); a row of weight 0 has loss and gradient 0 whatever its other numbers.  loss, logp: device fp32 [rows] or NULL (not wanted).
+ * An action at a masked class of another row: logp -infinity, r 0, gradient 0 (loss +infinity where beta > 0 and there is a reference).
+ * Numbers that 32 bits do not hold (an r A or exp(q) beyond 3.4e38 that counts) make the row's loss infinite and its gradient not finite.
+ * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0, all finite (RFAST_ERANGE). */
+int rfast_policy_loss(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits, const int32_t* actions,
+                      const float* old_logp, const float* advantage, const float* reference, const float* weight, float clip_low,
+                      float clip_high, float beta, float grad_scale, float* loss, float* logp, void* grad, int32_t grad_type,
+                      int64_t ld_grad, const int32_t* d_rows, void* hip_stream);
+
+/* Rows of a table of embeddings: out_t = scale table[token_t], rounded once.  table: device [vocabulary][ld_table >= d].  tokens: device int32
+ * [rows]; one outside [0, vocabulary) (-1 by convention) is padding: a row of zeros.  out: device [rows][ld_out >= d]. */
+int rfast_embedding(int32_t rows, int32_t vocabulary, int32_t d, const void* table, int32_t table_type, int64_t ld_table,
+                    const int32_t* tokens, float scale, void* out, int32_t out_type, int64_t ld_out, void* hip_stream);
+/* Its gradient: grad_v = scale sum of dy_t over the rows with token_t = v, in 32 bits in an order that the tokens alone decide (the same call
+ * gives the same bits).  accumulate 0: every row of grad is written, zeros where no token is.  accumulate 1: added to what grad holds (in 32
+ * bits, rounded once), rows without a token stay as they are.  workspace: device, 256-byte aligned, contents arbitrary. */
+size_t rfast_embedding_backward_workspace_bytes(int32_t rows, int32_t vocabulary, int32_t d);
+int rfast_embedding_backward(int32_t rows, int32_t vocabulary, int32_t d, const void* dy, int32_t dy_type, int64_t ld_dy,
+                             const int32_t* tokens, float scale, void* grad, int32_t grad_type, int64_t ld_grad, int32_t accumulate,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Rows sent to experts and back: a router chooses k of `experts` for every row, the pairs (row, choice) are sorted by expert, and rows travel
+ * along that order.  The sorted rows with row_ptr are what rfast_lora_forward and _backward take as rows and segments (adapter NULL).
+ *
+ * Choice: the k largest logits of a row, largest first, of equal ones the lowest expert; a logit of -infinity is an expert that is masked
+ * out and never chosen: choices that are left over get expert -1 and weight 0.  NaN counts as larger than all numbers.
+ *   normalise 1: weight_j = exp(l_j) / sum over the row's choices;   0: / sum over all experts.
+ * A chosen logit of NaN or +infinity makes the row's weights NaN.
+ * Order: pair i = row k + choice; row_ptr [experts + 1]: where each expert's pairs begin; place [rows k]: where a pair is in
+ * that order; order [rows k]: which pair is there.  Pairs of one expert keep their order.  A pair without an expert (a number outside [0, experts)) has
+ * place -1, and order holds -1 from row_ptr[experts] on.
+ * Limits: k 1 .. min(experts, 64); rfast_route: experts 1 .. 1024; rows k < 2^31. */
+size_t rfast_route_workspace_bytes(int32_t pairs, int32_t experts);
+/* logits: device [rows][ld >= experts].  expert, place: device int32 [rows][k]; weight: fp32 [rows][k]; order int32 [rows k]. */
+int rfast_route(int32_t rows, int32_t experts, int32_t k, const void* logits, int32_t logits_type, int64_t ld_logits, int32_t normalise,
+                int32_t* expert, float* weight, int32_t* row_ptr, int32_t* place, int32_t* order, void* workspace,
+                size_t workspace_bytes, void* hip_stream);
+/* The order alone, of experts (or adapters) chosen elsewhere: expert device int32 [pairs]; experts >= 1. */
+int rfast_route_plan(int32_t pairs, int32_t experts, const int32_t* expert, int32_t* row_ptr, int32_t* place, int32_t* order,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Gradient of the logits from that of the weights: dlogits_e = sum_j [e = expert_j] weight_j dweight_j - p_e sum_j weight_j dweight_j, p_e the share
+ * of e in the sum that weights are divided by.  expert, weight: as rfast_route returned them.  logits: read if normalise is 0 (else may be NULL).
+ * dlogits: device [rows][ld_dlogits >= experts], 0 for masked experts.  experts 1 .. 1024. */
+int rfast_route_backward(int32_t rows, int32_t experts, int32_t k, const void* logits, int32_t logits_type, int64_t ld_logits,
+                         int32_t normalise, const int32_t* expert, const float* weight, const float* dweight, void* dlogits,
+                         int32_t dlogits_type, int64_t ld_dlogits, void* hip_stream);
+/* sorted[place_tj] = x_t.  x: device [rows][ld_x >= d], type `type`; sorted: device [sorted_rows][ld_sorted >= d] of the same type.  A place outside
+ * [0, sorted_rows) is none.  Rows of `sorted` that are nobody's place are not written; no place may be there twice. */
+int rfast_route_gather(int32_t rows, int32_t k, int32_t d, const void* x, int32_t type, int64_t ld_x, const int32_t* place, void* sorted,
+                       int32_t sorted_rows, int64_t ld_sorted, void* hip_stream);
+/* y_t = sum_j weight_tj sorted[place_tj] (weight NULL: 1, which is the gradient of rfast_route_gather), summed in 32 bits in the order of j and rounded once;
+ * a place outside [0, sorted_rows) counts for nothing.  y: device [rows][ld_y >= d]. */
+int rfast_route_combine(int32_t rows, int32_t k, int32_t d, const void* sorted, int32_t type, int32_t sorted_rows, int64_t ld_sorted,
+                        const int32_t* place, const float* weight, void* y, int32_t y_type, int64_t ld_y, void* hip_stream);
+/* Its gradient: dsorted[place_tj] = weight_tj dy_t (rounded once; rows that are nobody's place are not written), dweight_tj = <sorted[place_tj], dy_t>
+ * in 32 bits (0 without a place).  sorted, dy and dsorted have one type.  weight NULL: 1.  dsorted or dweight may be NULL (not wanted). */
+int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, const void* sorted, int32_t type, int32_t sorted_rows,
+                                 int64_t ld_sorted, const int32_t* place, const float* weight, const void* dy, int64_t ld_dy,
+                                 void* dsorted, int64_t ld_dsorted, float* dweight, void* hip_stream);
+
 const char* rfast_last_error(const rfast_ctx* ctx);
 void rfast_destroy(rfast_ctx* ctx);
 

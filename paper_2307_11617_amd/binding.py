@@ -55,7 +55,9 @@ EXPORTS = ["rfast_common_roots", "rfast_workspace_bytes", "rfast_create", "rfast
            "rfast_read_state", "rfast_write_state", "rfast_diagnostics", "rfast_diagnostics_static", "rfast_profile_enable", "rfast_kernel_time", "rfast_last_error",
            "rfast_destroy", "rfast_softmax_xent", "rfast_lora_workspace_bytes", "rfast_lora_forward", "rfast_lora_backward",
            "rfast_adamw_workspace_bytes", "rfast_adamw_create", "rfast_adamw_step", "rfast_adamw_steps", "rfast_adamw_set_steps",
-           "rfast_adamw_destroy", "rfast_adamw_state_bytes", "rfast_set_adamw"]
+           "rfast_adamw_destroy", "rfast_adamw_state_bytes", "rfast_set_adamw", "rfast_policy_loss", "rfast_embedding",
+           "rfast_embedding_backward_workspace_bytes", "rfast_embedding_backward", "rfast_route_workspace_bytes", "rfast_route", "rfast_route_plan",
+           "rfast_route_backward", "rfast_route_gather", "rfast_route_combine", "rfast_route_combine_backward"]
 
 
 def lib():
@@ -148,6 +150,29 @@ def lib():
     L.rfast_adamw_set_steps.argtypes = [vp, vp, vp]
     L.rfast_adamw_destroy.restype = None
     L.rfast_adamw_destroy.argtypes = [vp]
+    f32 = C.c_float
+    L.rfast_policy_loss.restype = C.c_int
+    L.rfast_policy_loss.argtypes = [i32, i32, vp, i32, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i32, i64, vp, vp]
+    L.rfast_embedding.restype = C.c_int
+    L.rfast_embedding.argtypes = [i32, i32, i32, vp, i32, i64, vp, f32, vp, i32, i64, vp]
+    L.rfast_embedding_backward_workspace_bytes.restype = sz
+    L.rfast_embedding_backward_workspace_bytes.argtypes = [i32, i32, i32]
+    L.rfast_embedding_backward.restype = C.c_int
+    L.rfast_embedding_backward.argtypes = [i32, i32, i32, vp, i32, i64, vp, f32, vp, i32, i64, i32, vp, sz, vp]
+    L.rfast_route_workspace_bytes.restype = sz
+    L.rfast_route_workspace_bytes.argtypes = [i32, i32]
+    L.rfast_route.restype = C.c_int
+    L.rfast_route.argtypes = [i32, i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.rfast_route_plan.restype = C.c_int
+    L.rfast_route_plan.argtypes = [i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.rfast_route_backward.restype = C.c_int
+    L.rfast_route_backward.argtypes = [i32, i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, i32, i64, vp]
+    L.rfast_route_gather.restype = C.c_int
+    L.rfast_route_gather.argtypes = [i32, i32, i32, vp, i32, i64, vp, vp, i32, i64, vp]
+    L.rfast_route_combine.restype = C.c_int
+    L.rfast_route_combine.argtypes = [i32, i32, i32, vp, i32, i32, i64, vp, vp, vp, i32, i64, vp]
+    L.rfast_route_combine_backward.restype = C.c_int
+    L.rfast_route_combine_backward.argtypes = [i32, i32, i32, vp, i32, i32, i64, vp, vp, vp, i64, vp, i64, vp, vp]
     _lib = L
     return L
 

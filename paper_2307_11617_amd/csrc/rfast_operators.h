@@ -26,6 +26,26 @@ inline bool rfast_overlap(const RfastArea& a, const RfastArea& b) {
   return behind < a.wide || behind + b.wide > a.apart;
 }
 
+// Stable sort of `count` numbers; those outside [0, keys) come last.  Any of the outputs but one may be NULL (rfast_sort.hip).
+struct RfastSort {
+  int32_t count, keys;
+  const int32_t* key;   // [count]
+  int32_t* row_ptr;     // [keys + 1]: where each number begins
+  int32_t* place;       // [count]: where element i is, -1 if outside
+  int32_t* order;       // [count]: which element is there, -1 behind the last number inside
+  int32_t* sorted;      // [count]: the numbers, `keys` for those outside
+  void* workspace;      // rfast_sort_bytes, 256-byte aligned
+};
+size_t rfast_sort_bytes(int32_t count, int32_t keys);
+hipError_t rfast_sort(const RfastSort& s, hipStream_t stream);
+
+inline bool rfast_type_ok(int32_t t) { return t == RFAST_F32 || t == RFAST_BF16; }
+inline int rfast_type_bytes(int32_t t) { return t == RFAST_F32 ? 4 : 2; }
+inline dim3 rfast_grid_of(int64_t blocks) {  // a dimension of a launch has fewer than 2^32 lanes
+  const int64_t x = blocks < 1 << 21 ? blocks : 1 << 21;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
 typedef unsigned short u16;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -87,6 +107,45 @@ template <bool STREAM> __device__ inline void store_four(u16* p, int64_t left, c
   } else {
     for (int j = 0; j < 4; ++j)
       if (j < left) p[j] = to_bf16(v[j]);
+  }
+}
+
+// Eight neighbours, as above.
+template <bool STREAM> __device__ inline void load_eight(const u16* p, int64_t left, float* v) {
+  if (left >= 8) {
+    const any_u32x4 t = wide_load<any_u32x4, STREAM>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[2 * j] = __uint_as_float(t[j] << 16), v[2 * j + 1] = __uint_as_float(t[j] & 0xFFFF0000u);
+  } else {
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? from_bf16(p[j]) : 0.f;
+  }
+}
+template <bool STREAM> __device__ inline void load_eight(const float* p, int64_t left, float* v) {
+  if (left >= 8) {
+    const any_f32x4 a = wide_load<any_f32x4, STREAM>(p), b = wide_load<any_f32x4, STREAM>(p + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+  } else {
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? p[j] : 0.f;
+  }
+}
+template <bool STREAM> __device__ inline void store_eight(u16* p, int64_t left, const float* v) {
+  if (left >= 8) {
+    const any_u32x4 t = {to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3]), to_bf16_pair(v[4], v[5]), to_bf16_pair(v[6], v[7])};
+    wide_store<any_u32x4, STREAM>(p, t);
+  } else {
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[j] = to_bf16(v[j]);
+  }
+}
+template <bool STREAM> __device__ inline void store_eight(float* p, int64_t left, const float* v) {
+  if (left >= 8) {
+    const any_f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    wide_store<any_f32x4, STREAM>(p, a);
+    wide_store<any_f32x4, STREAM>(p + 4, b);
+  } else {
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[j] = v[j];
   }
 }
 

@@ -1,0 +1,472 @@
+// Rows sent to experts and back.
+//
+//   choice     the k largest logits of a row; w_j = exp(l_j) / sum, over the choices or over all experts
+//   dispatch   X[place_tj] = x_t                      its gradient: dx_t = sum_j dX[place_tj]
+//   return     y_t = sum_j w_tj R[place_tj]           its gradient: dR[place_tj] = w_tj dy_t, dw_tj = <R[place_tj], dy_t>
+//   router     dl_e = sum_j [e = e_j] w_j dw_j - p_e sum_j w_j dw_j
+//
+// All but the choice move rows and compute one or two operations per element: memory bounds them.  Work goes by the unsorted row t, of which k
+// sorted rows are written or read, so that every byte is moved once: the dispatch reads x_t once for all k copies.
+#include <type_traits>
+
+#include "rfast_operators.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChoicesMost = 64, kExpertsMost = 1024;
+constexpr int kColumnsMost = 0x7ffffc00;  // columns of whole slabs stay within 32 bits
+
+__device__ inline int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+__device__ inline float wide(float f) { return f; }
+__device__ inline float wide(u16 b) { return from_bf16(b); }
+__device__ inline void narrow(float* p, float f) { *p = f; }
+__device__ inline void narrow(u16* p, float f) { *p = to_bf16(f); }
+
+// ---------------------------------------------------------------------------------------------------------- the choice
+struct Choice {
+  const void* logits;
+  int32_t* expert;
+  float* weight;
+  int64_t ld;
+  int32_t rows, experts, k, normalise;
+};
+
+// Whole numbers in the order of the floats, equal for -0 and 0; 0 is below all of them.  NaN is the largest.
+__device__ inline uint32_t ordered(float f) {
+  if (f != f) return 0xFFFFFFFFu;
+  const uint32_t u = __float_as_uint(f + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+constexpr uint32_t kMasked = 0x007FFFFFu;  // ordered(-infinity)
+__device__ inline float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+
+template <int LANES, class T, class F> __device__ inline T lanes_reduce(T v, F f) {
+#pragma unroll
+  for (int d = 1; d < LANES; d <<= 1) v = f(v, (T)__shfl_xor(v, d, 64));
+  return v;
+}
+
+// LANES lanes hold a row, HOLD neighbouring experts each; the largest is taken out k times.  Lane j keeps choice j.
+template <class IN, int LANES, int HOLD> __global__ void __launch_bounds__(kThreads) rfast_route_choice(Choice a) {
+  const int64_t row = (block_number() * kThreads + threadIdx.x) / LANES;
+  if (row >= a.rows) return;
+  const int lane = threadIdx.x % LANES, base = (threadIdx.x & 63) - lane;
+  const IN* l = (const IN*)a.logits + row * a.ld;
+  float logit[HOLD];
+  uint32_t o[HOLD];
+#pragma unroll
+  for (int j = 0; j < HOLD; ++j) {
+    const int e = lane * HOLD + j;
+    logit[j] = e < a.experts ? wide(l[e]) : -INFINITY;
+    o[j] = e < a.experts ? ordered(logit[j]) : 0u;
+  }
+  int32_t expert = -1;
+  float mine = -INFINITY, top = -INFINITY;
+  for (int j = 0; j < a.k; ++j) {
+    uint32_t m = o[0];
+#pragma unroll
+    for (int i = 1; i < HOLD; ++i) m = max(m, o[i]);
+    const uint32_t most = lanes_reduce<LANES>(m, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    if (j == 0) top = value_of(most);
+    uint64_t have = __ballot(m == most) >> base;
+    if (LANES < 64) have &= (1ull << (LANES & 63)) - 1;
+    const int winner = __ffsll((unsigned long long)have) - 1;  // of equal ones the lowest: a lane's experts are neighbours
+    int at = 0;
+#pragma unroll
+    for (int i = HOLD - 1; i >= 0; --i) at = o[i] == most ? i : at;
+    const int32_t chosen = __shfl(lane * HOLD + at, base + winner, 64);
+    if (lane == winner) {
+#pragma unroll
+      for (int i = 0; i < HOLD; ++i) o[i] = i == at ? 0u : o[i];
+    }
+    if (lane == j && most > kMasked) expert = chosen, mine = value_of(most);
+  }
+  const float shift = top == -INFINITY ? 0.f : top;
+  float e = expert >= 0 ? expf(mine - shift) : 0.f, part = e;
+  if (!a.normalise) {
+    part = 0.f;
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j) part += expf(logit[j] - shift);
+  }
+  const float total = lanes_reduce<LANES>(part, [](float x, float y) { return x + y; });
+  if (lane < a.k) {
+    a.expert[row * a.k + lane] = expert;
+    a.weight[row * a.k + lane] = expert >= 0 ? e / total : 0.f;
+  }
+}
+
+template <class IN> hipError_t launch_choice(const Choice& a, hipStream_t s) {
+  const auto go = [&](auto lanes, auto hold) {
+    constexpr int L = decltype(lanes)::value, H = decltype(hold)::value;
+    hipLaunchKernelGGL((rfast_route_choice<IN, L, H>), rfast_grid_of(((int64_t)a.rows * L + kThreads - 1) / kThreads), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+#define RFAST_TRY(L, H) \
+  if (a.experts <= L * H && a.k <= L) return go(integral_constant<int, L>(), integral_constant<int, H>())
+  RFAST_TRY(8, 1);
+  RFAST_TRY(8, 2);
+  RFAST_TRY(8, 4);
+  RFAST_TRY(16, 4);
+  RFAST_TRY(32, 4);
+  RFAST_TRY(64, 4);
+  RFAST_TRY(64, 8);
+  RFAST_TRY(64, 16);
+#undef RFAST_TRY
+  return hipErrorInvalidValue;
+}
+
+struct ChoiceBack {
+  const void* logits;
+  const int32_t* expert;
+  const float *weight, *dweight;
+  void* dlogits;
+  int64_t ld, ld_out;
+  int32_t rows, experts, k, normalise;
+};
+
+// A wavefront per row; lane j has choice j, and the experts go by 64.
+template <class IN, class OUT> __global__ void __launch_bounds__(kThreads) rfast_route_choice_back(ChoiceBack a) {
+  const int64_t row = (block_number() * kThreads + threadIdx.x) / 64;
+  if (row >= a.rows) return;
+  const int lane = threadIdx.x & 63;
+  int32_t expert = -1;
+  float w = 0.f, wd = 0.f;
+  if (lane < a.k) {
+    expert = a.expert[row * a.k + lane];
+    if ((uint32_t)expert < (uint32_t)a.experts) {
+      w = a.weight[row * a.k + lane];
+      wd = w * a.dweight[row * a.k + lane];
+    } else {
+      expert = -1;
+    }
+  }
+  const auto add = [](float x, float y) { return x + y; };
+  const float mean = wave_reduce(wd, add);
+  const IN* l = (const IN*)a.logits + row * a.ld;
+  float shift = 0.f, total = 1.f;
+  if (!a.normalise) {
+    float top = -INFINITY, sum = 0.f;
+    for (int e = lane; e < a.experts; e += 64) top = fmaxf(top, wide(l[e]));
+    top = wave_max(top);
+    shift = top == -INFINITY ? 0.f : top;
+    for (int e = lane; e < a.experts; e += 64) sum += expf(wide(l[e]) - shift);
+    total = wave_reduce(sum, add);
+    if (total == 0.f) total = 1.f;  // (a row of masked experts)
+  }
+  OUT* out = (OUT*)a.dlogits + row * a.ld_out;
+  for (int first = 0; first < a.experts; first += 64) {
+    const int e = first + lane;
+    float g = a.normalise || e >= a.experts ? 0.f : -mean * (expf(wide(l[e]) - shift) / total);
+    for (int j = 0; j < a.k; ++j) {
+      const int32_t chosen = __shfl(expert, j, 64);
+      const float add_j = __shfl(a.normalise ? wd - w * mean : wd, j, 64);
+      g += chosen == e ? add_j : 0.f;
+    }
+    if (e < a.experts) narrow(out + e, g);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ the rows
+struct Rows {
+  const void* in;       // gather: x; combine: sorted
+  const int32_t* place;
+  const float* weight;
+  const void* dy;
+  void* out;
+  float* dweight;
+  int64_t ld_in, ld_dy, ld_out;
+  int32_t rows, k, d, sorted_rows;
+};
+
+// Columns of 16 bytes; LANES lanes per row and slab.  Units of 2 bytes, whatever the type.
+template <int LANES> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
+  const int64_t unit = (block_number() * kThreads + threadIdx.x) / LANES;
+  const int64_t row = unit / slabs;
+  if (row >= a.rows) return;
+  const int64_t col = ((unit % slabs) * LANES + threadIdx.x % LANES) * 8;
+  if (col >= a.d) return;
+  const u16* x = (const u16*)a.in + row * a.ld_in + col;
+  const int left = (int)min((int64_t)8, a.d - col);
+  any_u32x4 v = {};
+  u16 tail[8];
+  if (left == 8) v = *(const any_u32x4*)x;
+  else
+    for (int j = 0; j < 8; ++j) tail[j] = j < left ? x[j] : 0;
+  const int32_t* place = a.place + row * a.k;
+  for (int j = 0; j < a.k; ++j) {
+    const int32_t to = place[j];
+    if ((uint32_t)to >= (uint32_t)a.sorted_rows) continue;
+    u16* out = (u16*)a.out + to * a.ld_out + col;
+    if (left == 8) *(any_u32x4*)out = v;
+    else
+      for (int i = 0; i < 8; ++i)
+        if (i < left) out[i] = tail[i];
+  }
+}
+
+template <class IN, class OUT, int LANES> __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, int slabs) {
+  const int64_t unit = (block_number() * kThreads + threadIdx.x) / LANES;
+  const int64_t row = unit / slabs;
+  if (row >= a.rows) return;
+  const int col = ((int)(unit % slabs) * LANES + threadIdx.x % LANES) * 8;
+  if (col >= a.d) return;
+  const int32_t* place = a.place + row * a.k;
+  const float* weight = a.weight ? a.weight + row * a.k : nullptr;
+  float y[8] = {};
+#pragma unroll 4
+  for (int j = 0; j < a.k; ++j) {
+    const int32_t from = place[j];
+    if ((uint32_t)from >= (uint32_t)a.sorted_rows) continue;
+    const float w = weight ? weight[j] : 1.f;
+    float v[8];
+    load_eight<false>((const IN*)a.in + from * a.ld_in + col, a.d - col, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += w * v[i];
+  }
+  store_eight<false>((OUT*)a.out + row * a.ld_out + col, a.d - col, y);
+}
+
+// A workgroup of WAVES wavefronts per row: every choice's product with dy is a sum over the workgroup.
+template <class T, int WAVES> __global__ void __launch_bounds__(64 * WAVES) rfast_route_combine_back(Rows a) {
+  __shared__ float box[kChoicesMost][WAVES];
+  const int64_t row = block_number();
+  if (row >= a.rows) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const T* dy = (const T*)a.dy + row * a.ld_dy;
+  for (int j = 0; j < a.k; ++j) {
+    const int32_t at = a.place[row * a.k + j];
+    float dot = 0.f;
+    if ((uint32_t)at < (uint32_t)a.sorted_rows) {
+      const float w = a.weight ? a.weight[row * a.k + j] : 1.f;
+      for (int64_t col = threadIdx.x * 8; col < a.d; col += 64 * WAVES * 8) {
+        float g[8];
+        load_eight<false>(dy + col, a.d - col, g);
+        if (a.dweight) {
+          float v[8];
+          load_eight<false>((const T*)a.in + at * a.ld_in + col, a.d - col, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) dot += v[i] * g[i];
+        }
+        if (a.out) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[i] *= w;
+          store_eight<false>((T*)a.out + at * a.ld_out + col, a.d - col, g);
+        }
+      }
+    }
+    if (a.dweight) {
+      dot = wave_reduce(dot, [](float x, float y) { return x + y; });
+      if (lane == 0) box[j][wave] = dot;
+    }
+  }
+  if (!a.dweight) return;
+  __syncthreads();
+  if (threadIdx.x < a.k) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += box[threadIdx.x][w];
+    a.dweight[row * a.k + threadIdx.x] = sum;
+  }
+}
+
+// Lanes per row of `columns` columns, eight of them each.
+template <class F> hipError_t by_lanes(int64_t columns, F go) {
+  using std::integral_constant;
+  if (columns <= 64) return go(integral_constant<int, 8>());
+  if (columns <= 128) return go(integral_constant<int, 16>());
+  if (columns <= 256) return go(integral_constant<int, 32>());
+  return go(integral_constant<int, 64>());
+}
+
+RfastArea area(const void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) { return {p, rows, ld * bytes, columns * bytes}; }
+RfastArea area(const void* p, int64_t count) { return {p, 1, count * 4, count * 4}; }
+
+bool counts_ok(int32_t rows, int32_t k, int32_t d, int32_t sorted_rows) {
+  return rows >= 0 && k >= 1 && k <= kChoicesMost && d >= 1 && d <= kColumnsMost && sorted_rows >= 0 && (int64_t)rows * k <= 0x7fffffff;
+}
+const char* const kCounts = "need rows, sorted_rows >= 0, k 1 .. 64, d 1 .. 2^31 - 1024 and rows k < 2^31";
+const char* const kTypes = "types must be RFAST_F32 or RFAST_BF16";
+const char* const kAddress = "an address is no multiple of its element's size";
+const char* const kApart = "rows are at least as far apart as they are long";
+const char* const kNull = "NULL argument";
+
+int plan(int32_t pairs, int32_t experts, const int32_t* expert, int32_t* row_ptr, int32_t* place, int32_t* order, void* workspace,
+         hipStream_t s) {
+  const hipError_t e = rfast_sort({pairs, experts, expert, row_ptr, place, order, nullptr, workspace}, s);
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "sort launch");
+}
+
+// Of outputs of whole numbers and the workspace, none may overlap another or an input.
+int apart(const RfastArea* in, int n_in, const RfastArea* out, int n_out) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (rfast_overlap(out[i], in[j])) return rfast_refuse(RFAST_EINVAL, "an output or the workspace overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (rfast_overlap(out[i], out[j])) return rfast_refuse(RFAST_EINVAL, "outputs or the workspace overlap");
+  }
+  return RFAST_OK;
+}
+
+}  // namespace
+
+extern "C" size_t rfast_route_workspace_bytes(int32_t pairs, int32_t experts) {
+  return pairs >= 0 && experts >= 1 ? rfast_sort_bytes(pairs, experts) : 0;
+}
+
+extern "C" int rfast_route_plan(int32_t pairs, int32_t experts, const int32_t* expert, int32_t* row_ptr, int32_t* place, int32_t* order,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (pairs < 0 || experts < 1) return rfast_refuse(RFAST_EINVAL, "need pairs >= 0 and experts >= 1");
+  if (!row_ptr || (pairs && (!expert || !place || !order))) return rfast_refuse(RFAST_EINVAL, kNull);
+  if ((uintptr_t)row_ptr % 4 || (uintptr_t)expert % 4 || (uintptr_t)place % 4 || (uintptr_t)order % 4) return rfast_refuse(RFAST_EINVAL, kAddress);
+  const size_t need = rfast_route_workspace_bytes(pairs, experts);
+  if (!workspace || (uintptr_t)workspace % 256) return rfast_refuse(RFAST_EINVAL, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < need) return rfast_refuse(RFAST_ENOMEM, "workspace too small: need " + std::to_string(need) + " bytes");
+  const RfastArea in[] = {area(expert, pairs)},
+                  out[] = {area(row_ptr, (int64_t)experts + 1), area(place, pairs), area(order, pairs), {workspace, 1, (int64_t)need, (int64_t)need}};
+  if (const int bad = apart(in, pairs ? 1 : 0, out, 4)) return bad;
+  return plan(pairs, experts, expert, row_ptr, place, order, workspace, (hipStream_t)hip_stream);
+}
+
+extern "C" int rfast_route(int32_t rows, int32_t experts, int32_t k, const void* logits, int32_t logits_type, int64_t ld_logits,
+                           int32_t normalise, int32_t* expert, float* weight, int32_t* row_ptr, int32_t* place, int32_t* order,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (rows < 0 || experts < 1 || experts > kExpertsMost || k < 1 || k > kChoicesMost || k > experts || (int64_t)rows * k > 0x7fffffff)
+    return rfast_refuse(RFAST_EINVAL, "need rows >= 0, experts 1 .. 1024, k 1 .. min(experts, 64) and rows k < 2^31");
+  if (!rfast_type_ok(logits_type)) return rfast_refuse(RFAST_EINVAL, kTypes);
+  if (normalise != 0 && normalise != 1) return rfast_refuse(RFAST_EINVAL, "normalise must be 0 or 1");
+  if (!row_ptr || (rows && (!logits || !expert || !weight || !place || !order))) return rfast_refuse(RFAST_EINVAL, kNull);
+  if (rows && ld_logits < experts) return rfast_refuse(RFAST_EINVAL, kApart);
+  const int lw = rfast_type_bytes(logits_type), pairs = rows * k;
+  if ((rows && ((uintptr_t)logits % lw || (uintptr_t)expert % 4 || (uintptr_t)weight % 4 || (uintptr_t)place % 4 || (uintptr_t)order % 4)) ||
+      (uintptr_t)row_ptr % 4)
+    return rfast_refuse(RFAST_EINVAL, kAddress);
+  const size_t need = rfast_route_workspace_bytes(pairs, experts);
+  if (!workspace || (uintptr_t)workspace % 256) return rfast_refuse(RFAST_EINVAL, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < need) return rfast_refuse(RFAST_ENOMEM, "workspace too small: need " + std::to_string(need) + " bytes");
+  const RfastArea in[] = {area(logits, rows, ld_logits, experts, lw)},
+                  out[] = {area(row_ptr, (int64_t)experts + 1), {workspace, 1, (int64_t)need, (int64_t)need}, area(expert, pairs), area(weight, pairs),
+                           area(place, pairs), area(order, pairs)};
+  if (const int bad = apart(in, rows ? 1 : 0, out, rows ? 6 : 2)) return bad;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  if (rows) {
+    const Choice a = {logits, expert, weight, ld_logits, rows, experts, k, normalise};
+    const hipError_t e = logits_type == RFAST_F32 ? launch_choice<float>(a, s) : launch_choice<u16>(a, s);
+    if (e != hipSuccess) return rfast_refuse_hip(e, "router launch");
+  }
+  return plan(pairs, experts, expert, row_ptr, place, order, workspace, s);
+}
+
+extern "C" int rfast_route_backward(int32_t rows, int32_t experts, int32_t k, const void* logits, int32_t logits_type, int64_t ld_logits,
+                                    int32_t normalise, const int32_t* expert, const float* weight, const float* dweight, void* dlogits,
+                                    int32_t dlogits_type, int64_t ld_dlogits, void* hip_stream) {
+  if (rows < 0 || experts < 1 || experts > kExpertsMost || k < 1 || k > kChoicesMost || k > experts || (int64_t)rows * k > 0x7fffffff)
+    return rfast_refuse(RFAST_EINVAL, "need rows >= 0, experts 1 .. 1024, k 1 .. min(experts, 64) and rows k < 2^31");
+  if (!rfast_type_ok(dlogits_type) || (!normalise && !rfast_type_ok(logits_type))) return rfast_refuse(RFAST_EINVAL, kTypes);
+  if (normalise != 0 && normalise != 1) return rfast_refuse(RFAST_EINVAL, "normalise must be 0 or 1");
+  if (rows == 0) return RFAST_OK;
+  if (!expert || !weight || !dweight || !dlogits || (!normalise && !logits)) return rfast_refuse(RFAST_EINVAL, kNull);
+  if (ld_dlogits < experts || (!normalise && ld_logits < experts)) return rfast_refuse(RFAST_EINVAL, kApart);
+  const int lw = normalise ? 4 : rfast_type_bytes(logits_type), ow = rfast_type_bytes(dlogits_type);
+  if ((!normalise && (uintptr_t)logits % lw) || (uintptr_t)dlogits % ow || (uintptr_t)expert % 4 || (uintptr_t)weight % 4 || (uintptr_t)dweight % 4)
+    return rfast_refuse(RFAST_EINVAL, kAddress);
+  const int64_t pairs = (int64_t)rows * k;
+  const RfastArea in[] = {area(expert, pairs), area(weight, pairs), area(dweight, pairs), area(logits, rows, ld_logits, experts, lw)},
+                  out[] = {area(dlogits, rows, ld_dlogits, experts, ow)};
+  if (const int bad = apart(in, normalise ? 3 : 4, out, 1)) return bad;
+  const ChoiceBack a = {logits, expert, weight, dweight, dlogits, ld_logits, ld_dlogits, rows, experts, k, normalise};
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const dim3 grid = rfast_grid_of(((int64_t)rows + 3) / 4);
+  const bool lf = logits_type == RFAST_F32, of = dlogits_type == RFAST_F32;
+  if (lf && of) hipLaunchKernelGGL((rfast_route_choice_back<float, float>), grid, dim3(kThreads), 0, s, a);
+  else if (lf) hipLaunchKernelGGL((rfast_route_choice_back<float, u16>), grid, dim3(kThreads), 0, s, a);
+  else if (of) hipLaunchKernelGGL((rfast_route_choice_back<u16, float>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((rfast_route_choice_back<u16, u16>), grid, dim3(kThreads), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "router gradient launch");
+}
+
+extern "C" int rfast_route_gather(int32_t rows, int32_t k, int32_t d, const void* x, int32_t type, int64_t ld_x, const int32_t* place, void* sorted,
+                                  int32_t sorted_rows, int64_t ld_sorted, void* hip_stream) {
+  if (!counts_ok(rows, k, d, sorted_rows)) return rfast_refuse(RFAST_EINVAL, kCounts);
+  if (!rfast_type_ok(type)) return rfast_refuse(RFAST_EINVAL, kTypes);
+  if (rows == 0 || sorted_rows == 0) return RFAST_OK;
+  if (!x || !place || !sorted) return rfast_refuse(RFAST_EINVAL, kNull);
+  if (ld_x < d || ld_sorted < d) return rfast_refuse(RFAST_EINVAL, kApart);
+  const int w = rfast_type_bytes(type);
+  if ((uintptr_t)x % w || (uintptr_t)sorted % w || (uintptr_t)place % 4) return rfast_refuse(RFAST_EINVAL, kAddress);
+  const RfastArea in[] = {area(x, rows, ld_x, d, w), area(place, (int64_t)rows * k)}, out[] = {area(sorted, sorted_rows, ld_sorted, d, w)};
+  if (const int bad = apart(in, 2, out, 1)) return bad;
+  const int64_t half = w / 2, columns = d * half;
+  if (columns > kColumnsMost) return rfast_refuse(RFAST_EINVAL, "rows of nearly 2^32 bytes or more");
+  const Rows a = {x, place, nullptr, nullptr, sorted, nullptr, ld_x * half, 0, ld_sorted * half, rows, k, (int32_t)columns, sorted_rows};
+  const hipError_t e = by_lanes(columns, [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    const int slabs = (int)((columns + 511) / 512);
+    hipLaunchKernelGGL((rfast_route_gather_kernel<L>), rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0,
+                       (hipStream_t)hip_stream, a, slabs);
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "dispatch launch");
+}
+
+extern "C" int rfast_route_combine(int32_t rows, int32_t k, int32_t d, const void* sorted, int32_t type, int32_t sorted_rows, int64_t ld_sorted,
+                                   const int32_t* place, const float* weight, void* y, int32_t y_type, int64_t ld_y, void* hip_stream) {
+  if (!counts_ok(rows, k, d, sorted_rows)) return rfast_refuse(RFAST_EINVAL, kCounts);
+  if (!rfast_type_ok(type) || !rfast_type_ok(y_type)) return rfast_refuse(RFAST_EINVAL, kTypes);
+  if (rows == 0) return RFAST_OK;
+  if ((sorted_rows && !sorted) || !place || !y) return rfast_refuse(RFAST_EINVAL, kNull);
+  if ((sorted_rows && ld_sorted < d) || ld_y < d) return rfast_refuse(RFAST_EINVAL, kApart);
+  const int w = rfast_type_bytes(type), yw = rfast_type_bytes(y_type);
+  if ((uintptr_t)sorted % w || (uintptr_t)y % yw || (uintptr_t)place % 4 || (uintptr_t)weight % 4) return rfast_refuse(RFAST_EINVAL, kAddress);
+  const int64_t pairs = (int64_t)rows * k;
+  const RfastArea in[] = {area(sorted, sorted_rows, ld_sorted, d, w), area(place, pairs), area(weight, pairs)}, out[] = {area(y, rows, ld_y, d, yw)};
+  if (const int bad = apart(in, 3, out, 1)) return bad;
+  const Rows a = {sorted, place, weight, nullptr, y, nullptr, ld_sorted, 0, ld_y, rows, k, d, sorted_rows};
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const hipError_t e = by_lanes(d, [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    const int slabs = (int)(((int64_t)d + 511) / 512);
+    const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
+    const bool tf = type == RFAST_F32, yf = y_type == RFAST_F32;
+    if (tf && yf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
+    else if (tf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
+    else if (yf) hipLaunchKernelGGL((rfast_route_combine_kernel<u16, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
+    else hipLaunchKernelGGL((rfast_route_combine_kernel<u16, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return launch");
+}
+
+extern "C" int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, const void* sorted, int32_t type, int32_t sorted_rows,
+                                            int64_t ld_sorted, const int32_t* place, const float* weight, const void* dy, int64_t ld_dy,
+                                            void* dsorted, int64_t ld_dsorted, float* dweight, void* hip_stream) {
+  if (!counts_ok(rows, k, d, sorted_rows)) return rfast_refuse(RFAST_EINVAL, kCounts);
+  if (!rfast_type_ok(type)) return rfast_refuse(RFAST_EINVAL, kTypes);
+  if (rows == 0 || (!dsorted && !dweight)) return RFAST_OK;
+  const bool reads = dweight && sorted_rows, writes = dsorted && sorted_rows;
+  if ((reads && !sorted) || !place || !dy) return rfast_refuse(RFAST_EINVAL, kNull);
+  if ((reads && ld_sorted < d) || ld_dy < d || (writes && ld_dsorted < d)) return rfast_refuse(RFAST_EINVAL, kApart);
+  const int w = rfast_type_bytes(type);
+  if ((reads && (uintptr_t)sorted % w) || (uintptr_t)dy % w || (uintptr_t)dsorted % w || (uintptr_t)place % 4 || (uintptr_t)weight % 4 ||
+      (uintptr_t)dweight % 4)
+    return rfast_refuse(RFAST_EINVAL, kAddress);
+  const int64_t pairs = (int64_t)rows * k;
+  const RfastArea in[] = {area(place, pairs), area(weight, pairs), area(dy, rows, ld_dy, d, w), area(reads ? sorted : nullptr, sorted_rows, ld_sorted, d, w)},
+                  out[] = {area(dsorted, sorted_rows, ld_dsorted, d, w), area(dweight, pairs)};
+  if (const int bad = apart(in, 4, out, 2)) return bad;
+  const Rows a = {sorted, place, weight, dy, writes ? dsorted : nullptr, dweight, ld_sorted, ld_dy, ld_dsorted, rows, k, d, sorted_rows};
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const dim3 grid = rfast_grid_of(rows);
+  const bool f = type == RFAST_F32;
+  if (d <= 1024) {
+    if (f) hipLaunchKernelGGL((rfast_route_combine_back<float, 1>), grid, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((rfast_route_combine_back<u16, 1>), grid, dim3(64), 0, s, a);
+  } else {
+    if (f) hipLaunchKernelGGL((rfast_route_combine_back<float, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((rfast_route_combine_back<u16, 4>), grid, dim3(256), 0, s, a);
+  }
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return gradient launch");
+}

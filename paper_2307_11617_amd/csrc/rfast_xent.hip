@@ -1,6 +1,9 @@
-// Softmax cross-entropy of rows of logits with its gradient.
+// Softmax cross-entropy of rows of logits with its gradient, and the clipped loss of a policy.
 //
 //   lse = log sum exp l_k,  loss = lse - l_label,  grad_k = c (exp(l_k - lse) - [k == label])
+//
+// The policy's loss is a function of logp = l_label - lse and of the row's own numbers, so its gradient is the same with another c per row, and both
+// are one kernel.
 //
 // Some five operations per logit, so the bound is one read of the logits and one write of the gradient.  A row therefore stays in
 // registers between the two: of 8 to 64 lanes up to 1024 logits (2048 of bf16), of a workgroup of 256 to 1024 lanes beyond.  Rows longer than the registers
@@ -23,6 +26,24 @@ struct Args {
   int64_t ld_logits, ld_grad;
   int32_t rows, K;
   float scale;
+  // of a policy (`lse` is NULL)
+  const float* old;
+  const float* advantage;
+  const float* reference;
+  const float* weight;
+  float* logp;
+  float low, high, beta;  // low, high: the ratio's borders
+};
+
+// A row's numbers beside its logits.
+struct Row {
+  float old = 0.f, advantage = 0.f, reference = 0.f, weight = 1.f;
+  __device__ void load(const Args& a, int64_t row) {
+    old = a.old[row];
+    advantage = a.advantage[row];
+    if (a.reference) reference = a.reference[row];
+    if (a.weight) weight = a.weight[row];
+  }
 };
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
@@ -94,6 +115,30 @@ __device__ inline void finish_row(const Args& a, int64_t row, float shift, float
   if (a.loss) a.loss[row] = !counts || sum == 0.f ? 0.f : log_sum + (shift - own);
 }
 
+// Loss, logp and the gradient's factor of a policy's row.  expf and expm1f of the mathematical library: the ratio's error is that of logp.
+__device__ inline float finish_policy(const Args& a, const Row& r, int64_t row, float shift, float sum, bool counts, float own, bool writes) {
+  if (!counts || sum == 0.f) {
+    if (writes && a.loss) a.loss[row] = 0.f;
+    if (writes && a.logp) a.logp[row] = 0.f;
+    return 0.f;
+  }
+  const float logp = (own - shift) - kLn2 * __builtin_amdgcn_logf(sum);
+  const float ratio = logp == -INFINITY ? 0.f : expf(logp - r.old), A = r.advantage;
+  const bool cut = (A > 0.f && ratio > a.high) || (A < 0.f && ratio < a.low);
+  // (an infinite ratio with an advantage of zero counts for nothing)
+  const float gain = A == 0.f && ratio > 0.f ? 0.f : A * (cut ? (A > 0.f ? a.high : a.low) : ratio);
+  float loss = -gain, slope = cut ? 0.f : -gain;
+  if (a.reference && a.beta != 0.f) {
+    const float q = r.reference - logp, m = expm1f(q);
+    loss += a.beta * (isinf(q) && q > 0.f ? q : m - q);  // (inf - inf where the action is masked)
+    if (logp != -INFINITY) slope -= a.beta * m;
+  }
+  const bool nothing = r.weight == 0.f;
+  if (writes && a.loss) a.loss[row] = nothing ? 0.f : r.weight * loss;
+  if (writes && a.logp) a.logp[row] = logp;
+  return nothing ? 0.f : -a.scale * (r.weight * slope);
+}
+
 template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane, int lanes) {
   for (int64_t k = lane; k < K; k += lanes) grad[k] = (OUT)0;  // (the last step of a row of nearly 2^31 passes 32 bits)
 }
@@ -103,7 +148,7 @@ template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane,
 // overlap at the ends of a row: group h begins at 8 h - m, moved into [0, K - 8] (4 instead of 8 in 32 bits), where m is how far a row of
 // a workgroup's begins behind a multiple of 16 bytes, so that all but the first and last group are aligned (4096 rows of 50001: 184 us with
 // m = 0, 152 so).  What a group shares with the one before is left out of its sum, and its gradient is written twice alike.
-template <class IN, class OUT, int LANES, int GROUPS>
+template <class IN, class OUT, int LANES, int GROUPS, bool POLICY>
 __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 1) rfast_xent_kernel(Args a) {
   constexpr int N = Group<IN>::N, ROWS = LANES <= 64 ? 256 / LANES : 1, SPAN = LANES * N;
   __shared__ float box[2][16];
@@ -113,11 +158,14 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
   if (row >= a.rows || (a.d_rows && row >= *a.d_rows)) return;
   const IN* l = (const IN*)a.logits + row * a.ld_logits;
   OUT* grad = a.grad ? (OUT*)a.grad + row * a.ld_grad : nullptr;
+  Row r;
+  if constexpr (POLICY) r.load(a, row);
   const int label = a.labels[row], last = a.K - N;  // last: where the last group begins (below 0: a row shorter than a group)
   const int m = LANES > 64 ? (int)((uintptr_t)l / sizeof(IN) % N) : 0;
   const bool counts = label >= 0 && label < a.K;
   if (!counts && !a.lse) {
     if (lane == 0 && a.loss) a.loss[row] = 0.f;
+    if (POLICY && lane == 0 && a.logp) a.logp[row] = 0.f;
     if (grad) zero_row(grad, a.K, lane, LANES);
     return;
   }
@@ -159,13 +207,15 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
     }
   }
   sum = row_reduce<LANES>(sum, box[1], [](float x, float y) { return x + y; });
-  if (lane == 0) finish_row(a, row, shift, sum, counts, own);
+  float scale = a.scale;
+  if constexpr (POLICY) scale = finish_policy(a, r, row, shift, sum, counts, own, lane == 0);
+  else if (lane == 0) finish_row(a, row, shift, sum, counts, own);
   if (!grad) return;
-  if (!counts || sum == 0.f) {
+  if (!counts || sum == 0.f || r.weight == 0.f) {
     zero_row(grad, a.K, lane, LANES);
     return;
   }
-  const float c = a.scale / sum;
+  const float c = scale / sum;
   forget();
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q) {
@@ -175,7 +225,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
     for (int j = 0; j < N; ++j) g[j] = power(v[q].at(j), shift) * c;
     if ((unsigned)(label - at) < (unsigned)N) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) g[j] -= j == label - at ? a.scale : 0.f;
+      for (int j = 0; j < N; ++j) g[j] -= j == label - at ? scale : 0.f;
     }
     if (h * N - m >= a.K) continue;
     if (LANES > 8 || GROUPS > 1 || last >= 0) {
@@ -189,7 +239,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
 }
 
 // Rows that no workgroup's registers hold.
-template <class IN, class OUT>
+template <class IN, class OUT, bool POLICY>
 __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
   constexpr int N = Group<IN>::N, SPAN = 1024 * N;
   __shared__ float box[2][16];
@@ -197,10 +247,13 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
   if (row >= a.rows || (a.d_rows && row >= *a.d_rows)) return;
   const IN* l = (const IN*)a.logits + row * a.ld_logits;
   OUT* grad = a.grad ? (OUT*)a.grad + row * a.ld_grad : nullptr;
+  Row r;
+  if constexpr (POLICY) r.load(a, row);
   const int label = a.labels[row];
   const bool counts = label >= 0 && label < a.K;
   if (!counts && !a.lse) {
     if (threadIdx.x == 0 && a.loss) a.loss[row] = 0.f;
+    if (POLICY && threadIdx.x == 0 && a.logp) a.logp[row] = 0.f;
     if (grad) zero_row(grad, a.K, threadIdx.x, 1024);
     return;
   }
@@ -225,14 +278,16 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
   const float shift = shift_of(row_reduce<1024>(top, box[0], [](float x, float y) { return fmaxf(x, y); }));
   if (shift > top) sum *= power(top, shift);
   sum = row_reduce<1024>(sum, box[1], [](float x, float y) { return x + y; });
-  if (threadIdx.x == 0) finish_row(a, row, shift, sum, counts, own);
+  float scale = a.scale;
+  if constexpr (POLICY) scale = finish_policy(a, r, row, shift, sum, counts, own, threadIdx.x == 0);
+  else if (threadIdx.x == 0) finish_row(a, row, shift, sum, counts, own);
   if (!grad) return;
   // (where the gradient takes the logits' place, `own` has been read before any lane writes: the reductions are barriers)
-  if (!counts || sum == 0.f) {
+  if (!counts || sum == 0.f || r.weight == 0.f) {
     zero_row(grad, a.K, threadIdx.x, 1024);
     return;
   }
-  const float c = a.scale / sum;
+  const float c = scale / sum;
   for (int64_t k = first; k < a.K; k += SPAN) {
     Group<IN> v;
     const bool whole = k + N <= a.K;
@@ -240,7 +295,7 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
     else v.load(l + k, (int)(a.K - k));
     float g[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) g[j] = power(v.at(j), shift) * c - (k + j == label ? a.scale : 0.f);
+    for (int j = 0; j < N; ++j) g[j] = power(v.at(j), shift) * c - (k + j == label ? scale : 0.f);
     if (whole) {
       store_group<N>(grad + k, g);
     } else {
@@ -251,16 +306,11 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
   }
 }
 
-dim3 grid_of(int64_t blocks) {  // a dimension of a launch has fewer than 2^32 lanes
-  const int64_t x = blocks < 1 << 21 ? blocks : 1 << 21;
-  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
-}
-
-template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
+template <class IN, class OUT, bool POLICY> hipError_t launch(const Args& a, hipStream_t s) {
   constexpr int N = Group<IN>::N;
   const auto go = [&](auto lanes, auto groups) {
     constexpr int L = decltype(lanes)::value, G = decltype(groups)::value, rows = L <= 64 ? 256 / L : 1;
-    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G>), grid_of(((int64_t)a.rows + rows - 1) / rows), dim3(L <= 64 ? 256 : L), 0, s, a);
+    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G, POLICY>), rfast_grid_of(((int64_t)a.rows + rows - 1) / rows), dim3(L <= 64 ? 256 : L), 0, s, a);
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -285,34 +335,78 @@ template <class IN, class OUT> hipError_t launch(const Args& a, hipStream_t s) {
     RFAST_TRY(1024, 16);
   }
 #undef RFAST_TRY
-  hipLaunchKernelGGL((rfast_xent_long_kernel<IN, OUT>), grid_of(a.rows), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL((rfast_xent_long_kernel<IN, OUT, POLICY>), rfast_grid_of(a.rows), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
-bool type_ok(int32_t t) { return t == RFAST_F32 || t == RFAST_BF16; }
-
-}  // namespace
-
-extern "C" int rfast_softmax_xent(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits,
-                                  const int32_t* labels, float grad_scale, float* loss, float* lse, void* grad, int32_t grad_type,
-                                  int64_t ld_grad, const int32_t* d_rows, void* hip_stream) {
+// What both losses refuse of logits, labels and gradient.
+int check(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits, const int32_t* labels, void* grad,
+          int32_t grad_type, int64_t ld_grad, const int32_t* d_rows) {
   if (rows < 0 || K < 1) return rfast_refuse(RFAST_EINVAL, "need rows >= 0 and K >= 1");
-  if (!type_ok(logits_type) || (grad && !type_ok(grad_type))) return rfast_refuse(RFAST_EINVAL, "types must be RFAST_F32 or RFAST_BF16");
+  if (!rfast_type_ok(logits_type) || (grad && !rfast_type_ok(grad_type)))
+    return rfast_refuse(RFAST_EINVAL, "types must be RFAST_F32 or RFAST_BF16");
   if (rows == 0) return RFAST_OK;
   if (!logits || !labels) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   if (ld_logits < K || (grad && ld_grad < K)) return rfast_refuse(RFAST_EINVAL, "rows are at least K elements apart");
-  const int lw = logits_type == RFAST_F32 ? 4 : 2, gw = grad_type == RFAST_F32 ? 4 : 2;
-  if ((uintptr_t)logits % lw || (uintptr_t)labels % 4 || (uintptr_t)loss % 4 || (uintptr_t)lse % 4 || (grad && (uintptr_t)grad % gw) ||
-      (uintptr_t)d_rows % 4)
+  const int lw = rfast_type_bytes(logits_type), gw = rfast_type_bytes(grad_type);
+  if ((uintptr_t)logits % lw || (uintptr_t)labels % 4 || (grad && (uintptr_t)grad % gw) || (uintptr_t)d_rows % 4)
     return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");
   if (grad) {
     const RfastArea in = {logits, rows, ld_logits * lw, (int64_t)K * lw}, out = {grad, rows, ld_grad * gw, (int64_t)K * gw};
     if (rfast_overlap(in, out) && !(grad == logits && lw == gw && ld_logits == ld_grad))
       return rfast_refuse(RFAST_EINVAL, "the gradient overlaps the logits without being in their place");
   }
-  const Args a = {logits, labels, loss, lse, grad, d_rows, ld_logits, ld_grad, rows, K, grad_scale};
-  const hipStream_t s = (hipStream_t)hip_stream;
+  return RFAST_OK;
+}
+
+template <bool POLICY> int launch_types(const Args& a, int32_t logits_type, int32_t grad_type, hipStream_t s) {
   const bool lf = logits_type == RFAST_F32, gf = grad_type == RFAST_F32;
-  const hipError_t e = lf ? (gf ? launch<float, float>(a, s) : launch<float, u16>(a, s)) : (gf ? launch<u16, float>(a, s) : launch<u16, u16>(a, s));
-  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "cross-entropy launch");
+  const hipError_t e = lf ? (gf ? launch<float, float, POLICY>(a, s) : launch<float, u16, POLICY>(a, s))
+                          : (gf ? launch<u16, float, POLICY>(a, s) : launch<u16, u16, POLICY>(a, s));
+  return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, POLICY ? "policy loss launch" : "cross-entropy launch");
+}
+
+}  // namespace
+
+extern "C" int rfast_softmax_xent(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits,
+                                  const int32_t* labels, float grad_scale, float* loss, float* lse, void* grad, int32_t grad_type,
+                                  int64_t ld_grad, const int32_t* d_rows, void* hip_stream) {
+  const int bad = check(rows, K, logits, logits_type, ld_logits, labels, grad, grad_type, ld_grad, d_rows);
+  if (bad != RFAST_OK || rows == 0) return bad;
+  if ((uintptr_t)loss % 4 || (uintptr_t)lse % 4) return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");
+  Args a = {logits, labels, loss, lse, grad, d_rows, ld_logits, ld_grad, rows, K, grad_scale};
+  return launch_types<false>(a, logits_type, grad_type, (hipStream_t)hip_stream);
+}
+
+extern "C" int rfast_policy_loss(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits, const int32_t* actions,
+                                 const float* old_logp, const float* advantage, const float* reference, const float* weight,
+                                 float clip_low, float clip_high, float beta, float grad_scale, float* loss, float* logp, void* grad,
+                                 int32_t grad_type, int64_t ld_grad, const int32_t* d_rows, void* hip_stream) {
+  const int bad = check(rows, K, logits, logits_type, ld_logits, actions, grad, grad_type, ld_grad, d_rows);
+  if (bad != RFAST_OK) return bad;
+  if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f && clip_high < INFINITY && beta >= 0.f && beta < INFINITY))
+    return rfast_refuse(RFAST_ERANGE, "need 0 <= clip_low <= 1, clip_high >= 0 and beta >= 0, all finite");
+  if (rows == 0) return RFAST_OK;
+  if (!old_logp || !advantage) return rfast_refuse(RFAST_EINVAL, "NULL argument");
+  const void* in[] = {actions, old_logp, advantage, reference, weight, d_rows};
+  void* out[] = {loss, logp};
+  const int lw = rfast_type_bytes(logits_type), gw = rfast_type_bytes(grad_type);
+  const RfastArea l = {logits, rows, ld_logits * lw, (int64_t)K * lw}, g = {grad, rows, ld_grad * gw, (int64_t)K * gw};
+  const int64_t bytes = 4 * (int64_t)rows;
+  for (const void* p : in) {
+    if ((uintptr_t)p % 4) return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");
+    const RfastArea q = {p, 1, bytes, p == d_rows ? 4 : bytes};
+    if (rfast_overlap(g, q)) return rfast_refuse(RFAST_EINVAL, "the gradient overlaps an input");
+    for (void* o : out)
+      if (rfast_overlap({o, 1, bytes, bytes}, q)) return rfast_refuse(RFAST_EINVAL, "loss or logp overlaps an input");
+  }
+  for (void* o : out) {
+    const RfastArea q = {o, 1, bytes, bytes};
+    if ((uintptr_t)o % 4) return rfast_refuse(RFAST_EINVAL, "an address is no multiple of its element's size");
+    if (rfast_overlap(q, l) || rfast_overlap(q, g)) return rfast_refuse(RFAST_EINVAL, "loss or logp overlaps the logits or their gradient");
+  }
+  if (rfast_overlap({loss, 1, bytes, bytes}, {logp, 1, bytes, bytes})) return rfast_refuse(RFAST_EINVAL, "loss and logp overlap");
+  const Args a = {logits, actions, loss, nullptr, grad, d_rows, ld_logits, ld_grad, rows, K, grad_scale, old_logp, advantage, reference, weight,
+                  logp, 1.f - clip_low, 1.f + clip_high, beta};
+  return launch_types<true>(a, logits_type, grad_type, (hipStream_t)hip_stream);
 }

@@ -1,5 +1,5 @@
 """The operators that take tensors instead of a context (include/rfast.h, same names): low-rank adapters beside a shared
-projection, softmax cross-entropy with its gradient, and AdamW over many tensors.
+projection, rows sent to experts and back, token embeddings, softmax cross-entropy and the clipped policy loss with their gradients, and AdamW over many tensors.
 
 Every call runs on the current stream of its tensors' device and neither waits nor reads anything back, so that it can be captured
 into a graph.  Workspaces come from torch's allocator with each call: calls on different streams, and graphs, share none.
@@ -9,6 +9,7 @@ calls' own results."""
 from __future__ import annotations
 
 import ctypes as C
+from typing import Any, NamedTuple
 
 import numpy as np
 
@@ -111,6 +112,230 @@ def rfast_softmax_xent(logits, labels, grad_scale=1.0, grad_dtype=None, grad=Non
     p_rows = None if rows is None else _vector(rows, "rows", 1, torch.int32, dev)
     _call(dev, lib().rfast_softmax_xent, T, K, logits.data_ptr(), lt, ld, p_labels, grad_scale, p_loss, p_lse, p_grad, gt, ldg, p_rows)
     return loss, grad
+
+
+def rfast_policy_loss(logits, actions, old_logp, advantage, reference=None, weight=None, clip=(0.2, 0.2), beta=0.0, grad_scale=1.0,
+                      grad_dtype=None, grad=None, loss=None, logp=None, rows=None):
+    """(loss, grad) of the clipped policy loss of rows of logits [T][K] (float32 or bfloat16): actions int32 [T] (outside [0, K): padding);
+    old_logp, advantage and, where given, reference and weight float32 [T].  With r = exp(logp - old_logp) a row's loss is
+    weight (-min(r advantage, clip(r, 1 - clip[0], 1 + clip[1]) advantage) + beta (exp(q) - q - 1)), q = reference - logp (no second term without
+    one), grad its derivative by the logits times grad_scale.  grad_dtype, grad, loss, rows: as in rfast_softmax_xent.  logp: float32 [T] to receive
+    log probabilities of the actions."""
+    torch = _t()
+    f32 = torch.float32
+    if logits.dim() != 2 or not logits.is_cuda or logits.shape[1] < 1:
+        raise RFastError(-1, "logits: need a matrix on the GPU with at least one class")
+    T, K = logits.shape
+    _sizes(T, K)
+    dev = logits.device
+    ld, lt = _matrix(logits, "logits", T, K, None, dev), _type(logits, "logits")
+    given = (_vector(actions, "actions", T, torch.int32, dev), _vector(old_logp, "old_logp", T, f32, dev), _vector(advantage, "advantage", T, f32, dev),
+             None if reference is None else _vector(reference, "reference", T, f32, dev),
+             None if weight is None else _vector(weight, "weight", T, f32, dev))
+    loss = torch.empty(T, dtype=f32, device=dev) if loss is None else loss
+    p_loss = _vector(loss, "loss", T, f32, dev)
+    p_logp = None if logp is None else _vector(logp, "logp", T, f32, dev)
+    if grad is None:
+        grad = torch.empty((T, K), dtype=grad_dtype or logits.dtype, device=dev)
+        ldg, gt, p_grad = K, _type(grad, "grad"), grad.data_ptr()
+    elif grad is False:
+        grad, p_grad, gt, ldg = None, None, F32, 0
+    else:
+        _need(grad_dtype is None or grad.dtype == grad_dtype, "grad: its type is not grad_dtype")
+        ldg, gt, p_grad = _matrix(grad, "grad", T, K, None, dev), _type(grad, "grad"), grad.data_ptr()
+    p_rows = None if rows is None else _vector(rows, "rows", 1, torch.int32, dev)
+    _call(dev, lib().rfast_policy_loss, T, K, logits.data_ptr(), lt, ld, *given, clip[0], clip[1], beta, grad_scale, p_loss, p_logp, p_grad, gt, ldg,
+          p_rows)
+    return loss, grad
+
+
+# ------------------------------------------------------------------------------------------------------- embeddings
+def rfast_embedding(table, tokens, scale=1.0, out=None, out_dtype=None):
+    """Rows scale table[token] of a table [V][d] (float32 or bfloat16), tokens int32 [T] (outside [0, V): padding, a row of zeros), in out_dtype
+    (default: the table's)."""
+    torch = _t()
+    _need(table.dim() == 2 and table.is_cuda, "table: need a matrix on the GPU")
+    (V, d), T, dev = table.shape, tokens.numel(), table.device
+    _sizes(T, V, d)
+    ld = _matrix(table, "table", V, d, None, dev)
+    if out is None:
+        out, ld_out = torch.empty((T, d), dtype=out_dtype or table.dtype, device=dev), max(d, 1)
+    else:
+        _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
+        ld_out = _matrix(out, "out", T, d, None, dev)
+    _call(dev, lib().rfast_embedding, T, V, d, table.data_ptr(), _type(table, "table"), ld, _vector(tokens, "tokens", T, torch.int32, dev), scale,
+          out.data_ptr(), _type(out, "out"), ld_out)
+    return out
+
+
+def rfast_embedding_backward_workspace_bytes(rows, vocabulary, d):
+    _sizes(rows, vocabulary, d)
+    return int(lib().rfast_embedding_backward_workspace_bytes(rows, vocabulary, d))
+
+
+def rfast_embedding_backward(dy, tokens, vocabulary, scale=1.0, grad=None, grad_dtype=None, accumulate=False):
+    """Gradient [vocabulary][d] of rfast_embedding's table for dy [T][d] (float32 or bfloat16), in grad_dtype (default float32): every row is
+    written, zeros where no token is.  accumulate: added to what `grad` holds, rows without a token stay as they are."""
+    torch = _t()
+    _need(dy.dim() == 2 and dy.is_cuda, "dy: need a matrix on the GPU")
+    (T, d), dev, V = dy.shape, dy.device, int(vocabulary)
+    _sizes(T, V, d)
+    ld = _matrix(dy, "dy", T, d, None, dev)
+    p_tokens = _vector(tokens, "tokens", T, torch.int32, dev)
+    if grad is None:
+        _need(not accumulate, "accumulate: need the gradient to add to")
+        _need(V >= 1, "need a vocabulary of at least one")
+        grad, ld_grad = torch.empty((V, d), dtype=grad_dtype or torch.float32, device=dev), max(d, 1)
+    else:
+        _need(grad_dtype is None or grad.dtype == grad_dtype, "grad: its type is not grad_dtype")
+        ld_grad = _matrix(grad, "grad", V, d, None, dev)
+    nbytes = rfast_embedding_backward_workspace_bytes(T, V, d)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, lib().rfast_embedding_backward, T, V, d, dy.data_ptr(), _type(dy, "dy"), ld, p_tokens, scale, grad.data_ptr(), _type(grad, "grad"),
+          ld_grad, 1 if accumulate else 0, ws.data_ptr(), nbytes)
+    return grad
+
+
+# ---------------------------------------------------------------------------------------- rows to experts and back
+class RFastRoute(NamedTuple):
+    """What a router decided for T rows: expert int32 [T][k] and weight float32 [T][k]; the pairs (row, choice) sorted by expert: row_ptr int32
+    [experts + 1], place int32 [T][k] (where a pair is, -1: nowhere) and order int32 [T k] (which pair is there)."""
+    expert: Any
+    weight: Any
+    row_ptr: Any
+    place: Any
+    order: Any
+
+
+def rfast_route_workspace_bytes(pairs, experts):
+    _sizes(pairs, experts)
+    return int(lib().rfast_route_workspace_bytes(pairs, experts))
+
+
+def rfast_route(logits, k, normalise=True):
+    """The k experts of every row of logits [T][experts] (float32 or bfloat16; at most 1024 experts, k at most 64) with the largest logits (of equal
+    ones the lowest; masked ones, -infinity, never: expert -1, weight 0), their weights (exp(logit) over the sum of the chosen, or of all if
+    normalise is false), and the order of the pairs by expert."""
+    torch = _t()
+    _need(logits.dim() == 2 and logits.is_cuda, "logits: need a matrix on the GPU")
+    (T, E), dev, k = logits.shape, logits.device, int(k)
+    _need(1 <= k <= min(E, 64) and E <= 1024, "need 1 to 1024 experts and k from 1 to min(experts, 64)")
+    _sizes(T * k)
+    ld, lt = _matrix(logits, "logits", T, E, None, dev), _type(logits, "logits")
+    i32 = torch.int32
+    r = RFastRoute(torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=torch.float32, device=dev),
+                   torch.empty(E + 1, dtype=i32, device=dev), torch.empty((T, k), dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev))
+    nbytes = rfast_route_workspace_bytes(T * k, E)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, lib().rfast_route, T, E, k, logits.data_ptr(), lt, ld, 1 if normalise else 0, *[t.data_ptr() for t in r], ws.data_ptr(), nbytes)
+    return r
+
+
+def rfast_route_plan(expert, experts):
+    """(row_ptr, place, order) of experts (or adapters) chosen elsewhere: expert int32 of any shape, numbers outside [0, experts) go nowhere; place has
+    its shape."""
+    torch = _t()
+    P, dev, i32 = expert.numel(), expert.device, torch.int32
+    _need(expert.is_cuda, "expert: need a tensor on the GPU")
+    _sizes(P, experts)
+    _need(experts >= 1, "need at least one expert")
+    p_expert = _vector(expert, "expert", P, i32, dev)
+    row_ptr, place, order = (torch.empty(s, dtype=i32, device=dev) for s in (experts + 1, expert.shape, P))
+    nbytes = rfast_route_workspace_bytes(P, experts)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, lib().rfast_route_plan, P, experts, p_expert, row_ptr.data_ptr(), place.data_ptr(), order.data_ptr(), ws.data_ptr(), nbytes)
+    return row_ptr, place, order
+
+
+def rfast_route_backward(logits, expert, weight, dweight, normalise=True, dlogits=None, grad_dtype=None):
+    """Gradient [T][experts] of rfast_route's logits for dweight float32 [T][k]; expert and weight as it returned them; in grad_dtype (default: the
+    logits')."""
+    torch = _t()
+    _need(logits.dim() == 2 and logits.is_cuda and expert.dim() == 2, "need logits [rows][experts] on the GPU and expert [rows][k]")
+    (T, E), dev, k = logits.shape, logits.device, expert.shape[1]
+    _sizes(T, E, k)
+    ld, lt = _matrix(logits, "logits", T, E, None, dev), _type(logits, "logits")
+    given = (_vector(expert, "expert", T * k, torch.int32, dev), _vector(weight, "weight", T * k, torch.float32, dev),
+             _vector(dweight, "dweight", T * k, torch.float32, dev))
+    if dlogits is None:
+        dlogits, ld_out = torch.empty((T, E), dtype=grad_dtype or logits.dtype, device=dev), max(E, 1)
+    else:
+        _need(grad_dtype is None or dlogits.dtype == grad_dtype, "dlogits: its type is not grad_dtype")
+        ld_out = _matrix(dlogits, "dlogits", T, E, None, dev)
+    _call(dev, lib().rfast_route_backward, T, E, k, logits.data_ptr(), lt, ld, 1 if normalise else 0, *given, dlogits.data_ptr(),
+          _type(dlogits, "dlogits"), ld_out)
+    return dlogits
+
+
+def _pairs(place, dev):
+    _need(place.dim() == 2, "place: need a matrix [rows][k]")
+    T, k = place.shape
+    _sizes(T * k)
+    return T, k, _vector(place, "place", T * k, _torch.int32, dev)
+
+
+def rfast_route_gather(x, place, out=None):
+    """Rows sorted by expert, [T k][d]: row place[t][j] is x[t] (x [T][d], float32 or bfloat16).  Rows that are nobody's place are not written: they
+    stay as they are in `out` (whose rows may be any number; a place outside is none), and hold anything without one.  Its gradient is
+    rfast_route_combine(dout, place)."""
+    torch = _t()
+    _need(x.dim() == 2 and x.is_cuda, "x: need a matrix on the GPU")
+    (T, d), dev = x.shape, x.device
+    ld = _matrix(x, "x", T, d, None, dev)
+    rows, k, p_place = _pairs(place, dev)
+    _need(rows == T, "place: need one row per row of x")
+    if out is None:
+        out = torch.empty((T * k, d), dtype=x.dtype, device=dev)
+    _need(out.dim() == 2, "out: need a matrix")
+    P = out.shape[0]
+    _sizes(P, d)
+    ld_out = _matrix(out, "out", P, d, x.dtype, dev)
+    _call(dev, lib().rfast_route_gather, T, k, d, x.data_ptr(), _type(x, "x"), ld, p_place, out.data_ptr(), P, ld_out)
+    return out
+
+
+def rfast_route_combine(rows, place, weight=None, out=None, out_dtype=None):
+    """y [T][d], y[t] = sum over j of weight[t][j] rows[place[t][j]], of rows sorted by expert [P][d] (float32 or bfloat16); weight float32 [T][k] (None: 1); a
+    place outside [0, P) counts for nothing.  In out_dtype (default: the rows')."""
+    torch = _t()
+    _need(rows.dim() == 2 and rows.is_cuda, "rows: need a matrix on the GPU")
+    (P, d), dev = rows.shape, rows.device
+    _sizes(P, d)
+    ld = _matrix(rows, "rows", P, d, None, dev)
+    T, k, p_place = _pairs(place, dev)
+    p_weight = None if weight is None else _vector(weight, "weight", T * k, torch.float32, dev)
+    if out is None:
+        out, ld_out = torch.empty((T, d), dtype=out_dtype or rows.dtype, device=dev), max(d, 1)
+    else:
+        _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
+        ld_out = _matrix(out, "out", T, d, None, dev)
+    _call(dev, lib().rfast_route_combine, T, k, d, rows.data_ptr(), _type(rows, "rows"), P, ld, p_place, p_weight, out.data_ptr(), _type(out, "out"),
+          ld_out)
+    return out
+
+
+def rfast_route_combine_backward(rows, place, weight, dy, drows=None, dweight=None):
+    """(drows, dweight) of rfast_route_combine for dy [T][d] of the rows' type: drows [P][d] of that type (rows that are nobody's place are not written:
+    they stay as they are in `drows`, and hold anything without one), dweight float32 [T][k].  Either may be False: not wanted."""
+    torch = _t()
+    _need(rows.dim() == 2 and rows.is_cuda, "rows: need a matrix on the GPU")
+    (P, d), dev = rows.shape, rows.device
+    _sizes(P, d)
+    ld = _matrix(rows, "rows", P, d, None, dev)
+    T, k, p_place = _pairs(place, dev)
+    p_weight = None if weight is None else _vector(weight, "weight", T * k, torch.float32, dev)
+    ld_dy = _matrix(dy, "dy", T, d, rows.dtype, dev)
+    ld_out = d
+    if drows is None:
+        drows = torch.empty((P, d), dtype=rows.dtype, device=dev)
+    elif drows is not False:
+        ld_out = _matrix(drows, "drows", P, d, rows.dtype, dev)
+    if dweight is None:
+        dweight = torch.empty((T, k), dtype=torch.float32, device=dev)
+    p_dweight = None if dweight is False else _vector(dweight, "dweight", T * k, torch.float32, dev)
+    _call(dev, lib().rfast_route_combine_backward, T, k, d, rows.data_ptr(), _type(rows, "rows"), P, ld, p_place, p_weight, dy.data_ptr(), ld_dy,
+          None if drows is False else drows.data_ptr(), ld_out, p_dweight)
+    return (None if drows is False else drows), (None if dweight is False else dweight)
 
 
 def rfast_lora_workspace_bytes(shape, which):
