@@ -180,85 +180,139 @@ struct Rows {
   int32_t rows, k, d, sorted_rows;
 };
 
-// Columns of 16 bytes; LANES lanes per row and slab.  Units of 2 bytes, whatever the type.
-template <int LANES> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
+// Work on columns: LANES lanes take a row, eight neighbouring columns each, and rows of more than 512 columns are cut into slabs, a wavefront
+// each.  WHOLE (d >= 8): the last group of a row is moved back to end with it and shares columns with the one before, which both write alike, so that
+// every access is a whole one; else a row is a single group, element by element.
+struct Spot {
+  int64_t row;
+  int col;   // the group's first column
+  int left;  // its columns (WHOLE: 8)
+  bool in;
+};
+template <int LANES, bool WHOLE> __device__ inline Spot spot_of(int32_t rows, int32_t d, int slabs) {
   const int64_t unit = (block_number() * kThreads + threadIdx.x) / LANES;
-  const int64_t row = unit / slabs;
-  if (row >= a.rows) return;
-  const int64_t col = ((unit % slabs) * LANES + threadIdx.x % LANES) * 8;
-  if (col >= a.d) return;
-  const u16* x = (const u16*)a.in + row * a.ld_in + col;
-  const int left = (int)min((int64_t)8, a.d - col);
+  Spot s;
+  s.row = unit / slabs;
+  const int col = ((int)(unit - s.row * slabs) * LANES + threadIdx.x % LANES) * 8;
+  if constexpr (LANES == 64)  // (a wavefront's lanes have one row: what belongs to it is read once)
+    s.row = (int64_t)__builtin_amdgcn_readfirstlane((int)(s.row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)s.row);
+  s.in = s.row < rows && col < d;
+  s.col = WHOLE ? min(col, d - 8) : col;
+  s.left = WHOLE ? 8 : d - col;
+  return s;
+}
+
+// Units of 2 bytes, whatever the type.
+template <int LANES, bool WHOLE> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
+  const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
+  if (!s.in) return;
+  const u16* x = (const u16*)a.in + s.row * a.ld_in + s.col;
   any_u32x4 v = {};
-  u16 tail[8];
-  if (left == 8) v = *(const any_u32x4*)x;
+  u16 few[8];
+  if constexpr (WHOLE) v = *(const any_u32x4*)x;
   else
-    for (int j = 0; j < 8; ++j) tail[j] = j < left ? x[j] : 0;
-  const int32_t* place = a.place + row * a.k;
+    for (int j = 0; j < 8; ++j) few[j] = j < s.left ? x[j] : 0;
+  const int32_t* place = a.place + s.row * a.k;
   for (int j = 0; j < a.k; ++j) {
     const int32_t to = place[j];
     if ((uint32_t)to >= (uint32_t)a.sorted_rows) continue;
-    u16* out = (u16*)a.out + to * a.ld_out + col;
-    if (left == 8) *(any_u32x4*)out = v;
+    u16* out = (u16*)a.out + to * a.ld_out + s.col;
+    if constexpr (WHOLE) wide_store<any_u32x4, true>(out, v);
     else
       for (int i = 0; i < 8; ++i)
-        if (i < left) out[i] = tail[i];
+        if (i < s.left) out[i] = few[i];
   }
 }
 
-template <class IN, class OUT, int LANES> __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, int slabs) {
-  const int64_t unit = (block_number() * kThreads + threadIdx.x) / LANES;
-  const int64_t row = unit / slabs;
-  if (row >= a.rows) return;
-  const int col = ((int)(unit % slabs) * LANES + threadIdx.x % LANES) * 8;
-  if (col >= a.d) return;
-  const int32_t* place = a.place + row * a.k;
-  const float* weight = a.weight ? a.weight + row * a.k : nullptr;
+// AT_ONCE choices' rows are under way together; one without a place reads row 0 and counts for nothing.
+template <class IN, class OUT, int LANES, bool WHOLE, int AT_ONCE>
+__global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, int slabs) {
+  const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
+  if (!s.in) return;
+  const int32_t* place = a.place + s.row * a.k;
+  const float* weight = a.weight ? a.weight + s.row * a.k : nullptr;
   float y[8] = {};
-#pragma unroll 4
-  for (int j = 0; j < a.k; ++j) {
-    const int32_t from = place[j];
-    if ((uint32_t)from >= (uint32_t)a.sorted_rows) continue;
-    const float w = weight ? weight[j] : 1.f;
-    float v[8];
-    load_eight<false>((const IN*)a.in + from * a.ld_in + col, a.d - col, v);
+  if (a.sorted_rows > 0) {
+    for (int first = 0; first < a.k; first += AT_ONCE) {
+      float w[AT_ONCE], v[AT_ONCE][8];
+      bool live[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] += w * v[i];
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int j = min(first + i, a.k - 1);
+        const int32_t from = place[j];
+        live[i] = first + i < a.k && (uint32_t)from < (uint32_t)a.sorted_rows;
+        w[i] = weight ? weight[j] : 1.f;
+        load_eight<true>((const IN*)a.in + (live[i] ? from : 0) * a.ld_in + s.col, s.left, v[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) y[c] += live[i] ? w[i] * v[i][c] : 0.f;
+    }
   }
-  store_eight<false>((OUT*)a.out + row * a.ld_out + col, a.d - col, y);
+  store_eight<false>((OUT*)a.out + s.row * a.ld_out + s.col, s.left, y);
 }
 
-// A workgroup of WAVES wavefronts per row: every choice's product with dy is a sum over the workgroup.
-template <class T, int WAVES> __global__ void __launch_bounds__(64 * WAVES) rfast_route_combine_back(Rows a) {
+// A workgroup of WAVES wavefronts per row, AT_ONCE choices at a time: a choice's product with dy is a sum over the workgroup.
+template <class T, int WAVES, bool WHOLE, int AT_ONCE> __global__ void __launch_bounds__(64 * WAVES) rfast_route_combine_back(Rows a) {
   __shared__ float box[kChoicesMost][WAVES];
   const int64_t row = block_number();
   if (row >= a.rows) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const T* dy = (const T*)a.dy + row * a.ld_dy;
-  for (int j = 0; j < a.k; ++j) {
-    const int32_t at = a.place[row * a.k + j];
-    float dot = 0.f;
-    if ((uint32_t)at < (uint32_t)a.sorted_rows) {
-      const float w = a.weight ? a.weight[row * a.k + j] : 1.f;
-      for (int64_t col = threadIdx.x * 8; col < a.d; col += 64 * WAVES * 8) {
-        float g[8];
-        load_eight<false>(dy + col, a.d - col, g);
-        if (a.dweight) {
-          float v[8];
-          load_eight<false>((const T*)a.in + at * a.ld_in + col, a.d - col, v);
+  const bool dots = a.dweight && a.sorted_rows > 0;
+  for (int first = 0; first < a.k; first += AT_ONCE) {
+    int64_t at[AT_ONCE];
+    bool live[AT_ONCE];
+    float w[AT_ONCE], dot[AT_ONCE];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dot += v[i] * g[i];
-        }
-        if (a.out) {
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int j = min(first + i, a.k - 1);
+      const int32_t p = a.place[row * a.k + j];
+      live[i] = first + i < a.k && (uint32_t)p < (uint32_t)a.sorted_rows;
+      at[i] = live[i] ? p : 0;
+      w[i] = a.weight ? a.weight[row * a.k + j] : 1.f;
+      dot[i] = 0.f;
+    }
+    for (int64_t begin = threadIdx.x * 8; begin < a.d; begin += 64 * WAVES * 8) {
+      const int col = WHOLE ? (int)min(begin, (int64_t)a.d - 8) : (int)begin, left = WHOLE ? 8 : a.d - col;
+      const int again = (int)begin - col;  // columns that the group before has too
+      float g[8], v[AT_ONCE][8];
+      load_eight<false>(dy + col, left, g);
+      if (dots) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) g[i] *= w;
-          store_eight<false>((T*)a.out + at * a.ld_out + col, a.d - col, g);
+        for (int i = 0; i < AT_ONCE; ++i) load_eight<true>((const T*)a.in + at[i] * a.ld_in + col, left, v[i]);
+      }
+      if (a.out) {
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          float o[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) o[c] = w[i] * g[c];
+          if (live[i]) store_eight<true>((T*)a.out + at[i] * a.ld_out + col, left, o);
         }
+      }
+      if (dots) {
+        if (again > 0) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) g[c] = c < again ? 0.f : g[c];
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[i][c] = c < again ? 0.f : v[i][c];
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+          for (int c = 0; c < 8; ++c) dot[i] += v[i][c] * g[c];
       }
     }
     if (a.dweight) {
-      dot = wave_reduce(dot, [](float x, float y) { return x + y; });
-      if (lane == 0) box[j][wave] = dot;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const float sum = wave_reduce(live[i] ? dot[i] : 0.f, [](float x, float y) { return x + y; });
+        if (lane == 0 && first + i < a.k) box[first + i][wave] = sum;
+      }
     }
   }
   if (!a.dweight) return;
@@ -271,13 +325,21 @@ template <class T, int WAVES> __global__ void __launch_bounds__(64 * WAVES) rfas
   }
 }
 
-// Lanes per row of `columns` columns, eight of them each.
+// go(lanes per row, whole groups) for rows of `columns` columns.
 template <class F> hipError_t by_lanes(int64_t columns, F go) {
   using std::integral_constant;
-  if (columns <= 64) return go(integral_constant<int, 8>());
-  if (columns <= 128) return go(integral_constant<int, 16>());
-  if (columns <= 256) return go(integral_constant<int, 32>());
-  return go(integral_constant<int, 64>());
+  if (columns < 8) return go(integral_constant<int, 8>(), std::false_type());
+  if (columns <= 64) return go(integral_constant<int, 8>(), std::true_type());
+  if (columns <= 128) return go(integral_constant<int, 16>(), std::true_type());
+  if (columns <= 256) return go(integral_constant<int, 32>(), std::true_type());
+  return go(integral_constant<int, 64>(), std::true_type());
+}
+// go(choices at once)
+template <class F> hipError_t by_choices(int32_t k, F go) {
+  using std::integral_constant;
+  if (k <= 2) return go(integral_constant<int, 2>());
+  if (k <= 4) return go(integral_constant<int, 4>());
+  return go(integral_constant<int, 8>());
 }
 
 RfastArea area(const void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) { return {p, rows, ld * bytes, columns * bytes}; }
@@ -401,10 +463,11 @@ extern "C" int rfast_route_gather(int32_t rows, int32_t k, int32_t d, const void
   const int64_t half = w / 2, columns = d * half;
   if (columns > kColumnsMost) return rfast_refuse(RFAST_EINVAL, "rows of nearly 2^32 bytes or more");
   const Rows a = {x, place, nullptr, nullptr, sorted, nullptr, ld_x * half, 0, ld_sorted * half, rows, k, (int32_t)columns, sorted_rows};
-  const hipError_t e = by_lanes(columns, [&](auto lanes) {
+  const hipError_t e = by_lanes(columns, [&](auto lanes, auto whole) {
     constexpr int L = decltype(lanes)::value;
+    constexpr bool W = decltype(whole)::value;
     const int slabs = (int)((columns + 511) / 512);
-    hipLaunchKernelGGL((rfast_route_gather_kernel<L>), rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0,
+    hipLaunchKernelGGL((rfast_route_gather_kernel<L, W>), rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0,
                        (hipStream_t)hip_stream, a, slabs);
     return hipGetLastError();
   });
@@ -425,16 +488,19 @@ extern "C" int rfast_route_combine(int32_t rows, int32_t k, int32_t d, const voi
   if (const int bad = apart(in, 3, out, 1)) return bad;
   const Rows a = {sorted, place, weight, nullptr, y, nullptr, ld_sorted, 0, ld_y, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const hipError_t e = by_lanes(d, [&](auto lanes) {
-    constexpr int L = decltype(lanes)::value;
-    const int slabs = (int)(((int64_t)d + 511) / 512);
-    const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
-    const bool tf = type == RFAST_F32, yf = y_type == RFAST_F32;
-    if (tf && yf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else if (tf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else if (yf) hipLaunchKernelGGL((rfast_route_combine_kernel<u16, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else hipLaunchKernelGGL((rfast_route_combine_kernel<u16, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    return hipGetLastError();
+  const hipError_t e = by_lanes(d, [&](auto lanes, auto whole) {
+    return by_choices(k, [&](auto choices) {
+      constexpr int L = decltype(lanes)::value, C = decltype(choices)::value;
+      constexpr bool W = decltype(whole)::value;
+      const int slabs = (int)(((int64_t)d + 511) / 512);
+      const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
+      const bool tf = type == RFAST_F32, yf = y_type == RFAST_F32;
+      if (tf && yf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, float, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
+      else if (tf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, u16, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
+      else if (yf) hipLaunchKernelGGL((rfast_route_combine_kernel<u16, float, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
+      else hipLaunchKernelGGL((rfast_route_combine_kernel<u16, u16, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
+      return hipGetLastError();
+    });
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return launch");
 }
@@ -459,14 +525,16 @@ extern "C" int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, 
   const Rows a = {sorted, place, weight, dy, writes ? dsorted : nullptr, dweight, ld_sorted, ld_dy, ld_dsorted, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
   const dim3 grid = rfast_grid_of(rows);
-  const bool f = type == RFAST_F32;
-  if (d <= 1024) {
-    if (f) hipLaunchKernelGGL((rfast_route_combine_back<float, 1>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((rfast_route_combine_back<u16, 1>), grid, dim3(64), 0, s, a);
-  } else {
-    if (f) hipLaunchKernelGGL((rfast_route_combine_back<float, 4>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((rfast_route_combine_back<u16, 4>), grid, dim3(256), 0, s, a);
-  }
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = by_choices(k, [&](auto choices) {
+    constexpr int C = decltype(choices)::value;
+    const auto go = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+      return hipGetLastError();
+    };
+    const bool f = type == RFAST_F32;
+    if (d < 8) return f ? go(rfast_route_combine_back<float, 1, false, C>, 64) : go(rfast_route_combine_back<u16, 1, false, C>, 64);
+    if (d <= 1024) return f ? go(rfast_route_combine_back<float, 1, true, C>, 64) : go(rfast_route_combine_back<u16, 1, true, C>, 64);
+    return f ? go(rfast_route_combine_back<float, 4, true, C>, 256) : go(rfast_route_combine_back<u16, 4, true, C>, 256);
+  });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return gradient launch");
 }

@@ -73,10 +73,15 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts) 
   const int me = blockIdx.x, b = threadIdx.x;
   int32_t total = 0, before = 0;
   if (b < bins) {
-    for (int p = 0; p < parts; ++p) {
-      const int32_t c = a.counts[(int64_t)p * bins + b];
-      total += c;
-      before += p < me ? c : 0;
+    for (int p = 0; p < parts; p += 16) {  // (sixteen loads under way; those past the last part read it again)
+      int32_t c[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = a.counts[(int64_t)min(p + i, parts - 1) * bins + b];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        total += p + i < parts ? c[i] : 0;
+        before += p + i < me ? c[i] : 0;
+      }
     }
   }
   const int32_t at = before_me(total, box);
