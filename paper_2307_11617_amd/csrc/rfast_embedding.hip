@@ -3,9 +3,11 @@
 //   out_t = s E[token_t]                 dE[v] = s sum_{t: token_t = v} dy_t
 //
 // Both move bytes and compute next to nothing, so what bounds them is memory where they are large and the latency of launches
-// where they are small.  The gradient sorts the tokens (stable, so that a row's terms are added in the order of t), finds where each token's run of
-// rows begins and ends, and then writes every row of the gradient once: zeros, or the sum of its run.  Runs of more than 64 rows (frequent tokens have
-// thousands) would leave one wavefront working for long: they are summed beforehand by parts of up to 64 rows.
+// where they are small.  The gradient sorts the tokens (stable, so that a row's terms are added in the order of t) and clears the table's gradient beside
+// the sort, which would leave the card idle.  A wavefront then adds the rows of a chunk of 16 to 64 sorted positions, run by run: where a run begins and
+// ends inside the chunk its sum is that row of the gradient, else the chunk's part of it goes to the workspace, and a last launch adds
+// the parts of such runs.  So frequent tokens (one in thirty rows) and rare ones cost the same per row of dy.
+#include <algorithm>
 #include <type_traits>
 
 #include "rfast_operators.h"
@@ -13,7 +15,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 64;  // sorted rows whose sum a wavefront makes beforehand
+constexpr int kChunkMost = 64;  // sorted positions that a wavefront adds up
+constexpr int kAtOnce = 8;      // rows of dy under way together
 
 struct Lookup {
   const void* table;
@@ -44,122 +47,141 @@ template <class IN, class OUT, int LANES> __global__ void __launch_bounds__(kThr
 struct Back {
   const void* dy;
   const int32_t* sorted;  // [rows] tokens in order, `vocabulary` for padding
-  const int32_t* order;   // [rows] the row of dy
-  int32_t* begin;         // [vocabulary] of the tokens that are there; the others' hold anything
-  int32_t* end;
-  float* part;            // [chunks][2][d]
+  const int32_t* order;   // [rows] the row of dy, -1 for padding
+  float* part;            // [chunks][2][d]: of a run that an earlier chunk began, of one that goes on behind the chunk
   void* grad;
   int64_t ld_dy, ld_grad;
-  int32_t rows, vocabulary, d, slabs;
+  int32_t rows, vocabulary, d, slabs, chunk;
   float scale;
 };
 
-// Sum of dy over sorted positions [lo, hi), eight columns of a lane.
-template <class IN> __device__ inline void sum_rows(const Back& a, int32_t lo, int32_t hi, int col, float* v) {
-  const IN* dy = (const IN*)a.dy + col;
-#pragma unroll 4
-  for (int32_t p = lo; p < hi; ++p) {
-    float t[8];
-    load_eight<false>(dy + a.order[p] * a.ld_dy, a.d - col, t);
+// Where a lane's eight columns are.  WHOLE (d >= 8): the last group of a row is moved back to end with it, so that every access is a whole one;
+// the columns that it shares with the group before are written twice alike, or not (`again` of them) where they are added to.
+struct Spot {
+  int col, left, again;
+};
+template <int LANES, bool WHOLE> __device__ inline Spot spot_of(int32_t d, int slab) {
+  const int col = (slab * LANES + threadIdx.x % LANES) * 8;
+  if (WHOLE) return {min(col, d - 8), 8, max(col - (d - 8), 0)};
+  return {col, d - col, 0};
+}
+
+template <class OUT, bool ADD> __device__ inline void store_sum(OUT* grad, const Spot& s, float scale, const float* sum, const float* had) {
+  float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += t[j];
-  }
-}
-
-// A wavefront per chunk of 64 sorted positions and slab of 512 columns: where runs begin and end, and the sums of the chunk's parts of long runs.
-// A run of more than 64 rows that has a part of this chunk has its first or its last position, so there are at most two.
-template <class IN> __global__ void __launch_bounds__(kThreads) rfast_embedding_runs(Back a) {
-  const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / 64) + threadIdx.x / 64;
-  const int64_t chunk = unit / a.slabs, first = chunk * kChunk;
-  if (first >= a.rows) return;
-  const int slab = (int)(unit % a.slabs), lane = threadIdx.x & 63;
-  const int64_t p = first + lane;
-  const int count = (int)min((int64_t)kChunk, a.rows - first);
-  const int32_t mine = p < a.rows ? a.sorted[p] : -1;
-  const int32_t back = chunk > 0 ? a.sorted[p - kChunk] : -1;             // the chunk before
-  const int32_t ahead = p + kChunk < a.rows ? a.sorted[p + kChunk] : -1;  // the chunk behind
-  const int32_t before = __shfl_up(mine, 1, 64), after = __shfl_down(mine, 1, 64);
-  const int32_t last = __shfl(back, 63, 64), next = __shfl(ahead, 0, 64);
-  const int32_t left = lane > 0 ? before : last, right = lane < 63 ? after : next;
-  const bool token = mine >= 0 && mine < a.vocabulary;
-  if (slab == 0 && token) {
-    if (left != mine) a.begin[mine] = (int32_t)p;
-    if (right != mine) a.end[mine] = (int32_t)p + 1;
-  }
-  const int col = (slab * 64 + lane) * 8;
-  const int32_t head = __shfl(mine, 0, 64), tail = __shfl(mine, count - 1, 64);
-  const uint64_t in_head = __ballot(mine == head), in_tail = __ballot(mine == tail);
-  const int behind = __popcll(__ballot(back == head)), beyond = __popcll(__ballot(ahead == tail));
-  const int n_head = __popcll(in_head), n_tail = __popcll(in_tail);
-  // (where one run has the whole chunk, both counts apply)
-  if (head != a.vocabulary && behind + n_head + (head == tail ? beyond : 0) > kChunk && col < a.d) {
-    float v[8] = {};
-    sum_rows<IN>(a, (int32_t)first, (int32_t)first + n_head, col, v);
-    store_eight<false>(a.part + (2 * chunk) * a.d + col, a.d - col, v);
-  }
-  if (tail != head && tail != a.vocabulary && n_tail + beyond > kChunk && col < a.d) {
-    float v[8] = {};
-    sum_rows<IN>(a, (int32_t)first + count - n_tail, (int32_t)first + count, col, v);
-    store_eight<false>(a.part + (2 * chunk + 1) * a.d + col, a.d - col, v);
-  }
-}
-
-// LANES lanes per row of the gradient (or, where it is accumulated, per sorted position, of which the first of a run works).
-template <class IN, class OUT, int LANES, bool ADD> __global__ void __launch_bounds__(kThreads) rfast_embedding_grad(Back a, int64_t units) {
-  const int64_t unit = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x) / LANES;
-  if (unit >= units) return;
-  const int64_t at = unit / a.slabs;
-  const int col = ((int)(unit % a.slabs) * LANES + threadIdx.x % LANES) * 8;
-  if (col >= a.d) return;
-  int32_t token, lo = 0, hi = 0;
-  if constexpr (ADD) {
-    token = a.sorted[at];
-    if (token >= a.vocabulary || (at > 0 && a.sorted[at - 1] == token)) return;
-    lo = (int32_t)at;
-    hi = a.end[token];
+  for (int j = 0; j < 8; ++j) v[j] = ADD ? had[j] + scale * sum[j] : scale * sum[j];
+  if (ADD && s.again > 0) {
+    for (int j = 0; j < 8; ++j)
+      if (j >= s.again) store_four<false>(grad + j, 1, v + j);
   } else {
-    token = (int32_t)at;
-    // begin[] is not cleared: a number counts only if a run of this very token begins there, whatever was in memory
-    const int32_t b = a.begin[at];
-    if ((uint32_t)b < (uint32_t)a.rows && a.sorted[b] == token && (b == 0 || a.sorted[b - 1] != token)) lo = b, hi = a.end[at];
+    store_eight<false>(grad, s.left, v);
   }
-  float v[8] = {};
-  if (hi - lo > kChunk) {
-    const float* part = a.part + col;
-    for (int32_t c = lo / kChunk; c <= (hi - 1) / kChunk; ++c) {
-      float t[8];
-      load_eight<false>(part + (2 * (int64_t)c + (lo > c * kChunk)) * a.d, a.d - col, t);
+}
+
+// LANES lanes per chunk and slab of columns.
+template <class IN, class OUT, int LANES, bool WHOLE, bool ADD> __global__ void __launch_bounds__(kThreads) rfast_embedding_sums(Back a) {
+  constexpr int UNITS = kThreads / LANES;
+  __shared__ int2 list[UNITS][kChunkMost];  // token, row of dy
+  const int mine = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * UNITS + mine;
+  const int64_t chunk = unit / a.slabs, lo = chunk * a.chunk;
+  const int n = (int)max((int64_t)0, min((int64_t)a.chunk, a.rows - lo));
+  for (int i = lane; i < n; i += LANES) list[mine][i] = make_int2(a.sorted[lo + i], a.order[lo + i]);
+  __syncthreads();
+  const Spot s = spot_of<LANES, WHOLE>(a.d, (int)(unit - chunk * a.slabs));
+  if (n == 0 || s.again >= 8 || s.left <= 0) return;
+  const int32_t before = lo > 0 ? a.sorted[lo - 1] : -1, behind = lo + n < a.rows ? a.sorted[lo + n] : -1;
+  const IN* dy = (const IN*)a.dy + s.col;
+  OUT* grad = (OUT*)a.grad + s.col;
+  float* part = a.part + 2 * chunk * a.d + s.col;
+  float sum[8] = {};
+  bool begun = list[mine][0].x == before;  // the run at hand began in an earlier chunk
+  for (int first = 0; first < n; first += kAtOnce) {
+    float v[kAtOnce][8], had[kAtOnce][8];
+    int32_t token[kAtOnce + 1];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += t[j];
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int2 e = list[mine][min(first + i, n - 1)];
+      token[i] = e.x;
+      load_eight<false>(dy + max(e.y, 0) * a.ld_dy, s.left, v[i]);
+      if constexpr (ADD) load_eight<false>(grad + (e.x < a.vocabulary ? e.x : 0) * a.ld_grad, s.left, had[i]);
     }
-  } else {
-    sum_rows<IN>(a, lo, hi, col, v);
-  }
-  OUT* grad = (OUT*)a.grad + token * a.ld_grad + col;
+    token[kAtOnce] = first + kAtOnce < n ? list[mine][first + kAtOnce].x : behind;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= a.scale;
-  if constexpr (ADD) {
-    float had[8];
-    load_eight<false>(grad, a.d - col, had);
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (first + i >= n || token[i] == a.vocabulary) break;  // (padding comes last)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += had[j];
+      for (int j = 0; j < 8; ++j) sum[j] += v[i][j];
+      const bool end = first + i == n - 1;
+      const int32_t next = end ? behind : token[i + 1];
+      if (next != token[i] || end) {
+        if (begun || next == token[i]) store_eight<false>(part + (begun ? 0 : a.d), s.left, sum);
+        else store_sum<OUT, ADD>(grad + token[i] * a.ld_grad, s, a.scale, sum, had[i]);
+        begun = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+      }
+    }
   }
-  store_eight<false>(grad, a.d - col, v);
 }
 
-// Lanes per row of d columns, eight of them each: a power of two from 8 to 64.
+// The runs that go on behind the chunk that they begin in: LANES lanes per chunk and slab.
+template <class OUT, int LANES, bool WHOLE, bool ADD> __global__ void __launch_bounds__(kThreads) rfast_embedding_join(Back a) {
+  const int64_t unit = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x) / LANES;
+  const int64_t chunk = unit / a.slabs, lo = chunk * a.chunk, hi = lo + a.chunk;
+  if (hi >= a.rows) return;
+  const int32_t token = a.sorted[hi];
+  if (token == a.vocabulary || a.sorted[hi - 1] != token || (lo > 0 && a.sorted[lo - 1] == token)) return;
+  // how many of the chunks behind begin with it, LANES at a time
+  const int lane = threadIdx.x % LANES, base = (threadIdx.x & 63) - lane;
+  int64_t more = 0;
+  for (;;) {
+    const int64_t p = hi + (more + lane) * a.chunk;
+    const bool has = p < a.rows && a.sorted[p] == token;
+    uint64_t all = __ballot(has) >> base;
+    if (LANES < 64) all |= ~0ull << (LANES & 63);
+    const int run = ~all ? __ffsll((unsigned long long)~all) - 1 : 64;
+    if (run >= LANES) {
+      more += LANES;
+    } else {
+      more += run;
+      break;
+    }
+  }
+  const Spot s = spot_of<LANES, WHOLE>(a.d, (int)(unit - chunk * a.slabs));
+  if (s.again >= 8 || s.left <= 0) return;
+  const float* part = a.part + 2 * chunk * a.d + s.col;
+  float sum[8], had[8];
+  OUT* grad = (OUT*)a.grad + token * a.ld_grad + s.col;
+  if constexpr (ADD) load_eight<false>(grad, s.left, had);
+  load_eight<false>(part + a.d, s.left, sum);
+  for (int64_t c = 1; c <= more; c += kAtOnce) {
+    float v[kAtOnce][8];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) load_eight<false>(part + 2 * min(c + i, more) * a.d, s.left, v[i]);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += c + i <= more ? v[i][j] : 0.f;
+  }
+  store_sum<OUT, ADD>(grad, s, a.scale, sum, had);
+}
+
+// go(lanes per row, eight columns each; whole groups)
 template <class F> hipError_t by_lanes(int32_t d, F go) {
   using std::integral_constant;
-  if (d <= 64) return go(integral_constant<int, 8>());
-  if (d <= 128) return go(integral_constant<int, 16>());
-  if (d <= 256) return go(integral_constant<int, 32>());
-  return go(integral_constant<int, 64>());
+  if (d < 8) return go(integral_constant<int, 8>(), std::false_type());
+  if (d <= 64) return go(integral_constant<int, 8>(), std::true_type());
+  if (d <= 128) return go(integral_constant<int, 16>(), std::true_type());
+  if (d <= 256) return go(integral_constant<int, 32>(), std::true_type());
+  return go(integral_constant<int, 64>(), std::true_type());
 }
-int slabs_of(int32_t d) { return (d + 511) / 512; }
+int slabs_of(int32_t d) { return (int)(((int64_t)d + 511) / 512); }
 
 size_t up(size_t b) { return (b + 255) / 256 * 256; }
 struct Layout {
-  size_t order, sorted, begin, end, part, sort, total;
+  size_t order, sorted, part, sort, total;
+  int chunk;
   Layout(int32_t rows, int32_t vocabulary, int32_t d) {
     size_t at = 0;
     const auto take = [&](size_t bytes) {
@@ -167,11 +189,14 @@ struct Layout {
       at += up(bytes);
       return here;
     };
+    // short chunks where long ones would be too few wavefronts for the card
+    const int64_t slabs = slabs_of(d), few = 8192;
+    chunk = 16;
+    while (chunk < kChunkMost && ((int64_t)rows + chunk - 1) / chunk * slabs > few) chunk *= 2;
+    const int64_t chunks = std::max(std::min(((int64_t)rows + 15) / 16, few / slabs), ((int64_t)rows + kChunkMost - 1) / kChunkMost);
     order = take((size_t)rows * 4);
     sorted = take((size_t)rows * 4);
-    begin = take((size_t)vocabulary * 4);
-    end = take((size_t)vocabulary * 4);
-    part = take(rows > kChunk ? ((size_t)rows + kChunk - 1) / kChunk * 2 * d * 4 : 0);
+    part = take((size_t)chunks * 2 * d * 4);
     sort = take(rfast_sort_bytes(rows, vocabulary));
     total = at;
   }
@@ -196,7 +221,7 @@ extern "C" int rfast_embedding(int32_t rows, int32_t vocabulary, int32_t d, cons
     return rfast_refuse(RFAST_EINVAL, "the output overlaps an input");
   const Lookup a = {table, tokens, out, ld_table, ld_out, rows, vocabulary, d, scale};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const hipError_t e = by_lanes(d, [&](auto lanes) {
+  const hipError_t e = by_lanes(d, [&](auto lanes, auto) {
     constexpr int L = decltype(lanes)::value;
     const int slabs = slabs_of(d);
     const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
@@ -235,32 +260,31 @@ extern "C" int rfast_embedding_backward(int32_t rows, int32_t vocabulary, int32_
   if (rows == 0 && accumulate) return RFAST_OK;
   char* ws = (char*)workspace;
   const hipStream_t s = (hipStream_t)hip_stream;
-  Back a = {dy, (int32_t*)(ws + at.sorted), (int32_t*)(ws + at.order), (int32_t*)(ws + at.begin), (int32_t*)(ws + at.end), (float*)(ws + at.part), grad,
-            ld_dy, ld_grad, rows, vocabulary, d, slabs_of(d), scale};
-  hipError_t e = hipSuccess;
+  const Back a = {dy, (int32_t*)(ws + at.sorted), (int32_t*)(ws + at.order), (float*)(ws + at.part), grad, ld_dy, ld_grad, rows, vocabulary, d,
+                  slabs_of(d), at.chunk, scale};
   const bool yf = dy_type == RFAST_F32, gf = grad_type == RFAST_F32;
-  if (rows) {
-    e = rfast_sort({rows, vocabulary, tokens, nullptr, nullptr, (int32_t*)a.order, (int32_t*)a.sorted, ws + at.sort}, s);
-    if (e != hipSuccess) return rfast_refuse_hip(e, "sort launch");
-    const int64_t waves = ((int64_t)rows + kChunk - 1) / kChunk * a.slabs;
-    const dim3 grid = rfast_grid_of((waves + kThreads / 64 - 1) / (kThreads / 64));
-    if (yf) hipLaunchKernelGGL((rfast_embedding_runs<float>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((rfast_embedding_runs<u16>), grid, dim3(kThreads), 0, s, a);
-  }
-  e = by_lanes(d, [&](auto lanes) {
+  hipError_t e = rfast_sort({rows, vocabulary, tokens, nullptr, nullptr, (int32_t*)a.order, (int32_t*)a.sorted, ws + at.sort,
+                             accumulate ? RfastFill{} : rfast_fill_of(grad, vocabulary, ld_grad, d, gw)}, s);
+  if (e != hipSuccess) return rfast_refuse_hip(e, "sort launch");
+  if (rows == 0) return RFAST_OK;
+  e = by_lanes(d, [&](auto lanes, auto whole) {
     constexpr int L = decltype(lanes)::value;
-    const int64_t units = (int64_t)(accumulate ? rows : vocabulary) * a.slabs;
-    const dim3 grid = rfast_grid_of((units * L + kThreads - 1) / kThreads);
-    const auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, units);
+    constexpr bool W = decltype(whole)::value;
+    const int64_t chunks = ((int64_t)rows + a.chunk - 1) / a.chunk;
+    const dim3 grid = rfast_grid_of((chunks * a.slabs * L + kThreads - 1) / kThreads);
+    const auto go = [&](auto sums, auto join) {
+      hipLaunchKernelGGL(sums, grid, dim3(kThreads), 0, s, a);
+      if (chunks > 1) hipLaunchKernelGGL(join, grid, dim3(kThreads), 0, s, a);
       return hipGetLastError();
     };
-    if (accumulate) {
-      if (yf) return gf ? go(rfast_embedding_grad<float, float, L, true>) : go(rfast_embedding_grad<float, u16, L, true>);
-      return gf ? go(rfast_embedding_grad<u16, float, L, true>) : go(rfast_embedding_grad<u16, u16, L, true>);
-    }
-    if (yf) return gf ? go(rfast_embedding_grad<float, float, L, false>) : go(rfast_embedding_grad<float, u16, L, false>);
-    return gf ? go(rfast_embedding_grad<u16, float, L, false>) : go(rfast_embedding_grad<u16, u16, L, false>);
+    const auto by_types = [&](auto add) {
+      constexpr bool A = decltype(add)::value;
+      if (gf) return yf ? go(rfast_embedding_sums<float, float, L, W, A>, rfast_embedding_join<float, L, W, A>)
+                        : go(rfast_embedding_sums<u16, float, L, W, A>, rfast_embedding_join<float, L, W, A>);
+      return yf ? go(rfast_embedding_sums<float, u16, L, W, A>, rfast_embedding_join<u16, L, W, A>)
+                : go(rfast_embedding_sums<u16, u16, L, W, A>, rfast_embedding_join<u16, L, W, A>);
+    };
+    return accumulate ? by_types(std::true_type()) : by_types(std::false_type());
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "embedding gradient launch");
 }

@@ -26,6 +26,23 @@ inline bool rfast_overlap(const RfastArea& a, const RfastArea& b) {
   return behind < a.wide || behind + b.wide > a.apart;
 }
 
+typedef unsigned short u16;
+
+// Memory to be cleared: `parts` parts of `wide` units of 2 bytes, `apart` units apart (the last one `last` units).
+struct RfastFill {
+  u16* p;
+  int64_t parts, apart, wide, last;
+};
+// A matrix of elements of `bytes` bytes.
+inline RfastFill rfast_fill_of(void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) {
+  const int64_t half = bytes / 2, all = rows * columns * half, piece = 1 << 12;
+  if (ld == columns && all > 0) {  // one piece of memory: in parts of 8 KB, whatever the rows
+    const int64_t parts = (all + piece - 1) / piece;
+    return {(u16*)p, parts, piece, piece, all - (parts - 1) * piece};
+  }
+  return {(u16*)p, rows, ld * half, columns * half, columns * half};
+}
+
 // Stable sort of `count` numbers; those outside [0, keys) come last.  Any of the outputs but one may be NULL (rfast_sort.hip).
 struct RfastSort {
   int32_t count, keys;
@@ -35,6 +52,7 @@ struct RfastSort {
   int32_t* order;       // [count]: which element is there, -1 behind the last number inside
   int32_t* sorted;      // [count]: the numbers, `keys` for those outside
   void* workspace;      // rfast_sort_bytes, 256-byte aligned
+  RfastFill fill;       // done beside the sort, which leaves nearly all of the card idle
 };
 size_t rfast_sort_bytes(int32_t count, int32_t keys);
 hipError_t rfast_sort(const RfastSort& s, hipStream_t stream);
@@ -46,7 +64,6 @@ inline dim3 rfast_grid_of(int64_t blocks) {  // a dimension of a launch has fewe
   return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
 
-typedef unsigned short u16;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));

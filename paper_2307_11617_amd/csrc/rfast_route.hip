@@ -356,7 +356,7 @@ const char* const kNull = "NULL argument";
 
 int plan(int32_t pairs, int32_t experts, const int32_t* expert, int32_t* row_ptr, int32_t* place, int32_t* order, void* workspace,
          hipStream_t s) {
-  const hipError_t e = rfast_sort({pairs, experts, expert, row_ptr, place, order, nullptr, workspace}, s);
+  const hipError_t e = rfast_sort({pairs, experts, expert, row_ptr, place, order, nullptr, workspace, {}}, s);
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "sort launch");
 }
 

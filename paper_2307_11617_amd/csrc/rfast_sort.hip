@@ -30,12 +30,31 @@ struct Part {
   bool first, last;
 };
 
+// What workgroups behind the sort's own clear: parts [lo, hi) of the fill, a wavefront each.
+struct Beside {
+  RfastFill fill;
+  int64_t lo, hi;
+  int blocks;  // of the sort
+};
+__device__ inline void clear_beside(const Beside& f) {
+  const int waves = blockDim.x / 64, lane = threadIdx.x & 63;
+  const any_u32x4 zero = {0, 0, 0, 0};
+  for (int64_t part = f.lo + (int64_t)(blockIdx.x - f.blocks) * waves + threadIdx.x / 64; part < f.hi; part += (int64_t)(gridDim.x - f.blocks) * waves) {
+    u16* p = f.fill.p + part * f.fill.apart;
+    const int64_t n = part == f.fill.parts - 1 ? f.fill.last : f.fill.wide;
+    int64_t i = lane * 8;
+    for (; i + 8 <= n; i += 512) wide_store<any_u32x4, true>(p + i, zero);
+    for (int j = 0; j < 8 && i + j < n; ++j) p[i + j] = 0;  // (of one lane: the end of the part)
+  }
+}
+
 __device__ inline int clip_key(int32_t k, int32_t keys) { return (uint32_t)k < (uint32_t)keys ? k : keys; }
 
 template <int DIGIT>
-__global__ void __launch_bounds__(kThreads) rfast_sort_count(Part a) {
+__global__ void __launch_bounds__(kThreads) rfast_sort_count(Part a, Beside beside) {
   constexpr int bins = 1 << DIGIT;
   __shared__ int32_t hist[bins];
+  if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
   for (int b = threadIdx.x; b < bins; b += kThreads) hist[b] = 0;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * a.per_part, hi = min(lo + a.per_part, (int64_t)a.count);
@@ -64,11 +83,12 @@ __device__ inline int32_t before_me(int32_t v, int32_t* box) {
 }
 
 template <int DIGIT>
-__global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts) {
+__global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, Beside beside) {
   constexpr int bins = 1 << DIGIT;
   __shared__ int32_t start[bins];          // where the next element of each digit of this part goes
   __shared__ int32_t hist[kWaves * bins];  // per wavefront: elements of each digit so far, then where they begin
   __shared__ int32_t box[kWaves];
+  if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int me = blockIdx.x, b = threadIdx.x;
   int32_t total = 0, before = 0;
@@ -146,6 +166,95 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts) 
   }
 }
 
+// All passes of up to CHUNKS * 1024 numbers in one workgroup of as many wavefronts as they need.
+template <int DIGIT, int CHUNKS>
+__global__ void __launch_bounds__(kThreads) rfast_sort_small(Part a, int passes, Beside beside) {
+  constexpr int bins = 1 << DIGIT, MOST = kThreads * CHUNKS;
+  __shared__ int32_t start[bins];
+  __shared__ int32_t hist[kWaves * bins];
+  __shared__ int32_t box[kWaves];
+  __shared__ int32_t moved[2][MOST];
+  if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, threads = blockDim.x;
+  const uint64_t below = (1ull << lane) - 1;
+  int32_t key[CHUNKS], from[CHUNKS], to[CHUNKS];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    from[c] = wave * (64 * CHUNKS) + c * 64 + lane;
+    key[c] = from[c] < a.count ? clip_key(a.key[from[c]], a.keys) : -1;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * DIGIT;
+    for (int i = threadIdx.x; i < waves * bins; i += threads) hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const bool is = key[c] >= 0;
+      const int digit = (key[c] >> shift) & (bins - 1);
+      uint64_t same = __ballot(is);
+#pragma unroll
+      for (int k = 0; k < DIGIT; ++k) {
+        const uint64_t one = __ballot((digit >> k) & 1);
+        same &= (digit >> k) & 1 ? one : ~one;
+      }
+      to[c] = 0;
+      if (is) {
+        const int32_t had = hist[wave * bins + digit];
+        to[c] = had + __popcll(same & below);
+        __builtin_amdgcn_wave_barrier();
+        if ((same & below) == 0) hist[wave * bins + digit] = had + __popcll(same);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    // of each digit: how many before each wavefront's, then where the digit begins (the workgroup may have fewer threads than digits)
+    int32_t carry = 0;
+    for (int first = 0; first < bins; first += threads) {
+      const int b = first + threadIdx.x;
+      int32_t total = 0;
+      if (b < bins) {
+        for (int w = 0; w < waves; ++w) {
+          const int32_t h = hist[w * bins + b];
+          hist[w * bins + b] = total;
+          total += h;
+        }
+      }
+      const int32_t at = carry + before_me(total, box);
+      if (b < bins) {
+        start[b] = at;
+        if (a.row_ptr && passes == 1 && b <= a.keys) a.row_ptr[b] = at;
+      }
+      for (int w = 0; w < waves; ++w) carry += box[w];
+      __syncthreads();
+    }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      if (key[c] < 0) continue;
+      const int digit = (key[c] >> shift) & (bins - 1);
+      to[c] += start[digit] + hist[wave * bins + digit];
+    }
+    if (pass + 1 < passes) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+        if (key[c] >= 0) moved[0][to[c]] = key[c], moved[1][to[c]] = from[c];
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        const int i = wave * (64 * CHUNKS) + c * 64 + lane;
+        key[c] = i < a.count ? moved[0][i] : -1;
+        from[c] = i < a.count ? moved[1][i] : 0;
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    if (key[c] < 0) continue;
+    if (a.out_key) a.out_key[to[c]] = key[c];
+    if (a.order) a.order[to[c]] = key[c] < a.keys ? from[c] : -1;
+    if (a.place) a.place[from[c]] = key[c] < a.keys ? to[c] : -1;
+  }
+}
+
 // row_ptr where numbers take several passes: how many of the sorted ones are below each
 __global__ void __launch_bounds__(256) rfast_sort_bounds(const int32_t* sorted, int32_t count, int32_t keys, int32_t* row_ptr) {
   const int64_t v = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
@@ -161,9 +270,12 @@ __global__ void __launch_bounds__(256) rfast_sort_bounds(const int32_t* sorted, 
 
 size_t up(size_t b) { return (b + 255) / 256 * 256; }
 
+constexpr int kSmallChunks = 8, kSmall = kSmallChunks * kThreads;
+
 struct Plan {
   int passes, digit, parts;
   int32_t per_part;
+  bool small;  // one launch
   Plan(int32_t count, int32_t keys) {
     int bits = 1;
     while (bits < 31 && (keys >> bits) != 0) ++bits;  // `keys` itself is a number too: that of elements outside
@@ -174,6 +286,7 @@ struct Plan {
     const int64_t per = (tiles + kPartsMost - 1) / kPartsMost;
     per_part = (int32_t)(per * kTile < 0x7fffffff ? per * kTile : 0x7fffffff);
     parts = count ? (int)(((int64_t)count + per_part - 1) / per_part) : 0;
+    small = count <= kSmall;
   }
 };
 
@@ -181,49 +294,93 @@ struct Plan {
 
 size_t rfast_sort_bytes(int32_t count, int32_t keys) {
   const Plan p(count, keys);
-  return up((size_t)p.parts << (p.digit + 2)) + (p.passes > 1 ? 4 : 0) * up((size_t)count * 4) + 256;
+  if (p.small) return up((size_t)count * 4) + 256;  // (the sorted numbers, for row_ptr)
+  return up((size_t)p.parts << (p.digit + 2)) + (p.passes > 1 ? 4 : 0) * up((size_t)count * 4) + 256 + up((size_t)kSmall * 4);
 }
 
 hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
   const Plan p(s.count, s.keys);
-  char* ws = (char*)s.workspace;
-  int32_t* counts = (int32_t*)ws;
-  ws += up((size_t)p.parts << (p.digit + 2));
-  int32_t* buffer[4] = {};
-  if (p.passes > 1) {
-    for (int i = 0; i < 4; ++i) buffer[i] = (int32_t*)ws, ws += up((size_t)s.count * 4);
-  }
-  const int32_t* sorted = nullptr;
-  for (int pass = 0; pass < p.passes && s.count; ++pass) {
-    Part a = {};
-    a.first = pass == 0;
-    a.last = pass == p.passes - 1;
-    a.count = s.count;
-    a.keys = s.keys;
-    a.per_part = p.per_part;
-    a.counts = counts;
-    a.shift = pass * p.digit;
-    a.key = a.first ? s.key : buffer[(pass & 1) ^ 1];
-    a.index = a.first ? nullptr : buffer[2 + ((pass & 1) ^ 1)];
-    a.out_key = a.last ? s.sorted : buffer[pass & 1];
-    a.out_index = a.last ? nullptr : buffer[2 + (pass & 1)];
-    if (a.last && !a.out_key && s.row_ptr && p.passes > 1) a.out_key = buffer[pass & 1];
-    if (a.last) {
-      a.order = s.order;
-      a.place = s.place;
-      a.row_ptr = p.passes == 1 ? s.row_ptr : nullptr;
-      sorted = a.out_key;
-    }
-    const auto go = [&](auto digit) {
-      constexpr int D = decltype(digit)::value;
-      hipLaunchKernelGGL((rfast_sort_count<D>), dim3(p.parts), dim3(kThreads), 0, stream, a);
-      hipLaunchKernelGGL((rfast_sort_place<D>), dim3(p.parts), dim3(kThreads), 0, stream, a, p.parts);
-    };
+  const int launches = s.count == 0 ? 1 : p.small ? 1 : 2 * p.passes;
+  int done = 0;
+  // the next launch's share of the fill, and the workgroups that it takes
+  const auto beside = [&](int blocks) {
+    Beside f = {s.fill, s.fill.parts * done / launches, s.fill.parts * (done + 1) / launches, blocks};
+    ++done;
+    return f;
+  };
+  const auto grid = [](const Beside& f, int threads) {
+    const int64_t waves = threads / 64, need = (f.hi - f.lo + waves - 1) / waves;
+    return dim3((unsigned)(f.blocks + (need < 512 * 16 / waves ? need : 512 * 16 / waves)));
+  };
+  const auto by_digit = [&](auto go) {
     using std::integral_constant;
     if (p.digit == 6) go(integral_constant<int, 6>());
     else if (p.digit == 8) go(integral_constant<int, 8>());
     else if (p.digit == 9) go(integral_constant<int, 9>());
     else go(integral_constant<int, 10>());
+  };
+  char* ws = (char*)s.workspace;
+  const int32_t* sorted = nullptr;
+  if (s.count == 0) {
+    if (s.fill.parts > 0) {
+      const Beside f = beside(0);
+      hipLaunchKernelGGL((rfast_sort_count<6>), grid(f, kThreads), dim3(kThreads), 0, stream, Part{}, f);
+    }
+  } else if (p.small) {
+    Part a = {};
+    a.key = s.key;
+    a.count = s.count;
+    a.keys = s.keys;
+    a.row_ptr = s.row_ptr;
+    a.order = s.order;
+    a.place = s.place;
+    a.out_key = s.sorted ? s.sorted : s.row_ptr && p.passes > 1 ? (int32_t*)ws : nullptr;
+    sorted = a.out_key;
+    by_digit([&](auto digit) {
+      constexpr int D = decltype(digit)::value;
+      const Beside f = beside(1);
+      const auto go = [&](auto kernel, int chunks) {
+        const int waves = (s.count + 64 * chunks - 1) / (64 * chunks), threads = s.fill.parts > 0 ? kThreads : 64 * waves;
+        hipLaunchKernelGGL(kernel, grid(f, threads), dim3(threads), 0, stream, a, p.passes, f);
+      };
+      if (s.count <= kThreads) go(rfast_sort_small<D, 1>, 1);
+      else if (s.count <= 4 * kThreads) go(rfast_sort_small<D, 4>, 4);
+      else go(rfast_sort_small<D, kSmallChunks>, kSmallChunks);
+    });
+  } else {
+    int32_t* counts = (int32_t*)ws;
+    ws += up((size_t)p.parts << (p.digit + 2));
+    int32_t* buffer[4] = {};
+    if (p.passes > 1) {
+      for (int i = 0; i < 4; ++i) buffer[i] = (int32_t*)ws, ws += up((size_t)s.count * 4);
+    }
+    for (int pass = 0; pass < p.passes; ++pass) {
+      Part a = {};
+      a.first = pass == 0;
+      a.last = pass == p.passes - 1;
+      a.count = s.count;
+      a.keys = s.keys;
+      a.per_part = p.per_part;
+      a.counts = counts;
+      a.shift = pass * p.digit;
+      a.key = a.first ? s.key : buffer[(pass & 1) ^ 1];
+      a.index = a.first ? nullptr : buffer[2 + ((pass & 1) ^ 1)];
+      a.out_key = a.last ? s.sorted : buffer[pass & 1];
+      a.out_index = a.last ? nullptr : buffer[2 + (pass & 1)];
+      if (a.last && !a.out_key && s.row_ptr && p.passes > 1) a.out_key = buffer[pass & 1];
+      if (a.last) {
+        a.order = s.order;
+        a.place = s.place;
+        a.row_ptr = p.passes == 1 ? s.row_ptr : nullptr;
+        sorted = a.out_key;
+      }
+      by_digit([&](auto digit) {
+        constexpr int D = decltype(digit)::value;
+        const Beside f = beside(p.parts), g = beside(p.parts);
+        hipLaunchKernelGGL((rfast_sort_count<D>), grid(f, kThreads), dim3(kThreads), 0, stream, a, f);
+        hipLaunchKernelGGL((rfast_sort_place<D>), grid(g, kThreads), dim3(kThreads), 0, stream, a, p.parts, g);
+      });
+    }
   }
   if (s.row_ptr && (p.passes > 1 || !s.count))
     hipLaunchKernelGGL(rfast_sort_bounds, rfast_grid_of(((int64_t)s.keys + 256) / 256), dim3(256), 0, stream, sorted, s.count, s.keys, s.row_ptr);
