@@ -17,6 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunkMost = 64;  // sorted positions that a wavefront adds up
 constexpr int kAtOnce = 8;      // rows of dy under way together
+constexpr int kParts = 16;      // parts of a run under way together
 
 struct Lookup {
   const void* table;
@@ -155,12 +156,12 @@ template <class OUT, int LANES, bool WHOLE, bool ADD> __global__ void __launch_b
   OUT* grad = (OUT*)a.grad + token * a.ld_grad + s.col;
   if constexpr (ADD) load_eight<false>(grad, s.left, had);
   load_eight<false>(part + a.d, s.left, sum);
-  for (int64_t c = 1; c <= more; c += kAtOnce) {
-    float v[kAtOnce][8];
+  for (int64_t c = 1; c <= more; c += kParts) {
+    float v[kParts][8];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) load_eight<false>(part + 2 * min(c + i, more) * a.d, s.left, v[i]);
+    for (int i = 0; i < kParts; ++i) load_eight<false>(part + 2 * min(c + i, more) * a.d, s.left, v[i]);
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
+    for (int i = 0; i < kParts; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += c + i <= more ? v[i][j] : 0.f;
   }
@@ -190,7 +191,7 @@ struct Layout {
       return here;
     };
     // short chunks where long ones would be too few wavefronts for the card
-    const int64_t slabs = slabs_of(d), few = 8192;
+    const int64_t slabs = slabs_of(d), few = 2048;
     chunk = 16;
     while (chunk < kChunkMost && ((int64_t)rows + chunk - 1) / chunk * slabs > few) chunk *= 2;
     const int64_t chunks = std::max(std::min(((int64_t)rows + 15) / 16, few / slabs), ((int64_t)rows + kChunkMost - 1) / kChunkMost);

@@ -11,8 +11,6 @@
 namespace {
 
 constexpr int kWaves = 16, kThreads = kWaves * 64;
-constexpr int kChunks = 4;                     // of 64 neighbours that a wavefront takes at a time
-constexpr int kTile = kThreads * kChunks;      // elements that a workgroup takes at a time
 constexpr int kDigitMost = 10;
 constexpr int kPartsMost = 256;
 
@@ -82,52 +80,90 @@ __device__ inline int32_t before_me(int32_t v, int32_t* box) {
   return off + s - v;
 }
 
-template <int DIGIT>
+// Lanes that have this lane's digit; lanes that are not `is` belong to nobody.
+template <int DIGIT> __device__ inline uint64_t alike(int digit, bool is) {
+  uint64_t same = __ballot(is);
+#pragma unroll
+  for (int k = 0; k < DIGIT; ++k) {
+    const int bit = __builtin_amdgcn_sbfe(digit, k, 1);  // 0 or all bits
+    const uint64_t one = __ballot(bit != 0);
+    same &= ~(one ^ (uint64_t)(int64_t)bit);
+  }
+  return same;
+}
+
+// Of a digit: what each wavefront has becomes what is before it; the sum over all.
+template <int BINS> __device__ inline int32_t before_waves(int32_t* hist, int waves, int32_t run) {
+  int32_t h[kWaves];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) h[w] = w < waves ? hist[w * BINS] : 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < waves) hist[w * BINS] = run;
+    run += h[w];
+  }
+  return run;
+}
+
+// Where the elements of a part go.  CHUNKS: of 64 neighbours that a wavefront takes at a time.
+template <int DIGIT, int CHUNKS>
 __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, Beside beside) {
-  constexpr int bins = 1 << DIGIT;
+  constexpr int bins = 1 << DIGIT, TILE = kThreads * CHUNKS;
+  constexpr int GROUPS = kThreads / bins < 8 ? kThreads / bins : 8;  // of threads that add up the parts' counts
   __shared__ int32_t start[bins];          // where the next element of each digit of this part goes
   __shared__ int32_t hist[kWaves * bins];  // per wavefront: elements of each digit so far, then where they begin
   __shared__ int32_t box[kWaves];
   if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int me = blockIdx.x, b = threadIdx.x;
-  int32_t total = 0, before = 0;
-  if (b < bins) {
-    for (int p = 0; p < parts; p += 16) {  // (sixteen loads under way; those past the last part read it again)
-      int32_t c[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) c[i] = a.counts[(int64_t)min(p + i, parts - 1) * bins + b];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        total += p + i < parts ? c[i] : 0;
-        before += p + i < me ? c[i] : 0;
-      }
-    }
-  }
-  const int32_t at = before_me(total, box);
-  if (b < bins) start[b] = at + before;
-  if (a.row_ptr && me == 0 && b <= a.keys) a.row_ptr[b] = at;  // (one pass: bins > keys)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = blockIdx.x, b = threadIdx.x;
   const int64_t lo = (int64_t)me * a.per_part, hi = min(lo + a.per_part, (int64_t)a.count);
   const uint64_t below = (1ull << lane) - 1;
-  for (int64_t tile = lo; tile < hi; tile += kTile) {
+  int32_t key[CHUNKS], from[CHUNKS], rank[CHUNKS];
+  const auto load = [&](int64_t tile) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const int64_t i = tile + wave * (64 * CHUNKS) + c * 64 + lane;
+      key[c] = i < hi ? a.key[i] : -1;
+      from[c] = a.index ? a.index[min(i, hi - 1)] : (int32_t)i;
+      if (a.first && i < hi) key[c] = clip_key(key[c], a.keys);
+    }
+  };
+  load(lo);
+  {
+    const int digit = threadIdx.x % bins, group = threadIdx.x / bins;
+    int32_t total = 0, before = 0;
+    if (group < GROUPS) {
+      for (int p = group; p < parts; p += 16 * GROUPS) {  // (sixteen loads under way; those past the last part read it again)
+        int32_t c[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = a.counts[(int64_t)min(p + i * GROUPS, parts - 1) * bins + digit];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          total += p + i * GROUPS < parts ? c[i] : 0;
+          before += p + i * GROUPS < me ? c[i] : 0;
+        }
+      }
+      hist[group * bins + digit] = total;
+      hist[(GROUPS + group) * bins + digit] = before;
+    }
+    __syncthreads();
+    total = before = 0;
+    if (b < bins) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) total += hist[g * bins + b], before += hist[(GROUPS + g) * bins + b];
+    }
+    const int32_t at = before_me(total, box);
+    if (b < bins) start[b] = at + before;
+    if (a.row_ptr && me == 0 && b <= a.keys) a.row_ptr[b] = at;  // (one pass: bins > keys)
+  }
+  for (int64_t tile = lo; tile < hi; tile += TILE) {
+    if (tile > lo) load(tile);
     for (int i = threadIdx.x; i < kWaves * bins; i += kThreads) hist[i] = 0;
     __syncthreads();
-    int32_t key[kChunks], rank[kChunks];
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int64_t i = tile + wave * (64 * kChunks) + c * 64 + lane;
-      key[c] = i < hi ? (a.first ? clip_key(a.key[i], a.keys) : a.key[i]) : -1;
-    }
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
+    for (int c = 0; c < CHUNKS; ++c) {
       const bool is = key[c] >= 0;
       const int digit = (key[c] >> a.shift) & (bins - 1);
-      uint64_t same = __ballot(is);
-#pragma unroll
-      for (int k = 0; k < DIGIT; ++k) {
-        const uint64_t one = __ballot((digit >> k) & 1);
-        same &= (digit >> k) & 1 ? one : ~one;
-      }
+      const uint64_t same = alike<DIGIT>(digit, is);
       rank[c] = 0;
       if (is) {
         const int32_t had = hist[wave * bins + digit];
@@ -138,28 +174,18 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, 
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
-    if (b < bins) {
-      int32_t run = start[b];
-      for (int w = 0; w < kWaves; ++w) {
-        const int32_t h = hist[w * bins + b];
-        hist[w * bins + b] = run;
-        run += h;
-      }
-      start[b] = run;
-    }
+    if (b < bins) start[b] = before_waves<bins>(hist + b, kWaves, start[b]);
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int64_t i = tile + wave * (64 * kChunks) + c * 64 + lane;
-      if (i >= hi) continue;
+    for (int c = 0; c < CHUNKS; ++c) {
+      if (key[c] < 0) continue;
       const int digit = (key[c] >> a.shift) & (bins - 1);
       const int32_t to = hist[wave * bins + digit] + rank[c];
-      const int32_t from = a.index ? a.index[i] : (int32_t)i;
       if (a.out_key) a.out_key[to] = key[c];
-      if (a.out_index) a.out_index[to] = from;
+      if (a.out_index) a.out_index[to] = from[c];
       if (a.last) {
-        if (a.order) a.order[to] = key[c] < a.keys ? from : -1;
-        if (a.place) a.place[from] = key[c] < a.keys ? to : -1;
+        if (a.order) a.order[to] = key[c] < a.keys ? from[c] : -1;
+        if (a.place) a.place[from[c]] = key[c] < a.keys ? to : -1;
       }
     }
     __syncthreads();
@@ -191,12 +217,7 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_small(Part a, int passes,
     for (int c = 0; c < CHUNKS; ++c) {
       const bool is = key[c] >= 0;
       const int digit = (key[c] >> shift) & (bins - 1);
-      uint64_t same = __ballot(is);
-#pragma unroll
-      for (int k = 0; k < DIGIT; ++k) {
-        const uint64_t one = __ballot((digit >> k) & 1);
-        same &= (digit >> k) & 1 ? one : ~one;
-      }
+      const uint64_t same = alike<DIGIT>(digit, is);
       to[c] = 0;
       if (is) {
         const int32_t had = hist[wave * bins + digit];
@@ -212,13 +233,7 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_small(Part a, int passes,
     for (int first = 0; first < bins; first += threads) {
       const int b = first + threadIdx.x;
       int32_t total = 0;
-      if (b < bins) {
-        for (int w = 0; w < waves; ++w) {
-          const int32_t h = hist[w * bins + b];
-          hist[w * bins + b] = total;
-          total += h;
-        }
-      }
+      if (b < bins) total = before_waves<bins>(hist + b, waves, 0);
       const int32_t at = carry + before_me(total, box);
       if (b < bins) {
         start[b] = at;
@@ -270,10 +285,10 @@ __global__ void __launch_bounds__(256) rfast_sort_bounds(const int32_t* sorted, 
 
 size_t up(size_t b) { return (b + 255) / 256 * 256; }
 
-constexpr int kSmallChunks = 8, kSmall = kSmallChunks * kThreads;
+constexpr int kSmallChunks = 4, kSmall = kSmallChunks * kThreads;
 
 struct Plan {
-  int passes, digit, parts;
+  int passes, digit, parts, chunks;
   int32_t per_part;
   bool small;  // one launch
   Plan(int32_t count, int32_t keys) {
@@ -282,9 +297,10 @@ struct Plan {
     passes = (bits + kDigitMost - 1) / kDigitMost;
     digit = (bits + passes - 1) / passes;
     digit = digit <= 6 ? 6 : digit < 8 ? 8 : digit;  // (forms of the kernels)
-    const int64_t tiles = ((int64_t)count + kTile - 1) / kTile;
+    chunks = count <= kPartsMost * kThreads ? 1 : 4;
+    const int64_t tile = kThreads * chunks, tiles = ((int64_t)count + tile - 1) / tile;
     const int64_t per = (tiles + kPartsMost - 1) / kPartsMost;
-    per_part = (int32_t)(per * kTile < 0x7fffffff ? per * kTile : 0x7fffffff);
+    per_part = (int32_t)(per * tile < 0x7fffffff ? per * tile : 0x7fffffff);
     parts = count ? (int)(((int64_t)count + per_part - 1) / per_part) : 0;
     small = count <= kSmall;
   }
@@ -340,7 +356,8 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
       constexpr int D = decltype(digit)::value;
       const Beside f = beside(1);
       const auto go = [&](auto kernel, int chunks) {
-        const int waves = (s.count + 64 * chunks - 1) / (64 * chunks), threads = s.fill.parts > 0 ? kThreads : 64 * waves;
+        // (as many threads as digits at least: a digit per thread)
+        const int need = (s.count + 64 * chunks - 1) / (64 * chunks) * 64, threads = s.fill.parts > 0 ? kThreads : need < 1 << D ? 1 << D : need;
         hipLaunchKernelGGL(kernel, grid(f, threads), dim3(threads), 0, stream, a, p.passes, f);
       };
       if (s.count <= kThreads) go(rfast_sort_small<D, 1>, 1);
@@ -378,7 +395,8 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
         constexpr int D = decltype(digit)::value;
         const Beside f = beside(p.parts), g = beside(p.parts);
         hipLaunchKernelGGL((rfast_sort_count<D>), grid(f, kThreads), dim3(kThreads), 0, stream, a, f);
-        hipLaunchKernelGGL((rfast_sort_place<D>), grid(g, kThreads), dim3(kThreads), 0, stream, a, p.parts, g);
+        if (p.chunks == 1) hipLaunchKernelGGL((rfast_sort_place<D, 1>), grid(g, kThreads), dim3(kThreads), 0, stream, a, p.parts, g);
+        else hipLaunchKernelGGL((rfast_sort_place<D, 4>), grid(g, kThreads), dim3(kThreads), 0, stream, a, p.parts, g);
       });
     }
   }
