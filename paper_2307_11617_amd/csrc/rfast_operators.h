@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <string>
+#include <type_traits>
 
 #include "rfast.h"
 
@@ -178,6 +179,29 @@ template <class F> __device__ inline float wave_reduce(float v, F f) {
   v = f(v, lane_of<0x140>(v));  // the other eight of sixteen (mirrored)
   v = f(v, __shfl_xor(v, 16, 64));
   return f(v, __shfl_xor(v, 32, 64));
+}
+// Over groups of LANES neighbours (8 to 64), whole numbers or floats of 32 bits, without going through LDS: the halves of 32 and of 64 lanes
+// are exchanged as registers.
+template <int LANES, class T, class F> __device__ inline T group_reduce(T v, F f) {
+  static_assert(sizeof(T) == 4 && LANES >= 8 && LANES <= 64);
+  const auto lane = [](T x, auto ctrl) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  v = f(v, lane(v, std::integral_constant<int, 0xB1>()));
+  v = f(v, lane(v, std::integral_constant<int, 0x4E>()));
+  v = f(v, lane(v, std::integral_constant<int, 0x141>()));
+  if constexpr (LANES >= 16) v = f(v, lane(v, std::integral_constant<int, 0x140>()));
+  if constexpr (LANES >= 32) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = f(__builtin_bit_cast(T, (uint32_t)both[0]), __builtin_bit_cast(T, (uint32_t)both[1]));
+  }
+  if constexpr (LANES >= 64) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    v = f(__builtin_bit_cast(T, (uint32_t)both[0]), __builtin_bit_cast(T, (uint32_t)both[1]));
+  }
+  return v;
 }
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });

@@ -41,65 +41,111 @@ __device__ inline uint32_t ordered(float f) {
 constexpr uint32_t kMasked = 0x007FFFFFu;  // ordered(-infinity)
 __device__ inline float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 
-template <int LANES, class T, class F> __device__ inline T lanes_reduce(T v, F f) {
-#pragma unroll
-  for (int d = 1; d < LANES; d <<= 1) v = f(v, (T)__shfl_xor(v, d, 64));
-  return v;
-}
+// Of few rows: the order by expert too, in the same launch of one workgroup.
+struct Order {
+  int32_t *row_ptr, *place, *order;
+};
+constexpr int kFewPairs = 256;
 
-// LANES lanes hold a row, HOLD neighbouring experts each; the largest is taken out k times.  Lane j keeps choice j.
-template <class IN, int LANES, int HOLD> __global__ void __launch_bounds__(kThreads) rfast_route_choice(Choice a) {
-  const int64_t row = (block_number() * kThreads + threadIdx.x) / LANES;
-  if (row >= a.rows) return;
+// LANES lanes hold a row, HOLD neighbouring experts each; the largest is taken out k times, and the lane that has it writes its number.  Lane j
+// keeps the value of choice j.
+// FEW: one workgroup has all rows.  A pair's place is how many pairs come before it: smaller experts, and equal ones of smaller pairs.  They are
+// counted outright, each thread reading all the others' (at most 256) from LDS: no digits, no passes.
+template <class IN, int LANES, int HOLD, bool FEW> __global__ void __launch_bounds__(FEW ? 1024 : kThreads) rfast_route_choice(Choice a, Order order) {
+  __shared__ int4 keys[FEW ? kFewPairs / 4 : 1];
+  int* const key = (int*)keys;
+  const int64_t row = FEW ? threadIdx.x / LANES : (block_number() * kThreads + threadIdx.x) / LANES;
   const int lane = threadIdx.x % LANES, base = (threadIdx.x & 63) - lane;
-  const IN* l = (const IN*)a.logits + row * a.ld;
-  float logit[HOLD];
-  uint32_t o[HOLD];
-#pragma unroll
-  for (int j = 0; j < HOLD; ++j) {
-    const int e = lane * HOLD + j;
-    logit[j] = e < a.experts ? wide(l[e]) : -INFINITY;
-    o[j] = e < a.experts ? ordered(logit[j]) : 0u;
+  const bool real = row < a.rows;
+  if (!FEW && !real) return;
+  const int pairs = FEW ? a.rows * a.k : 0;
+  if constexpr (FEW) {
+    for (int i = threadIdx.x; i < kFewPairs; i += blockDim.x) key[i] = 0x7fffffff;
+    __syncthreads();
   }
-  int32_t expert = -1;
-  float mine = -INFINITY, top = -INFINITY;
-  for (int j = 0; j < a.k; ++j) {
-    uint32_t m = o[0];
+  if (real) {
+    const IN* l = (const IN*)a.logits + row * a.ld;
+    float logit[HOLD];
+    uint32_t o[HOLD];
 #pragma unroll
-    for (int i = 1; i < HOLD; ++i) m = max(m, o[i]);
-    const uint32_t most = lanes_reduce<LANES>(m, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    if (j == 0) top = value_of(most);
-    uint64_t have = __ballot(m == most) >> base;
-    if (LANES < 64) have &= (1ull << (LANES & 63)) - 1;
-    const int winner = __ffsll((unsigned long long)have) - 1;  // of equal ones the lowest: a lane's experts are neighbours
-    int at = 0;
-#pragma unroll
-    for (int i = HOLD - 1; i >= 0; --i) at = o[i] == most ? i : at;
-    const int32_t chosen = __shfl(lane * HOLD + at, base + winner, 64);
-    if (lane == winner) {
-#pragma unroll
-      for (int i = 0; i < HOLD; ++i) o[i] = i == at ? 0u : o[i];
+    for (int j = 0; j < HOLD; ++j) {
+      const int e = lane * HOLD + j;
+      logit[j] = e < a.experts ? wide(l[e]) : -INFINITY;
+      o[j] = e < a.experts ? ordered(logit[j]) : 0u;
     }
-    if (lane == j && most > kMasked) expert = chosen, mine = value_of(most);
-  }
-  const float shift = top == -INFINITY ? 0.f : top;
-  float e = expert >= 0 ? expf(mine - shift) : 0.f, part = e;
-  if (!a.normalise) {
-    part = 0.f;
+    float mine = -INFINITY, top = -INFINITY;
+    for (int j = 0; j < a.k; ++j) {
+      uint32_t m = o[0];
 #pragma unroll
-    for (int j = 0; j < HOLD; ++j) part += expf(logit[j] - shift);
+      for (int i = 1; i < HOLD; ++i) m = max(m, o[i]);
+      const uint32_t most = group_reduce<LANES>(m, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+      if (j == 0) top = value_of(most);
+      uint64_t have = __ballot(m == most) >> base;
+      if (LANES < 64) have &= (1ull << (LANES & 63)) - 1;
+      if (lane == __ffsll((unsigned long long)have) - 1) {  // of equal ones the lowest: a lane's experts are neighbours
+        int at = 0;
+#pragma unroll
+        for (int i = HOLD - 1; i >= 0; --i) at = o[i] == most ? i : at;
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i) o[i] = i == at ? 0u : o[i];
+        const int32_t chosen = most > kMasked ? lane * HOLD + at : -1;
+        a.expert[row * a.k + j] = chosen;
+        if constexpr (FEW) key[row * a.k + j] = chosen >= 0 ? chosen : a.experts;
+      }
+      if (lane == j && most > kMasked) mine = value_of(most);
+    }
+    const float shift = top == -INFINITY ? 0.f : top;
+    const bool live = mine != -INFINITY;
+    const float e = live ? expf(mine - shift) : 0.f;
+    float part = e;
+    if (!a.normalise) {
+      part = 0.f;
+#pragma unroll
+      for (int j = 0; j < HOLD; ++j) part += expf(logit[j] - shift);
+    }
+    const float total = group_reduce<LANES>(part, [](float x, float y) { return x + y; });
+    if (lane < a.k) a.weight[row * a.k + lane] = live ? e / total : 0.f;
   }
-  const float total = lanes_reduce<LANES>(part, [](float x, float y) { return x + y; });
-  if (lane < a.k) {
-    a.expert[row * a.k + lane] = expert;
-    a.weight[row * a.k + lane] = expert >= 0 ? e / total : 0.f;
+  if constexpr (FEW) {
+    __syncthreads();
+    const int groups = (pairs + 3) / 4;
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+      const int mine = key[i];
+      int before = 0;
+      for (int g = 0; g < groups; ++g) {
+        const int4 q = keys[g];
+        before += (q.x < mine || (q.x == mine && 4 * g < i)) + (q.y < mine || (q.y == mine && 4 * g + 1 < i)) +
+                  (q.z < mine || (q.z == mine && 4 * g + 2 < i)) + (q.w < mine || (q.w == mine && 4 * g + 3 < i));
+      }
+      order.place[i] = mine < a.experts ? before : -1;
+      order.order[before] = mine < a.experts ? i : -1;
+    }
+    for (int v = threadIdx.x; v <= a.experts; v += blockDim.x) {
+      int before = 0;
+      for (int g = 0; g < groups; ++g) {
+        const int4 q = keys[g];
+        before += (q.x < v) + (q.y < v) + (q.z < v) + (q.w < v);
+      }
+      order.row_ptr[v] = before;
+    }
   }
 }
 
-template <class IN> hipError_t launch_choice(const Choice& a, hipStream_t s) {
+// Whether one workgroup has lanes for all rows.
+bool few_rows(int32_t rows, int lanes, int32_t k) { return (int64_t)rows * lanes <= 1024 && (int64_t)rows * k <= kFewPairs; }
+
+// The choice, and where rows are few the order too (`ordered`).
+template <class IN> hipError_t launch_choice(const Choice& a, const Order& order, bool& ordered, hipStream_t s) {
   const auto go = [&](auto lanes, auto hold) {
     constexpr int L = decltype(lanes)::value, H = decltype(hold)::value;
-    hipLaunchKernelGGL((rfast_route_choice<IN, L, H>), rfast_grid_of(((int64_t)a.rows * L + kThreads - 1) / kThreads), dim3(kThreads), 0, s, a);
+    ordered = few_rows(a.rows, L, a.k);
+    if (ordered) {
+      const int threads = (a.rows * L + 63) / 64 * 64;
+      hipLaunchKernelGGL((rfast_route_choice<IN, L, H, true>), dim3(1), dim3(threads), 0, s, a, order);
+    } else {
+      hipLaunchKernelGGL((rfast_route_choice<IN, L, H, false>), rfast_grid_of(((int64_t)a.rows * L + kThreads - 1) / kThreads), dim3(kThreads), 0, s, a,
+                         order);
+    }
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -156,12 +202,13 @@ template <class IN, class OUT> __global__ void __launch_bounds__(kThreads) rfast
     if (total == 0.f) total = 1.f;  // (a row of masked experts)
   }
   OUT* out = (OUT*)a.dlogits + row * a.ld_out;
+  const float given = a.normalise ? wd - w * mean : wd;
   for (int first = 0; first < a.experts; first += 64) {
     const int e = first + lane;
     float g = a.normalise || e >= a.experts ? 0.f : -mean * (expf(wide(l[e]) - shift) / total);
     for (int j = 0; j < a.k; ++j) {
-      const int32_t chosen = __shfl(expert, j, 64);
-      const float add_j = __shfl(a.normalise ? wd - w * mean : wd, j, 64);
+      const int32_t chosen = __builtin_amdgcn_readlane(expert, j);
+      const float add_j = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(given), j));
       g += chosen == e ? add_j : 0.f;
     }
     if (e < a.experts) narrow(out + e, g);
@@ -414,8 +461,11 @@ extern "C" int rfast_route(int32_t rows, int32_t experts, int32_t k, const void*
   const hipStream_t s = (hipStream_t)hip_stream;
   if (rows) {
     const Choice a = {logits, expert, weight, ld_logits, rows, experts, k, normalise};
-    const hipError_t e = logits_type == RFAST_F32 ? launch_choice<float>(a, s) : launch_choice<u16>(a, s);
+    const Order order_of = {row_ptr, place, order};
+    bool ordered = false;
+    const hipError_t e = logits_type == RFAST_F32 ? launch_choice<float>(a, order_of, ordered, s) : launch_choice<u16>(a, order_of, ordered, s);
     if (e != hipSuccess) return rfast_refuse_hip(e, "router launch");
+    if (ordered) return RFAST_OK;
   }
   return plan(pairs, experts, expert, row_ptr, place, order, workspace, s);
 }
