@@ -28,23 +28,6 @@ struct Lookup {
   float scale;
 };
 
-// LANES lanes take a row, eight columns each at a time; wide rows are cut into slabs of 512 columns, a wavefront each.
-template <class IN, class OUT, int LANES> __global__ void __launch_bounds__(kThreads) rfast_embedding_kernel(Lookup a, int slabs) {
-  const int64_t unit = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x) / LANES;
-  const int64_t row = unit / slabs;
-  if (row >= a.rows) return;
-  const int col = ((int)(unit % slabs) * LANES + threadIdx.x % LANES) * 8;
-  if (col >= a.d) return;
-  const int32_t token = a.tokens[row];
-  float v[8] = {};
-  if ((uint32_t)token < (uint32_t)a.vocabulary) {
-    load_eight<false>((const IN*)a.table + token * a.ld_table + col, a.d - col, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= a.scale;
-  }
-  store_eight<false>((OUT*)a.out + row * a.ld_out + col, a.d - col, v);
-}
-
 struct Back {
   const void* dy;
   const int32_t* sorted;  // [rows] tokens in order, `vocabulary` for padding
@@ -65,6 +48,25 @@ template <int LANES, bool WHOLE> __device__ inline Spot spot_of(int32_t d, int s
   const int col = (slab * LANES + threadIdx.x % LANES) * 8;
   if (WHOLE) return {min(col, d - 8), 8, max(col - (d - 8), 0)};
   return {col, d - col, 0};
+}
+
+// LANES lanes take a row, eight columns each; rows of more than 512 columns are cut into slabs, a wavefront each.  Rows of 16 bits go past the
+// caches (8001 x 4096: 19.8 -> 18.5 us; two or four rows to a lane changed nothing); in 32 bits, where a lane stores two halves of 32 bytes, that
+// would cost (65536 x 480: 32 -> 39).
+template <class IN, class OUT, int LANES, bool WHOLE> __global__ void __launch_bounds__(kThreads) rfast_embedding_kernel(Lookup a, int slabs) {
+  const int64_t unit = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x) / LANES;
+  const int64_t row = unit / slabs;
+  if (row >= a.rows) return;
+  const Spot s = spot_of<LANES, WHOLE>(a.d, (int)(unit - row * slabs));
+  if (s.again >= 8 || s.left <= 0) return;
+  const int32_t token = a.tokens[row];
+  float v[8] = {};
+  if ((uint32_t)token < (uint32_t)a.vocabulary) {
+    load_eight<false>((const IN*)a.table + token * a.ld_table + s.col, s.left, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= a.scale;
+  }
+  store_eight<sizeof(OUT) == 2>((OUT*)a.out + row * a.ld_out + s.col, s.left, v);
 }
 
 template <class OUT, bool ADD> __device__ inline void store_sum(OUT* grad, const Spot& s, float scale, const float* sum, const float* had) {
@@ -222,15 +224,16 @@ extern "C" int rfast_embedding(int32_t rows, int32_t vocabulary, int32_t d, cons
     return rfast_refuse(RFAST_EINVAL, "the output overlaps an input");
   const Lookup a = {table, tokens, out, ld_table, ld_out, rows, vocabulary, d, scale};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const hipError_t e = by_lanes(d, [&](auto lanes, auto) {
+  const hipError_t e = by_lanes(d, [&](auto lanes, auto whole) {
     constexpr int L = decltype(lanes)::value;
+    constexpr bool W = decltype(whole)::value;
     const int slabs = slabs_of(d);
     const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
     const bool tf = table_type == RFAST_F32, of = out_type == RFAST_F32;
-    if (tf && of) hipLaunchKernelGGL((rfast_embedding_kernel<float, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else if (tf) hipLaunchKernelGGL((rfast_embedding_kernel<float, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else if (of) hipLaunchKernelGGL((rfast_embedding_kernel<u16, float, L>), grid, dim3(kThreads), 0, s, a, slabs);
-    else hipLaunchKernelGGL((rfast_embedding_kernel<u16, u16, L>), grid, dim3(kThreads), 0, s, a, slabs);
+    if (tf && of) hipLaunchKernelGGL((rfast_embedding_kernel<float, float, L, W>), grid, dim3(kThreads), 0, s, a, slabs);
+    else if (tf) hipLaunchKernelGGL((rfast_embedding_kernel<float, u16, L, W>), grid, dim3(kThreads), 0, s, a, slabs);
+    else if (of) hipLaunchKernelGGL((rfast_embedding_kernel<u16, float, L, W>), grid, dim3(kThreads), 0, s, a, slabs);
+    else hipLaunchKernelGGL((rfast_embedding_kernel<u16, u16, L, W>), grid, dim3(kThreads), 0, s, a, slabs);
     return hipGetLastError();
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "embedding launch");

@@ -271,8 +271,8 @@ template <int LANES, bool WHOLE> __global__ void __launch_bounds__(kThreads) rfa
   }
 }
 
-// AT_ONCE choices' rows are under way together; one without a place reads row 0 and counts for nothing.
-template <class IN, class OUT, int LANES, bool WHOLE, int AT_ONCE>
+// AT_ONCE choices' rows are under way together; one without a place reads row 0 and counts for nothing.  FAR: the rows are read past the caches.
+template <class IN, class OUT, int LANES, bool WHOLE, int AT_ONCE, bool FAR>
 __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, int slabs) {
   const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
   if (!s.in) return;
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, i
         const int32_t from = place[j];
         live[i] = first + i < a.k && (uint32_t)from < (uint32_t)a.sorted_rows;
         w[i] = weight ? weight[j] : 1.f;
-        load_eight<true>((const IN*)a.in + (live[i] ? from : 0) * a.ld_in + s.col, s.left, v[i]);
+        load_eight<FAR>((const IN*)a.in + (live[i] ? from : 0) * a.ld_in + s.col, s.left, v[i]);
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i)
@@ -300,12 +300,15 @@ __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, i
   store_eight<false>((OUT*)a.out + s.row * a.ld_out + s.col, s.left, y);
 }
 
-// A workgroup of WAVES wavefronts per row, AT_ONCE choices at a time: a choice's product with dy is a sum over the workgroup.
-template <class T, int WAVES, bool WHOLE, int AT_ONCE> __global__ void __launch_bounds__(64 * WAVES) rfast_route_combine_back(Rows a) {
-  __shared__ float box[kChoicesMost][WAVES];
-  const int64_t row = block_number();
+// AT_ONCE choices at a time, LANES lanes per row, or the whole workgroup (LANES = 256), whose wavefronts' sums meet in LDS.
+template <class T, int LANES, bool WHOLE, int AT_ONCE, bool FAR> __global__ void __launch_bounds__(kThreads) rfast_route_combine_back(Rows a) {
+  constexpr int WAVES = LANES > 64 ? LANES / 64 : 1;
+  __shared__ float box[LANES > 64 ? kChoicesMost : 1][WAVES];
+  int64_t row = (block_number() * kThreads + threadIdx.x) / LANES;
+  if constexpr (LANES >= 64)
+    row = (int64_t)__builtin_amdgcn_readfirstlane((int)(row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)row);
   if (row >= a.rows) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x % LANES;
   const T* dy = (const T*)a.dy + row * a.ld_dy;
   const bool dots = a.dweight && a.sorted_rows > 0;
   for (int first = 0; first < a.k; first += AT_ONCE) {
@@ -321,14 +324,14 @@ template <class T, int WAVES, bool WHOLE, int AT_ONCE> __global__ void __launch_
       w[i] = a.weight ? a.weight[row * a.k + j] : 1.f;
       dot[i] = 0.f;
     }
-    for (int64_t begin = threadIdx.x * 8; begin < a.d; begin += 64 * WAVES * 8) {
+    for (int64_t begin = lane * 8; begin < a.d; begin += LANES * 8) {
       const int col = WHOLE ? (int)min(begin, (int64_t)a.d - 8) : (int)begin, left = WHOLE ? 8 : a.d - col;
       const int again = (int)begin - col;  // columns that the group before has too
       float g[8], v[AT_ONCE][8];
       load_eight<false>(dy + col, left, g);
       if (dots) {
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) load_eight<true>((const T*)a.in + at[i] * a.ld_in + col, left, v[i]);
+        for (int i = 0; i < AT_ONCE; ++i) load_eight<FAR>((const T*)a.in + at[i] * a.ld_in + col, left, v[i]);
       }
       if (a.out) {
 #pragma unroll
@@ -336,7 +339,7 @@ template <class T, int WAVES, bool WHOLE, int AT_ONCE> __global__ void __launch_
           float o[8];
 #pragma unroll
           for (int c = 0; c < 8; ++c) o[c] = w[i] * g[c];
-          if (live[i]) store_eight<true>((T*)a.out + at[i] * a.ld_out + col, left, o);
+          if (live[i]) store_eight<false>((T*)a.out + at[i] * a.ld_out + col, left, o);
         }
       }
       if (dots) {
@@ -357,18 +360,25 @@ template <class T, int WAVES, bool WHOLE, int AT_ONCE> __global__ void __launch_
     if (a.dweight) {
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        const float sum = wave_reduce(live[i] ? dot[i] : 0.f, [](float x, float y) { return x + y; });
-        if (lane == 0 && first + i < a.k) box[first + i][wave] = sum;
+        const float sum = group_reduce<(LANES < 64 ? LANES : 64)>(live[i] ? dot[i] : 0.f, [](float x, float y) { return x + y; });
+        if (first + i >= a.k) continue;
+        if constexpr (LANES > 64) {
+          if ((lane & 63) == 0) box[first + i][lane >> 6] = sum;
+        } else {
+          if (lane == 0) a.dweight[row * a.k + first + i] = sum;
+        }
       }
     }
   }
-  if (!a.dweight) return;
-  __syncthreads();
-  if (threadIdx.x < a.k) {
-    float sum = 0.f;
+  if constexpr (LANES > 64) {
+    if (!a.dweight) return;
+    __syncthreads();
+    if (lane < a.k) {
+      float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += box[threadIdx.x][w];
-    a.dweight[row * a.k + threadIdx.x] = sum;
+      for (int w = 0; w < WAVES; ++w) sum += box[lane][w];
+      a.dweight[row * a.k + lane] = sum;
+    }
   }
 }
 
@@ -391,6 +401,13 @@ template <class F> hipError_t by_choices(int32_t k, F go) {
 
 RfastArea area(const void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) { return {p, rows, ld * bytes, columns * bytes}; }
 RfastArea area(const void* p, int64_t count) { return {p, 1, count * 4, count * 4}; }
+
+// Rows of 16 bits that begin at multiples of 16 bytes and are more than the last-level cache (256 MB) holds are read past the caches: 8192 x 4
+// of 4096 return in 56 us so and in 61 otherwise, their gradient takes 97 and 107; 30000 x 2 of 192, which the cache holds, return in 10.9
+// so and in 8.2 otherwise, and in 32 bits, where a lane reads two halves of 32 bytes, it costs whatever the size (4096 x 8 of 2048: 61 and 56).
+bool is_far(const void* sorted, int64_t pairs, int64_t ld, int64_t d, int bytes) {
+  return bytes == 2 && pairs * d * bytes >= (int64_t)1 << 28 && (uintptr_t)sorted % 16 == 0 && ld % 8 == 0;
+}
 
 bool counts_ok(int32_t rows, int32_t k, int32_t d, int32_t sorted_rows) {
   return rows >= 0 && k >= 1 && k <= kChoicesMost && d >= 1 && d <= kColumnsMost && sorted_rows >= 0 && (int64_t)rows * k <= 0x7fffffff;
@@ -538,18 +555,24 @@ extern "C" int rfast_route_combine(int32_t rows, int32_t k, int32_t d, const voi
   if (const int bad = apart(in, 3, out, 1)) return bad;
   const Rows a = {sorted, place, weight, nullptr, y, nullptr, ld_sorted, 0, ld_y, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
+  const bool far = is_far(sorted, pairs, ld_sorted, d, w);
   const hipError_t e = by_lanes(d, [&](auto lanes, auto whole) {
     return by_choices(k, [&](auto choices) {
       constexpr int L = decltype(lanes)::value, C = decltype(choices)::value;
       constexpr bool W = decltype(whole)::value;
       const int slabs = (int)(((int64_t)d + 511) / 512);
       const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
-      const bool tf = type == RFAST_F32, yf = y_type == RFAST_F32;
-      if (tf && yf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, float, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
-      else if (tf) hipLaunchKernelGGL((rfast_route_combine_kernel<float, u16, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
-      else if (yf) hipLaunchKernelGGL((rfast_route_combine_kernel<u16, float, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
-      else hipLaunchKernelGGL((rfast_route_combine_kernel<u16, u16, L, W, C>), grid, dim3(kThreads), 0, s, a, slabs);
-      return hipGetLastError();
+      const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, slabs);
+        return hipGetLastError();
+      };
+      const bool yf = y_type == RFAST_F32;
+      if (type == RFAST_F32)
+        return yf ? go(rfast_route_combine_kernel<float, float, L, W, C, false>) : go(rfast_route_combine_kernel<float, u16, L, W, C, false>);
+      if constexpr (L == 64) {
+        if (far) return yf ? go(rfast_route_combine_kernel<u16, float, L, W, C, true>) : go(rfast_route_combine_kernel<u16, u16, L, W, C, true>);
+      }
+      return yf ? go(rfast_route_combine_kernel<u16, float, L, W, C, false>) : go(rfast_route_combine_kernel<u16, u16, L, W, C, false>);
     });
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return launch");
@@ -574,17 +597,25 @@ extern "C" int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, 
   if (const int bad = apart(in, 4, out, 2)) return bad;
   const Rows a = {sorted, place, weight, dy, writes ? dsorted : nullptr, dweight, ld_sorted, ld_dy, ld_dsorted, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const dim3 grid = rfast_grid_of(rows);
+  const bool far = reads && is_far(sorted, pairs, ld_sorted, d, w);
   const hipError_t e = by_choices(k, [&](auto choices) {
     constexpr int C = decltype(choices)::value;
-    const auto go = [&](auto kernel, int threads) {
-      hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
-      return hipGetLastError();
+    const auto types = [&](auto lanes, auto whole) {
+      constexpr int L = decltype(lanes)::value;
+      constexpr bool W = decltype(whole)::value;
+      const dim3 grid = rfast_grid_of(((int64_t)rows * L + kThreads - 1) / kThreads);
+      const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+      };
+      if (type == RFAST_F32) return go(rfast_route_combine_back<float, L, W, C, false>);
+      if constexpr (L >= 64) {
+        if (far) return go(rfast_route_combine_back<u16, L, W, C, true>);
+      }
+      return go(rfast_route_combine_back<u16, L, W, C, false>);
     };
-    const bool f = type == RFAST_F32;
-    if (d < 8) return f ? go(rfast_route_combine_back<float, 1, false, C>, 64) : go(rfast_route_combine_back<u16, 1, false, C>, 64);
-    if (d <= 1024) return f ? go(rfast_route_combine_back<float, 1, true, C>, 64) : go(rfast_route_combine_back<u16, 1, true, C>, 64);
-    return f ? go(rfast_route_combine_back<float, 4, true, C>, 256) : go(rfast_route_combine_back<u16, 4, true, C>, 256);
+    if (d > 1024) return types(std::integral_constant<int, 256>(), std::true_type());  // (a wavefront alone would go round three times and more)
+    return by_lanes(d, types);
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return gradient launch");
 }
