@@ -249,8 +249,8 @@ template <int LANES, bool WHOLE> __device__ inline Spot spot_of(int32_t rows, in
   return s;
 }
 
-// Units of 2 bytes, whatever the type.
-template <int LANES, bool WHOLE> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
+// Units of 2 bytes, whatever the type.  FAR: the copies are written past the caches.
+template <int LANES, bool WHOLE, bool FAR> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
   const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
   if (!s.in) return;
   const u16* x = (const u16*)a.in + s.row * a.ld_in + s.col;
@@ -264,7 +264,7 @@ template <int LANES, bool WHOLE> __global__ void __launch_bounds__(kThreads) rfa
     const int32_t to = place[j];
     if ((uint32_t)to >= (uint32_t)a.sorted_rows) continue;
     u16* out = (u16*)a.out + to * a.ld_out + s.col;
-    if constexpr (WHOLE) wide_store<any_u32x4, true>(out, v);
+    if constexpr (WHOLE) wide_store<any_u32x4, FAR>(out, v);
     else
       for (int i = 0; i < 8; ++i)
         if (i < s.left) out[i] = few[i];
@@ -405,8 +405,10 @@ RfastArea area(const void* p, int64_t count) { return {p, 1, count * 4, count * 
 // Rows of 16 bits that begin at multiples of 16 bytes and are more than the last-level cache (256 MB) holds are read past the caches: 8192 x 4
 // of 4096 return in 56 us so and in 61 otherwise, their gradient takes 97 and 107; 30000 x 2 of 192, which the cache holds, return in 10.9
 // so and in 8.2 otherwise, and in 32 bits, where a lane reads two halves of 32 bytes, it costs whatever the size (4096 x 8 of 2048: 61 and 56).
+// The dispatch writes units of 16 bytes whatever the type: 8192 x 8 rows of 8 KB in 99 us past the caches and in 114 otherwise, 60000 x 4 of 66 bytes
+// in 12.4 and 8.4.
 bool is_far(const void* sorted, int64_t pairs, int64_t ld, int64_t d, int bytes) {
-  return bytes == 2 && pairs * d * bytes >= (int64_t)1 << 28 && (uintptr_t)sorted % 16 == 0 && ld % 8 == 0;
+  return bytes == 2 && pairs * d * 2 >= (int64_t)1 << 28 && (uintptr_t)sorted % 16 == 0 && ld % 8 == 0;
 }
 
 bool counts_ok(int32_t rows, int32_t k, int32_t d, int32_t sorted_rows) {
@@ -534,9 +536,15 @@ extern "C" int rfast_route_gather(int32_t rows, int32_t k, int32_t d, const void
     constexpr int L = decltype(lanes)::value;
     constexpr bool W = decltype(whole)::value;
     const int slabs = (int)((columns + 511) / 512);
-    hipLaunchKernelGGL((rfast_route_gather_kernel<L, W>), rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0,
-                       (hipStream_t)hip_stream, a, slabs);
-    return hipGetLastError();
+    const auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0, (hipStream_t)hip_stream, a,
+                         slabs);
+      return hipGetLastError();
+    };
+    if constexpr (L == 64) {
+      if (is_far(sorted, (int64_t)rows * k, a.ld_out, columns, 2)) return go(rfast_route_gather_kernel<L, W, true>);
+    }
+    return go(rfast_route_gather_kernel<L, W, false>);
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "dispatch launch");
 }
