@@ -339,7 +339,7 @@ template <class T, int LANES, bool WHOLE, int AT_ONCE, bool FAR> __global__ void
           float o[8];
 #pragma unroll
           for (int c = 0; c < 8; ++c) o[c] = w[i] * g[c];
-          if (live[i]) store_eight<false>((T*)a.out + at[i] * a.ld_out + col, left, o);
+          if (live[i]) store_eight<FAR>((T*)a.out + at[i] * a.ld_out + col, left, o);
         }
       }
       if (dots) {
