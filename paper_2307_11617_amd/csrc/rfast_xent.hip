@@ -70,17 +70,13 @@ template <> struct Group<u16> {
   }
   __device__ float at(int j) const { return __uint_as_float(j & 1 ? raw[j >> 1] & 0xFFFF0000u : raw[j >> 1] << 16); }
 };
-template <int N> __device__ inline void store_group(float* p, const float* v) {
+template <int N, bool FAR = false> __device__ inline void store_group(float* p, const float* v) {
 #pragma unroll
-  for (int q = 0; q < N; q += 4) store_four<false>(p + q, 4, v + q);
+  for (int q = 0; q < N; q += 4) store_four<FAR>(p + q, 4, v + q);
 }
-template <int N> __device__ inline void store_group(u16* p, const float* v) {
-  if constexpr (N == 8) {
-    const any_u32x4 t = {to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3]), to_bf16_pair(v[4], v[5]), to_bf16_pair(v[6], v[7])};
-    *reinterpret_cast<any_u32x4*>(p) = t;
-  } else {
-    store_four<false>(p, 4, v);
-  }
+template <int N, bool FAR = false> __device__ inline void store_group(u16* p, const float* v) {
+  if constexpr (N == 8) store_eight<FAR>(p, 8, v);
+  else store_four<FAR>(p, 4, v);
 }
 
 // Over the row's lanes: LANES neighbours of a wavefront, or a workgroup's through `box`.
@@ -148,7 +144,7 @@ template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane,
 // overlap at the ends of a row: group h begins at 8 h - m, moved into [0, K - 8] (4 instead of 8 in 32 bits), where m is how far a row of
 // a workgroup's begins behind a multiple of 16 bytes, so that all but the first and last group are aligned (4096 rows of 50001: 184 us with
 // m = 0, 152 so).  What a group shares with the one before is left out of its sum, and its gradient is written twice alike.
-template <class IN, class OUT, int LANES, int GROUPS, bool POLICY>
+template <class IN, class OUT, int LANES, int GROUPS, bool POLICY, bool FAR>
 __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 1) rfast_xent_kernel(Args a) {
   constexpr int N = Group<IN>::N, ROWS = LANES <= 64 ? 256 / LANES : 1, SPAN = LANES * N;
   __shared__ float box[2][16];
@@ -229,7 +225,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
     }
     if (h * N - m >= a.K) continue;
     if (LANES > 8 || GROUPS > 1 || last >= 0) {
-      store_group<N>(grad + at, g);
+      store_group<N, FAR>(grad + at, g);
     } else {
 #pragma unroll
       for (int j = 0; j < N; j += 4)
@@ -308,9 +304,17 @@ __global__ void __launch_bounds__(1024) rfast_xent_long_kernel(Args a) {
 
 template <class IN, class OUT, bool POLICY> hipError_t launch(const Args& a, hipStream_t s) {
   constexpr int N = Group<IN>::N;
+  const bool far = a.grad && (int64_t)a.rows * a.K * (int64_t)sizeof(OUT) >= (int64_t)1 << 28;
   const auto go = [&](auto lanes, auto groups) {
     constexpr int L = decltype(lanes)::value, G = decltype(groups)::value, rows = L <= 64 ? 256 / L : 1;
-    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G, POLICY>), rfast_grid_of(((int64_t)a.rows + rows - 1) / rows), dim3(L <= 64 ? 256 : L), 0, s, a);
+    const dim3 grid = rfast_grid_of(((int64_t)a.rows + rows - 1) / rows), block(L <= 64 ? 256 : L);
+    if constexpr (L > 64 && N * sizeof(OUT) == 16) {
+      if (far) {
+        hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G, POLICY, true>), grid, block, 0, s, a);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((rfast_xent_kernel<IN, OUT, L, G, POLICY, false>), grid, block, 0, s, a);
     return hipGetLastError();
   };
   using std::integral_constant;
