@@ -525,14 +525,14 @@ void rfast_adamw_destroy(rfast_adamw* h);
  * term).  weight: device fp32 [rows] or NULL (1); a row of weight 0 has loss and gradient 0 whatever its other numbers.  loss, logp: device fp32 [rows] or NULL (not wanted).
  * An action at a masked class of another row: logp -infinity, r 0, gradient 0 (loss +infinity where beta > 0 and there is a reference).
  * Numbers that 32 bits do not hold (an r A or exp(q) beyond 3.4e38 that counts) make the row's loss infinite and its gradient not finite.
- * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0, all finite (RFAST_ERANGE). */
+ * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0 and grad_scale, all finite (RFAST_ERANGE). */
 int rfast_policy_loss(int32_t rows, int32_t K, const void* logits, int32_t logits_type, int64_t ld_logits, const int32_t* actions,
                       const float* old_logp, const float* advantage, const float* reference, const float* weight, float clip_low,
                       float clip_high, float beta, float grad_scale, float* loss, float* logp, void* grad, int32_t grad_type,
                       int64_t ld_grad, const int32_t* d_rows, void* hip_stream);
 
 /* Rows of a table of embeddings: out_t = scale table[token_t], rounded once.  table: device [vocabulary][ld_table >= d].  tokens: device int32
- * [rows]; one outside [0, vocabulary) (-1 by convention) is padding: a row of zeros.  out: device [rows][ld_out >= d]. */
+ * [rows]; one outside [0, vocabulary) (-1 by convention) is padding: a row of zeros.  out: device [rows][ld_out >= d].  scale: finite (RFAST_ERANGE). */
 int rfast_embedding(int32_t rows, int32_t vocabulary, int32_t d, const void* table, int32_t table_type, int64_t ld_table,
                     const int32_t* tokens, float scale, void* out, int32_t out_type, int64_t ld_out, void* hip_stream);
 /* Its gradient: grad_v = scale sum of dy_t over the rows with token_t = v, in 32 bits in an order that the tokens alone decide (the same call

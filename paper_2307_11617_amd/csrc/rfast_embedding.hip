@@ -213,6 +213,7 @@ extern "C" int rfast_embedding(int32_t rows, int32_t vocabulary, int32_t d, cons
                                const int32_t* tokens, float scale, void* out, int32_t out_type, int64_t ld_out, void* hip_stream) {
   if (!sizes_ok(rows, vocabulary, d)) return rfast_refuse(RFAST_EINVAL, "need rows >= 0, vocabulary >= 1 and d 1 .. 2^31 - 1024");
   if (!rfast_type_ok(table_type) || !rfast_type_ok(out_type)) return rfast_refuse(RFAST_EINVAL, "types must be RFAST_F32 or RFAST_BF16");
+  if (!(scale > -INFINITY && scale < INFINITY)) return rfast_refuse(RFAST_ERANGE, "scale must be finite");
   if (rows == 0) return RFAST_OK;
   if (!table || !tokens || !out) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   if (ld_table < d || ld_out < d) return rfast_refuse(RFAST_EINVAL, "rows are at least d elements apart");
@@ -248,6 +249,7 @@ extern "C" int rfast_embedding_backward(int32_t rows, int32_t vocabulary, int32_
                                         void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (!sizes_ok(rows, vocabulary, d)) return rfast_refuse(RFAST_EINVAL, "need rows >= 0, vocabulary >= 1 and d 1 .. 2^31 - 1024");
   if (!rfast_type_ok(dy_type) || !rfast_type_ok(grad_type)) return rfast_refuse(RFAST_EINVAL, "types must be RFAST_F32 or RFAST_BF16");
+  if (!(scale > -INFINITY && scale < INFINITY)) return rfast_refuse(RFAST_ERANGE, "scale must be finite");
   if (accumulate != 0 && accumulate != 1) return rfast_refuse(RFAST_EINVAL, "accumulate must be 0 or 1");
   if (!grad || (rows && (!dy || !tokens))) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   if (ld_grad < d || (rows && ld_dy < d)) return rfast_refuse(RFAST_EINVAL, "rows are at least d elements apart");

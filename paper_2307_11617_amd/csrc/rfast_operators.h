@@ -36,8 +36,8 @@ struct RfastFill {
 };
 // A matrix of elements of `bytes` bytes.
 inline RfastFill rfast_fill_of(void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) {
-  const int64_t half = bytes / 2, all = rows * columns * half, piece = 1 << 12;
-  if (ld == columns && all > 0) {  // one piece of memory: in parts of 8 KB, whatever the rows
+  const int64_t half = bytes / 2, all = rows * columns * half, piece = 1 << 13;
+  if (ld == columns && all > 0) {  // one piece of memory: in parts of 16 KB, whatever the rows
     const int64_t parts = (all + piece - 1) / piece;
     return {(u16*)p, parts, piece, piece, all - (parts - 1) * piece};
   }

@@ -388,8 +388,9 @@ extern "C" int rfast_policy_loss(int32_t rows, int32_t K, const void* logits, in
                                  int32_t grad_type, int64_t ld_grad, const int32_t* d_rows, void* hip_stream) {
   const int bad = check(rows, K, logits, logits_type, ld_logits, actions, grad, grad_type, ld_grad, d_rows);
   if (bad != RFAST_OK) return bad;
-  if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f && clip_high < INFINITY && beta >= 0.f && beta < INFINITY))
-    return rfast_refuse(RFAST_ERANGE, "need 0 <= clip_low <= 1, clip_high >= 0 and beta >= 0, all finite");
+  if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f && clip_high < INFINITY && beta >= 0.f && beta < INFINITY &&
+        grad_scale > -INFINITY && grad_scale < INFINITY))
+    return rfast_refuse(RFAST_ERANGE, "need 0 <= clip_low <= 1, clip_high >= 0, beta >= 0 and grad_scale, all finite");
   if (rows == 0) return RFAST_OK;
   if (!old_logp || !advantage) return rfast_refuse(RFAST_EINVAL, "NULL argument");
   const void* in[] = {actions, old_logp, advantage, reference, weight, d_rows};

@@ -76,6 +76,13 @@ def _matrix(t, name, rows, cols, dtype, device):
     return t.stride(0) if rows > 1 else max(cols, 1)
 
 
+def _new(device, dtype, rows, cols=None):
+    """An uninitialised tensor (with strides given torch is a third faster than without: 1.3 us)."""
+    if cols is None:
+        return _torch.empty_strided((rows,), (1,), dtype=dtype, device=device)
+    return _torch.empty_strided((rows, cols), (cols or 1, 1), dtype=dtype, device=device)
+
+
 def _vector(t, name, count, dtype, device):
     if t.dtype != dtype or t.device != device or t.numel() != count or not t.is_contiguous():
         raise RFastError(-1, f"{name}: need a contiguous {dtype} tensor of {count} elements on {device}")
@@ -132,11 +139,11 @@ def rfast_policy_loss(logits, actions, old_logp, advantage, reference=None, weig
     given = (_vector(actions, "actions", T, torch.int32, dev), _vector(old_logp, "old_logp", T, f32, dev), _vector(advantage, "advantage", T, f32, dev),
              None if reference is None else _vector(reference, "reference", T, f32, dev),
              None if weight is None else _vector(weight, "weight", T, f32, dev))
-    loss = torch.empty(T, dtype=f32, device=dev) if loss is None else loss
+    loss = _new(dev, f32, T) if loss is None else loss
     p_loss = _vector(loss, "loss", T, f32, dev)
     p_logp = None if logp is None else _vector(logp, "logp", T, f32, dev)
     if grad is None:
-        grad = torch.empty((T, K), dtype=grad_dtype or logits.dtype, device=dev)
+        grad = _new(dev, grad_dtype or logits.dtype, T, K)
         ldg, gt, p_grad = K, _type(grad, "grad"), grad.data_ptr()
     elif grad is False:
         grad, p_grad, gt, ldg = None, None, F32, 0
@@ -159,7 +166,7 @@ def rfast_embedding(table, tokens, scale=1.0, out=None, out_dtype=None):
     _sizes(T, V, d)
     ld = _matrix(table, "table", V, d, None, dev)
     if out is None:
-        out, ld_out = torch.empty((T, d), dtype=out_dtype or table.dtype, device=dev), max(d, 1)
+        out, ld_out = _new(dev, out_dtype or table.dtype, T, d), max(d, 1)
     else:
         _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
         ld_out = _matrix(out, "out", T, d, None, dev)
@@ -185,12 +192,12 @@ def rfast_embedding_backward(dy, tokens, vocabulary, scale=1.0, grad=None, grad_
     if grad is None:
         _need(not accumulate, "accumulate: need the gradient to add to")
         _need(V >= 1, "need a vocabulary of at least one")
-        grad, ld_grad = torch.empty((V, d), dtype=grad_dtype or torch.float32, device=dev), max(d, 1)
+        grad, ld_grad = _new(dev, grad_dtype or torch.float32, V, d), max(d, 1)
     else:
         _need(grad_dtype is None or grad.dtype == grad_dtype, "grad: its type is not grad_dtype")
         ld_grad = _matrix(grad, "grad", V, d, None, dev)
     nbytes = rfast_embedding_backward_workspace_bytes(T, V, d)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = _new(dev, torch.uint8, nbytes)
     _call(dev, lib().rfast_embedding_backward, T, V, d, dy.data_ptr(), _type(dy, "dy"), ld, p_tokens, scale, grad.data_ptr(), _type(grad, "grad"),
           ld_grad, 1 if accumulate else 0, ws.data_ptr(), nbytes)
     return grad
@@ -223,10 +230,9 @@ def rfast_route(logits, k, normalise=True):
     _sizes(T * k)
     ld, lt = _matrix(logits, "logits", T, E, None, dev), _type(logits, "logits")
     i32 = torch.int32
-    r = RFastRoute(torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=torch.float32, device=dev),
-                   torch.empty(E + 1, dtype=i32, device=dev), torch.empty((T, k), dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev))
+    r = RFastRoute(_new(dev, i32, T, k), _new(dev, torch.float32, T, k), _new(dev, i32, E + 1), _new(dev, i32, T, k), _new(dev, i32, T * k))
     nbytes = rfast_route_workspace_bytes(T * k, E)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = _new(dev, torch.uint8, nbytes)
     _call(dev, lib().rfast_route, T, E, k, logits.data_ptr(), lt, ld, 1 if normalise else 0, *[t.data_ptr() for t in r], ws.data_ptr(), nbytes)
     return r
 
@@ -240,9 +246,9 @@ def rfast_route_plan(expert, experts):
     _sizes(P, experts)
     _need(experts >= 1, "need at least one expert")
     p_expert = _vector(expert, "expert", P, i32, dev)
-    row_ptr, place, order = (torch.empty(s, dtype=i32, device=dev) for s in (experts + 1, expert.shape, P))
+    row_ptr, place, order = _new(dev, i32, experts + 1), torch.empty(expert.shape, dtype=i32, device=dev), _new(dev, i32, P)
     nbytes = rfast_route_workspace_bytes(P, experts)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = _new(dev, torch.uint8, nbytes)
     _call(dev, lib().rfast_route_plan, P, experts, p_expert, row_ptr.data_ptr(), place.data_ptr(), order.data_ptr(), ws.data_ptr(), nbytes)
     return row_ptr, place, order
 
@@ -258,7 +264,7 @@ def rfast_route_backward(logits, expert, weight, dweight, normalise=True, dlogit
     given = (_vector(expert, "expert", T * k, torch.int32, dev), _vector(weight, "weight", T * k, torch.float32, dev),
              _vector(dweight, "dweight", T * k, torch.float32, dev))
     if dlogits is None:
-        dlogits, ld_out = torch.empty((T, E), dtype=grad_dtype or logits.dtype, device=dev), max(E, 1)
+        dlogits, ld_out = _new(dev, grad_dtype or logits.dtype, T, E), max(E, 1)
     else:
         _need(grad_dtype is None or dlogits.dtype == grad_dtype, "dlogits: its type is not grad_dtype")
         ld_out = _matrix(dlogits, "dlogits", T, E, None, dev)
@@ -285,7 +291,7 @@ def rfast_route_gather(x, place, out=None):
     rows, k, p_place = _pairs(place, dev)
     _need(rows == T, "place: need one row per row of x")
     if out is None:
-        out = torch.empty((T * k, d), dtype=x.dtype, device=dev)
+        out = _new(dev, x.dtype, T * k, d)
     _need(out.dim() == 2, "out: need a matrix")
     P = out.shape[0]
     _sizes(P, d)
@@ -305,7 +311,7 @@ def rfast_route_combine(rows, place, weight=None, out=None, out_dtype=None):
     T, k, p_place = _pairs(place, dev)
     p_weight = None if weight is None else _vector(weight, "weight", T * k, torch.float32, dev)
     if out is None:
-        out, ld_out = torch.empty((T, d), dtype=out_dtype or rows.dtype, device=dev), max(d, 1)
+        out, ld_out = _new(dev, out_dtype or rows.dtype, T, d), max(d, 1)
     else:
         _need(out_dtype is None or out.dtype == out_dtype, "out: its type is not out_dtype")
         ld_out = _matrix(out, "out", T, d, None, dev)
@@ -327,11 +333,11 @@ def rfast_route_combine_backward(rows, place, weight, dy, drows=None, dweight=No
     ld_dy = _matrix(dy, "dy", T, d, rows.dtype, dev)
     ld_out = d
     if drows is None:
-        drows = torch.empty((P, d), dtype=rows.dtype, device=dev)
+        drows = _new(dev, rows.dtype, P, d)
     elif drows is not False:
         ld_out = _matrix(drows, "drows", P, d, rows.dtype, dev)
     if dweight is None:
-        dweight = torch.empty((T, k), dtype=torch.float32, device=dev)
+        dweight = _new(dev, torch.float32, T, k)
     p_dweight = None if dweight is False else _vector(dweight, "dweight", T * k, torch.float32, dev)
     _call(dev, lib().rfast_route_combine_backward, T, k, d, rows.data_ptr(), _type(rows, "rows"), P, ld, p_place, p_weight, dy.data_ptr(), ld_dy,
           None if drows is False else drows.data_ptr(), ld_out, p_dweight)

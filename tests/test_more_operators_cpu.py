@@ -30,7 +30,7 @@ def test_policy_refusals():
                dict(grad=DEV[0] + 8), dict(grad=DEV[0], gt=1), dict(grad=DEV[2]), dict(loss=DEV[2]), dict(logp=DEV[3] + 4), dict(loss=DEV[7]),
                dict(logp=DEV[0] + 16), dict(loss=DEV[8]), dict(loss=DEV[9])):
         assert policy(**kw) == -1, kw
-    for kw in (dict(low=-0.1), dict(low=1.5), dict(low=NAN), dict(high=-0.1), dict(high=INF), dict(high=NAN), dict(beta=-1.0), dict(beta=INF), dict(beta=NAN)):
+    for kw in (dict(low=-0.1), dict(low=1.5), dict(low=NAN), dict(high=-0.1), dict(high=INF), dict(high=NAN), dict(beta=-1.0), dict(beta=INF), dict(beta=NAN), dict(scale=INF), dict(scale=NAN)):
         assert policy(**kw) == -4, kw
         assert policy(rows=0, **kw) == -4, kw
     assert policy(rows=0) == 0
@@ -47,6 +47,8 @@ def test_embedding_refusals():
                dict(out=DEV[0]), dict(out=DEV[0] + 9 * 32), dict(out=DEV[1])):
         assert embedding(**kw) == -1, kw
     assert embedding(rows=0) == 0
+    for scale in (INF, -INF, NAN):
+        assert embedding(scale=scale) == -4 and back(scale=scale) == -4
 
 
 def back(**kw):
