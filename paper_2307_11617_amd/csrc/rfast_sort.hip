@@ -14,6 +14,8 @@ constexpr int kWaves = 16, kThreads = kWaves * 64;
 constexpr int kDigitMost = 10;
 constexpr int kPartsMost = 256;
 constexpr int kPartsCounted = 32;
+constexpr int kRankMost = 8192, kRanked = 32;
+constexpr int kBoundsRanked = 4096;            // numbers up to which row_ptr is counted with the places
 
 struct Part {
   const int32_t* key;   // of this pass, in its order
@@ -94,20 +96,20 @@ template <int DIGIT> __device__ inline uint64_t alike(int digit, bool is) {
 }
 
 // Of a digit: what each wavefront has becomes what is before it; the sum over all.
-template <int BINS> __device__ inline int32_t before_waves(int32_t* hist, int waves, int32_t run) {
+template <int BINS> __device__ inline int32_t before_waves(int32_t* hist, int32_t run) {
   int32_t h[kWaves];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) h[w] = w < waves ? hist[w * BINS] : 0;
+  for (int w = 0; w < kWaves; ++w) h[w] = hist[w * BINS];
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < waves) hist[w * BINS] = run;
+    hist[w * BINS] = run;
     run += h[w];
   }
   return run;
 }
 
 // Where the elements of a part go.  CHUNKS: of 64 neighbours that a wavefront takes at a time.  COUNT: of few parts (kPartsCounted) every workgroup
-// counts all elements itself, which saves a launch: 8192 numbers of 131072 by two passes 18.4 -> 15 us.
+// counts all elements itself, which saves a launch: a pass over 8192 numbers takes 6.3 us instead of 2.7 + 6.5, over 32768 9.5 and 2.8 + 6.3.
 template <int DIGIT, int CHUNKS, bool COUNT>
 __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, Beside beside) {
   constexpr int bins = 1 << DIGIT, TILE = kThreads * CHUNKS;
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, 
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
-    if (b < bins) start[b] = before_waves<bins>(hist + b, kWaves, start[b]);
+    if (b < bins) start[b] = before_waves<bins>(hist + b, start[b]);
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
@@ -211,81 +213,48 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, 
   }
 }
 
-// All passes of up to CHUNKS * 1024 numbers in one workgroup of as many wavefronts as they need.
-template <int DIGIT, int CHUNKS>
-__global__ void __launch_bounds__(kThreads) rfast_sort_small(Part a, int passes, Beside beside) {
-  constexpr int bins = 1 << DIGIT, MOST = kThreads * CHUNKS;
-  __shared__ int32_t start[bins];
-  __shared__ int32_t hist[kWaves * bins];
-  __shared__ int32_t box[kWaves];
-  __shared__ int32_t moved[2][MOST];
+// Up to kRankMost numbers without digits or passes: an element's place is how many numbers are smaller, or equal and before it.  A workgroup does that for
+// kRanked elements, 32 slices of all the numbers in LDS at a time: count^2 comparisons of two instructions.  1024 numbers take 3.8 us and 4096 take 6.4,
+// whatever their range (by passes in one workgroup 5 and 8 per digit, and more workgroups need launches); 8192 take 11, two passes 14 and one 6.
+// What it writes to row_ptr, the place of the first element of each number, it counts as elements behind the others.
+__global__ void __launch_bounds__(kThreads) rfast_sort_rank(Part a, Beside beside) {
+  constexpr int SLICES = kThreads / kRanked;
+  __shared__ int4 keys[kRankMost / 4];
+  __shared__ int32_t ranks[kRanked][SLICES + 1];
   if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, threads = blockDim.x;
-  const uint64_t below = (1ull << lane) - 1;
-  int32_t key[CHUNKS], from[CHUNKS], to[CHUNKS];
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
-    from[c] = wave * (64 * CHUNKS) + c * 64 + lane;
-    key[c] = from[c] < a.count ? clip_key(a.key[from[c]], a.keys) : -1;
+  int* const key = (int*)keys;
+  const int groups = (a.count + 3) / 4;
+  for (int i = threadIdx.x; i < 4 * groups; i += kThreads) key[i] = i < a.count ? clip_key(a.key[i], a.keys) : 0x7fffffff;
+  __syncthreads();
+  const int mine = threadIdx.x % kRanked, slice = threadIdx.x / kRanked, per = (groups + SLICES - 1) / SLICES;
+  const int64_t unit = (int64_t)blockIdx.x * kRanked + mine;
+  const bool element = unit < a.count;
+  const int index = element ? (int)unit : 0;
+  const uint32_t less = element ? (uint32_t)key[index] : (uint32_t)(unit - a.count), at_most = less + 1;  // (of row_ptr: no equal one is before)
+  const int lo = slice * per, hi = min(lo + per, groups), own = index / 4;
+  int32_t before = 0;
+#pragma unroll 4
+  for (int g = lo; g < hi; ++g) {
+    const int4 q = keys[g];
+    const uint32_t bound = g < own ? at_most : less;
+    before += ((uint32_t)q.x < bound) + ((uint32_t)q.y < bound) + ((uint32_t)q.z < bound) + ((uint32_t)q.w < bound);
   }
-  for (int pass = 0; pass < passes; ++pass) {
-    const int shift = pass * DIGIT;
-    for (int i = threadIdx.x; i < waves * bins; i += threads) hist[i] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const bool is = key[c] >= 0;
-      const int digit = (key[c] >> shift) & (bins - 1);
-      const uint64_t same = alike<DIGIT>(digit, is);
-      to[c] = 0;
-      if (is) {
-        const int32_t had = hist[wave * bins + digit];
-        to[c] = had + __popcll(same & below);
-        __builtin_amdgcn_wave_barrier();
-        if ((same & below) == 0) hist[wave * bins + digit] = had + __popcll(same);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
-    __syncthreads();
-    // of each digit: how many before each wavefront's, then where the digit begins (the workgroup may have fewer threads than digits)
-    int32_t carry = 0;
-    for (int first = 0; first < bins; first += threads) {
-      const int b = first + threadIdx.x;
-      int32_t total = 0;
-      if (b < bins) total = before_waves<bins>(hist + b, waves, 0);
-      const int32_t at = carry + before_me(total, box);
-      if (b < bins) {
-        start[b] = at;
-        if (a.row_ptr && passes == 1 && b <= a.keys) a.row_ptr[b] = at;
-      }
-      for (int w = 0; w < waves; ++w) carry += box[w];
-      __syncthreads();
-    }
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      if (key[c] < 0) continue;
-      const int digit = (key[c] >> shift) & (bins - 1);
-      to[c] += start[digit] + hist[wave * bins + digit];
-    }
-    if (pass + 1 < passes) {
-#pragma unroll
-      for (int c = 0; c < CHUNKS; ++c)
-        if (key[c] >= 0) moved[0][to[c]] = key[c], moved[1][to[c]] = from[c];
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) {
-        const int i = wave * (64 * CHUNKS) + c * 64 + lane;
-        key[c] = i < a.count ? moved[0][i] : -1;
-        from[c] = i < a.count ? moved[1][i] : 0;
-      }
-    }
+  if (element && own >= lo && own < hi) {
+    for (int i = 4 * own; i < index; ++i) before += (uint32_t)key[i] == less;
   }
+  ranks[mine][slice] = before;
+  __syncthreads();
+  if (threadIdx.x >= kRanked) return;
+  int32_t to = 0;
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
-    if (key[c] < 0) continue;
-    if (a.out_key) a.out_key[to[c]] = key[c];
-    if (a.order) a.order[to[c]] = key[c] < a.keys ? from[c] : -1;
-    if (a.place) a.place[from[c]] = key[c] < a.keys ? to[c] : -1;
+  for (int i = 0; i < SLICES; ++i) to += ranks[mine][i];
+  if (element) {
+    const int32_t k = (int32_t)less;
+    if (a.out_key) a.out_key[to] = k;
+    if (a.order) a.order[to] = k < a.keys ? index : -1;
+    if (a.place) a.place[index] = k < a.keys ? to : -1;
+  } else if (a.row_ptr && unit - a.count <= a.keys) {
+    a.row_ptr[unit - a.count] = to;
   }
 }
 
@@ -304,12 +273,10 @@ __global__ void __launch_bounds__(256) rfast_sort_bounds(const int32_t* sorted, 
 
 size_t up(size_t b) { return (b + 255) / 256 * 256; }
 
-constexpr int kSmallChunks = 2, kSmall = kSmallChunks * kThreads;
-
 struct Plan {
   int passes, digit, parts, chunks;
   int32_t per_part;
-  bool small, counted;  // one launch; no launch to count
+  bool ranked, counted;  // one launch for all; no launch to count
   Plan(int32_t count, int32_t keys) {
     int bits = 1;
     while (bits < 31 && (keys >> bits) != 0) ++bits;  // `keys` itself is a number too: that of elements outside
@@ -321,7 +288,7 @@ struct Plan {
     const int64_t per = (tiles + kPartsMost - 1) / kPartsMost;
     per_part = (int32_t)(per * tile < 0x7fffffff ? per * tile : 0x7fffffff);
     parts = count ? (int)(((int64_t)count + per_part - 1) / per_part) : 0;
-    small = count <= kSmall;
+    ranked = count <= kRankMost / 2 || (count <= kRankMost && passes > 1);
     counted = parts <= kPartsCounted;
   }
 };
@@ -330,13 +297,13 @@ struct Plan {
 
 size_t rfast_sort_bytes(int32_t count, int32_t keys) {
   const Plan p(count, keys);
-  if (p.small) return up((size_t)count * 4) + 256;  // (the sorted numbers, for row_ptr)
-  return up((size_t)p.parts << (p.digit + 2)) + (p.passes > 1 ? 4 : 0) * up((size_t)count * 4) + 256 + up((size_t)kSmall * 4);
+  if (p.ranked) return up((size_t)count * 4) + 256;  // (the sorted numbers, for row_ptr)
+  return up((size_t)p.parts << (p.digit + 2)) + (p.passes > 1 ? 4 : 0) * up((size_t)count * 4) + 256 + up((size_t)kRankMost * 4);
 }
 
 hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
   const Plan p(s.count, s.keys);
-  const int launches = s.count == 0 ? 1 : p.small ? 1 : p.counted ? p.passes : 2 * p.passes;
+  const int launches = s.count == 0 || p.ranked ? 1 : p.counted ? p.passes : 2 * p.passes;
   int done = 0;
   // the next launch's share of the fill, and the workgroups that it takes
   const auto beside = [&](int blocks) {
@@ -362,27 +329,19 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
       const Beside f = beside(0);
       hipLaunchKernelGGL((rfast_sort_count<6>), grid(f, kThreads), dim3(kThreads), 0, stream, Part{}, f);
     }
-  } else if (p.small) {
+  } else if (p.ranked) {
+    const bool bounds = s.row_ptr && s.keys <= kBoundsRanked;
     Part a = {};
     a.key = s.key;
     a.count = s.count;
     a.keys = s.keys;
-    a.row_ptr = s.row_ptr;
+    a.row_ptr = bounds ? s.row_ptr : nullptr;
     a.order = s.order;
     a.place = s.place;
-    a.out_key = s.sorted ? s.sorted : s.row_ptr && p.passes > 1 ? (int32_t*)ws : nullptr;
+    a.out_key = s.sorted ? s.sorted : s.row_ptr && !bounds ? (int32_t*)ws : nullptr;
     sorted = a.out_key;
-    by_digit([&](auto digit) {
-      constexpr int D = decltype(digit)::value;
-      const Beside f = beside(1);
-      const auto go = [&](auto kernel, int chunks) {
-        // (as many threads as digits at least: a digit per thread)
-        const int need = (s.count + 64 * chunks - 1) / (64 * chunks) * 64, threads = s.fill.parts > 0 ? kThreads : need < 1 << D ? 1 << D : need;
-        hipLaunchKernelGGL(kernel, grid(f, threads), dim3(threads), 0, stream, a, p.passes, f);
-      };
-      if (s.count <= kThreads) go(rfast_sort_small<D, 1>, 1);
-      else go(rfast_sort_small<D, kSmallChunks>, kSmallChunks);
-    });
+    const Beside f = beside((s.count + (bounds ? s.keys + 1 : 0) + kRanked - 1) / kRanked);
+    hipLaunchKernelGGL(rfast_sort_rank, grid(f, kThreads), dim3(kThreads), 0, stream, a, f);
   } else {
     int32_t* counts = (int32_t*)ws;
     ws += up((size_t)p.parts << (p.digit + 2));
@@ -424,7 +383,7 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
       });
     }
   }
-  if (s.row_ptr && (p.passes > 1 || !s.count))
+  if (s.row_ptr && (s.count == 0 || (p.ranked ? s.keys > kBoundsRanked : p.passes > 1)))
     hipLaunchKernelGGL(rfast_sort_bounds, rfast_grid_of(((int64_t)s.keys + 256) / 256), dim3(256), 0, stream, sorted, s.count, s.keys, s.row_ptr);
   return hipGetLastError();
 }
