@@ -680,18 +680,19 @@ class Step:
     def run(self):
         T, V, d, E, k, K = self.sizes
         x = rf.rfast_embedding(self.table, self.tokens)
-        r = rf.rfast_route(x @ self.gate.t(), k)
+        choice = (x @ self.gate.t()).masked_fill_((self.tokens < 0)[:, None], -INF)  # padding goes to no expert
+        r = rf.rfast_route(choice, k)
         xb = x.to(BF16)
-        rows = rf.rfast_route_gather(xb, r.place)
-        out = rf.rfast_lora_forward(rows, self.w, self.a, self.b, r.row_ptr, scale=0.5)
+        rows = rf.rfast_route_gather(xb, r.place, out=torch.full((T * k, d), NAN, dtype=BF16, device=DEV))
+        out = rf.rfast_lora_forward(rows, self.w, self.a, self.b, r.row_ptr, scale=0.5, out=torch.full_like(rows, NAN))
         y = rf.rfast_route_combine(out, r.place, r.weight, out_dtype=F32)
         logits = y @ self.head.t()
         logp = torch.empty_like(self.old)
         loss, dl = rf.rfast_policy_loss(logits, self.actions, self.old, self.adv, reference=self.ref, beta=0.1, grad_scale=1.0 / T, logp=logp)
         dy = (dl @ self.head).to(BF16)
-        dout, dweight = rf.rfast_route_combine_backward(out, r.place, r.weight, dy)
+        dout, dweight = rf.rfast_route_combine_backward(out, r.place, r.weight, dy, drows=torch.full_like(out, NAN))
         drows, da, db = rf.rfast_lora_backward(rows, self.w, self.a, self.b, r.row_ptr, None, dout, scale=0.5)
-        dgate_logits = rf.rfast_route_backward(x @ self.gate.t(), r.expert, r.weight, dweight)
+        dgate_logits = rf.rfast_route_backward(choice, r.expert, r.weight, dweight)
         dx = rf.rfast_route_combine(drows, r.place, out_dtype=F32) + dgate_logits @ self.gate
         dtable = rf.rfast_embedding_backward(dx, self.tokens, V)
         return dict(expert=r.expert, loss=loss, logp=logp, head=dl.t() @ y, a=da, b=db, gate=dgate_logits.t() @ x, table=dtable)
@@ -706,15 +707,15 @@ class Step:
         p = {n: getattr(self, n).double().requires_grad_() for n in ("table", "gate", "a", "b", "head")}
         real = (self.tokens >= 0).double()[:, None]
         x = p["table"][self.tokens.clamp(min=0).long()] * real
-        chosen = torch.gather(x @ p["gate"].t(), 1, expert.long())
+        chosen = torch.gather(x @ p["gate"].t(), 1, expert.clamp(min=0).long())
         weight = torch.softmax(chosen, dim=1)
         xb = rounded(x)
         y = 0
         for j in range(k):
-            e = expert[:, j].long()
+            e = expert[:, j].clamp(min=0).long()
             u = torch.matmul(p["a"][e], xb[:, :, None])
             out = rounded(xb @ self.w.double().t() + 0.5 * torch.matmul(p["b"][e], u)[:, :, 0])
-            y = y + weight[:, j:j + 1] * out
+            y = y + weight[:, j:j + 1] * out * real
         logs = torch.log_softmax(y @ p["head"].t(), dim=1)
         counts = self.actions >= 0
         logp = logs[torch.arange(T), self.actions.clamp(min=0).long()]
@@ -733,7 +734,7 @@ def test_a_step_of_all():
     x = torch.where((s.tokens >= 0)[:, None], s.table[s.tokens.clamp(min=0).long()], 0.0).double()
     near = torch.sort(x @ s.gate.double().t(), dim=1, descending=True)
     assert torch.equal(got["expert"][s.tokens >= 0].long(), near.indices[:, :2][s.tokens >= 0])
-    assert (got["expert"][s.tokens < 0] == torch.tensor([0, 1])).all()  # a row of zeros: all logits alike
+    assert (got["expert"][s.tokens < 0] == -1).all() and (s.tokens < 0).any()
     want, ratio = s.exact(got["expert"])
     clear = ((ratio - 0.8).abs() > 1e-3) & ((ratio - 1.2).abs() > 1e-3) | (s.actions < 0)
     assert clear.all()

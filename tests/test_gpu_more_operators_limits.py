@@ -95,6 +95,61 @@ def test_policy_offsets_pass_32_bits():
     assert torch.equal(loss[far], want_loss) and torch.equal(grad[far], want)
 
 
+@pytest.mark.parametrize("kind,out", [(BF16, BF16), (F32, F32)])
+def test_losses_past_the_caches(kind, out):
+    """A gradient of more than 256 MB takes another way out than one of a few rows.
+
+    Rows of an odd number of classes begin at different places behind a multiple of 16 bytes, from which groups of logits are counted, so the order of
+    a row's sum differs between the two calls.  Its terms are positive and the longest chain of additions has at most 144 of them (128 of a
+    lane, 6 + 4 of trees, and some), so two orders differ by 288 half steps of 32 bits relative, and with them e / sum; a logarithm by as much
+    absolutely, and by 8 half steps of itself for its function, product and sums.  The gradient then rounds three times, and to its type."""
+    T, K = 3001, 50001
+    half = 2.0 ** -24
+    logits = tiled(T, K, kind)
+    actions = torch.randint(-1, K, (T,), generator=gen(8), dtype=I32).to(DEV)
+    old, adv = torch.randn(T, generator=gen(9)).to(DEV) - 11.0, torch.randn(T, generator=gen(10)).to(DEV)
+    some = [0, 1, 1500, T - 2, T - 1]
+    xent = rf.rfast_softmax_xent(logits[some], actions[some])
+    policy = rf.rfast_policy_loss(logits[some], actions[some], old[some], adv[some])
+    hot = torch.nn.functional.one_hot(actions[some].clamp(min=0).long(), K) * (actions[some] >= 0)[:, None]
+
+    def alike(loss, grad, want, factor, more):
+        """factor: what multiplies softmax - onehot; more: its relative error."""
+        off = 288 * half + 8 * half * (want[0].abs() + 12)
+        assert ((loss[some] - want[0]).abs() <= factor * off + 8 * half * want[0].abs()).all()
+        g, w = grad[some].double(), want[1].double()
+        bound = (w.abs() + factor[:, None] * hot) * (288 + 8 + more[:, None]) * half + 2 * (2.0 ** -8 if out == BF16 else half) * w.abs()
+        assert ((g - w).abs() <= bound).all()
+
+    loss, grad = rf.rfast_softmax_xent(logits, actions, grad_dtype=out)
+    alike(loss, grad, xent, torch.ones(5, device=DEV), torch.zeros(5, device=DEV))
+    # the ratio's error is that of logp (below 24): 288 half steps and 8 of 24, and it is at most the loss over the advantage where it is not clipped
+    loss, grad = rf.rfast_policy_loss(logits, actions, old, adv, grad=logits)
+    alike(loss, grad, policy, torch.maximum(policy[0].abs(), torch.ones(5, device=DEV)), torch.full((5,), 288.0 + 8 * 24 + 8, device=DEV))
+
+
+@pytest.mark.parametrize("T,k,d", [(70000, 3, 1000), (9000, 9, 2048)])
+def test_rows_past_the_caches(T, k, d):
+    """So do more than 256 MB of rows."""
+    place = torch.randperm(T * k, generator=gen(11)).to(I32).view(T, k)
+    place[7, 0] = -1
+    place, weight, x = place.to(DEV), torch.rand((T, k), generator=gen(12)).to(DEV), tiled(T, d, BF16)
+    rows = rf.rfast_route_gather(x, place, out=torch.zeros((T * k, d), dtype=BF16, device=DEV))
+    want = torch.zeros_like(rows)
+    for j in range(k):
+        live = place[:, j] >= 0
+        want[place[live, j].long()] = x[live]
+    assert torch.equal(rows, want)
+    some = [0, 7, T // 2, T - 1]
+    at = torch.where(place[some] >= 0, torch.arange(len(some) * k, device=DEV, dtype=I32).view(-1, k), -1)
+    few = rows[place[some].clamp(min=0).long().view(-1)]
+    assert torch.equal(rf.rfast_route_combine(rows, place, weight)[some], rf.rfast_route_combine(few, at, weight[some]))
+    drows, dweight = rf.rfast_route_combine_backward(rows, place, weight, x, drows=want)
+    want, want_weight = rf.rfast_route_combine_backward(few, at, weight[some], x[some])
+    live = at.view(-1) >= 0
+    assert torch.equal(dweight[some], want_weight) and torch.equal(drows[place[some].view(-1)[live].long()], want[live])
+
+
 @pytest.mark.parametrize("pairs", [255, 256, 257, 1023, 1024, 1025, 2047, 2048, 2049, 3073, 8192, 32767, 32768, 32769, 262144, 262145])
 @pytest.mark.parametrize("experts", [40, 200, 400, 900, 60000, 300000])
 def test_sort_where_its_form_changes(pairs, experts):
