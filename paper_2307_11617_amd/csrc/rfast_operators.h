@@ -91,6 +91,14 @@ template <class V, bool STREAM> __device__ inline void wide_store(void* p, V v) 
   else *g = v;
 }
 
+// Memory cleared by a wavefront, 16 bytes a lane side by side: n units of 2 bytes.
+__device__ inline void clear_units(u16* p, int64_t n) {
+  const any_u32x4 zero = {0, 0, 0, 0};
+  int64_t i = (threadIdx.x & 63) * 8;
+  for (; i + 8 <= n; i += 512) wide_store<any_u32x4, true>(p + i, zero);
+  for (int j = 0; j < 8 && i + j < n; ++j) p[i + j] = 0;  // (of one lane: the end)
+}
+
 // Four neighbours of an array of `T` (float or u16 = bf16) from p on, as floats; `left` (1 or more) of them exist.
 template <bool STREAM> __device__ inline void load_four(const float* p, int64_t left, float* v) {
   if (left >= 4) {

@@ -38,15 +38,9 @@ struct Beside {
   int blocks;  // of the sort
 };
 __device__ inline void clear_beside(const Beside& f) {
-  const int waves = blockDim.x / 64, lane = threadIdx.x & 63;
-  const any_u32x4 zero = {0, 0, 0, 0};
-  for (int64_t part = f.lo + (int64_t)(blockIdx.x - f.blocks) * waves + threadIdx.x / 64; part < f.hi; part += (int64_t)(gridDim.x - f.blocks) * waves) {
-    u16* p = f.fill.p + part * f.fill.apart;
-    const int64_t n = part == f.fill.parts - 1 ? f.fill.last : f.fill.wide;
-    int64_t i = lane * 8;
-    for (; i + 8 <= n; i += 512) wide_store<any_u32x4, true>(p + i, zero);
-    for (int j = 0; j < 8 && i + j < n; ++j) p[i + j] = 0;  // (of one lane: the end of the part)
-  }
+  const int waves = kThreads / 64;
+  for (int64_t part = f.lo + (int64_t)(blockIdx.x - f.blocks) * waves + threadIdx.x / 64; part < f.hi; part += (int64_t)(gridDim.x - f.blocks) * waves)
+    clear_units(f.fill.p + part * f.fill.apart, part == f.fill.parts - 1 ? f.fill.last : f.fill.wide);
 }
 
 __device__ inline int clip_key(int32_t k, int32_t keys) { return (uint32_t)k < (uint32_t)keys ? k : keys; }
@@ -303,7 +297,7 @@ size_t rfast_sort_bytes(int32_t count, int32_t keys) {
 
 hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
   const Plan p(s.count, s.keys);
-  const int launches = s.count == 0 || p.ranked ? 1 : p.counted ? p.passes : 2 * p.passes;
+  const int launches = p.ranked ? 1 : p.counted ? p.passes : 2 * p.passes;
   int done = 0;
   // the next launch's share of the fill, and the workgroups that it takes
   const auto beside = [&](int blocks) {
@@ -311,9 +305,9 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
     ++done;
     return f;
   };
-  const auto grid = [](const Beside& f, int threads) {
-    const int64_t waves = threads / 64, need = (f.hi - f.lo + waves - 1) / waves;
-    return dim3((unsigned)(f.blocks + (need < 512 * 16 / waves ? need : 512 * 16 / waves)));
+  const auto grid = [](const Beside& f) {
+    const int64_t need = (f.hi - f.lo + kWaves - 1) / kWaves;
+    return dim3((unsigned)(f.blocks + (need < 512 ? need : 512)));
   };
   const auto by_digit = [&](auto go) {
     using std::integral_constant;
@@ -324,12 +318,7 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
   };
   char* ws = (char*)s.workspace;
   const int32_t* sorted = nullptr;
-  if (s.count == 0) {
-    if (s.fill.parts > 0) {
-      const Beside f = beside(0);
-      hipLaunchKernelGGL((rfast_sort_count<6>), grid(f, kThreads), dim3(kThreads), 0, stream, Part{}, f);
-    }
-  } else if (p.ranked) {
+  if (p.ranked && s.count > 0) {
     const bool bounds = s.row_ptr && s.keys <= kBoundsRanked;
     Part a = {};
     a.key = s.key;
@@ -341,8 +330,8 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
     a.out_key = s.sorted ? s.sorted : s.row_ptr && !bounds ? (int32_t*)ws : nullptr;
     sorted = a.out_key;
     const Beside f = beside((s.count + (bounds ? s.keys + 1 : 0) + kRanked - 1) / kRanked);
-    hipLaunchKernelGGL(rfast_sort_rank, grid(f, kThreads), dim3(kThreads), 0, stream, a, f);
-  } else {
+    hipLaunchKernelGGL(rfast_sort_rank, grid(f), dim3(kThreads), 0, stream, a, f);
+  } else if (s.count > 0) {
     int32_t* counts = (int32_t*)ws;
     ws += up((size_t)p.parts << (p.digit + 2));
     int32_t* buffer[4] = {};
@@ -373,11 +362,11 @@ hipError_t rfast_sort(const RfastSort& s, hipStream_t stream) {
         constexpr int D = decltype(digit)::value;
         const auto go = [&](auto kernel) {
           const Beside f = beside(p.parts);
-          hipLaunchKernelGGL(kernel, grid(f, kThreads), dim3(kThreads), 0, stream, a, p.parts, f);
+          hipLaunchKernelGGL(kernel, grid(f), dim3(kThreads), 0, stream, a, p.parts, f);
         };
         if (p.counted) return go(rfast_sort_place<D, 1, true>);
         const Beside f = beside(p.parts);
-        hipLaunchKernelGGL((rfast_sort_count<D>), grid(f, kThreads), dim3(kThreads), 0, stream, a, f);
+        hipLaunchKernelGGL((rfast_sort_count<D>), grid(f), dim3(kThreads), 0, stream, a, f);
         if (p.chunks == 1) go(rfast_sort_place<D, 1, false>);
         else go(rfast_sort_place<D, 4, false>);
       });
