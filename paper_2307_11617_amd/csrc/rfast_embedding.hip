@@ -6,7 +6,9 @@
 // where they are small.  The gradient sorts the tokens (stable, so that a row's terms are added in the order of t) and clears the table's gradient beside
 // the sort, which would leave the card idle.  A wavefront then adds the rows of a chunk of 16 to 64 sorted positions, run by run: where a run begins and
 // ends inside the chunk its sum is that row of the gradient, else the chunk's part of it goes to the workspace, and a last launch adds
-// the parts of such runs.  So frequent tokens (one in thirty rows) and rare ones cost the same per row of dy.
+// the parts of such runs.  So frequent tokens (one in thirty rows) and rare ones cost the same per row of dy.  32768 tokens of 50001 x 1024, bf16 to
+// 32 bits: sort and 205 MB of zeros 39 us, sums 20 (104 MB at 5.3 TB/s), parts 8; a wavefront per row of the table that looks its run up took 180 in all.
+// Sums are in 32 bits, rounded to the gradient's type once.
 #include <algorithm>
 #include <type_traits>
 
@@ -82,7 +84,8 @@ template <class OUT, bool ADD> __device__ inline void store_sum(OUT* grad, const
   }
 }
 
-// LANES lanes per chunk and slab of columns.
+// LANES lanes per chunk and slab of columns; kAtOnce rows are asked for before the first is added (sixteen, or past the caches: no faster, 19 -> 22 and 23 us
+// for 8192 tokens added to rows of 2048).
 template <class IN, class OUT, int LANES, bool WHOLE, bool ADD> __global__ void __launch_bounds__(kThreads) rfast_embedding_sums(Back a) {
   constexpr int UNITS = kThreads / LANES;
   __shared__ int2 list[UNITS][kChunkMost];  // token, row of dy
@@ -129,7 +132,8 @@ template <class IN, class OUT, int LANES, bool WHOLE, bool ADD> __global__ void 
   }
 }
 
-// The runs that go on behind the chunk that they begin in: LANES lanes per chunk and slab.
+// The runs that go on behind the chunk that they begin in: LANES lanes per chunk and slab.  Bound by its launch and some five trips to memory one behind
+// the other (5 to 8 us).
 template <class OUT, int LANES, bool WHOLE, bool ADD> __global__ void __launch_bounds__(kThreads) rfast_embedding_join(Back a) {
   const int64_t unit = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x) / LANES;
   const int64_t chunk = unit / a.slabs, lo = chunk * a.chunk, hi = lo + a.chunk;
@@ -272,7 +276,8 @@ struct Layout {
       at += up(bytes);
       return here;
     };
-    // short chunks where long ones would be too few wavefronts for the card
+    // short chunks where long ones would be too few wavefronts for the card; with 8192 instead of 2048 wavefronts the sums take as long (19.7 us for
+    // 32768 tokens x 1024) and the joins of frequent tokens longer (7.4 -> 11.5)
     const int64_t slabs = slabs_of(d), few = 2048;
     chunk = 16;
     while (chunk < kChunkMost && ((int64_t)rows + chunk - 1) / chunk * slabs > few) chunk *= 2;

