@@ -164,6 +164,32 @@ def test_sort_where_its_form_changes(pairs, experts):
     assert np.array_equal(p.cpu().numpy(), place) and np.array_equal(o.cpu().numpy(), order)
 
 
+@pytest.mark.parametrize("T", [16, 17, 63, 64, 65, 255, 256, 257, 4096, 4097, 8192, 8193])
+@pytest.mark.parametrize("V,d,gap", [(70, 8, 0), (70, 8, 3), (3000, 20, 0), (5, 1500, 1), (900, 256, 0), (900, 264, 0), (12, 7, 0)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embedding_gradient_where_its_form_changes(T, V, d, gap, accumulate):
+    """Small whole numbers, whose sums are exact in 32 bits, so that every order gives the same bits; rows of padding hold NaN."""
+    g = gen(T + V + d)
+    tokens = torch.randint(-1, V + 1, (T,), generator=g, dtype=I32)
+    tokens[torch.rand(T, generator=g) < 0.3] = V // 2
+    dy = torch.randint(-8, 9, (T, d), generator=g).float()
+    real = (tokens >= 0) & (tokens < V)
+    grad = torch.randint(-8, 9, (V, d + gap), generator=g).float()
+    want = grad.clone()
+    if not accumulate:
+        want[:, :d] = 0
+    want[:, :d].index_put_((tokens[real].long(),), dy[real] * 2, accumulate=True)
+    dy[~real] = float("nan")
+    grad = grad.to(DEV)
+    rf.rfast_embedding_backward(dy.to(DEV), tokens.to(DEV), V, scale=2.0, grad=grad[:, :d], accumulate=accumulate)
+    assert torch.equal(grad.cpu(), want)
+    grad = grad.to(BF16) * 0 + 1
+    half = dy.to(BF16).to(DEV)
+    rf.rfast_embedding_backward(half, tokens.to(DEV), V, scale=2.0, grad=grad[:, :d], accumulate=accumulate)
+    total = torch.zeros((V, d)).index_put_((tokens[real].long(),), dy[real] * 2, accumulate=True) + (1 if accumulate else 0)
+    assert torch.equal(grad[:, :d].cpu(), total.to(BF16)) and (grad[:, d:] == 1).all()
+
+
 @pytest.mark.parametrize("rows", [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 128, 129, 256, 257])
 @pytest.mark.parametrize("experts,k", [(5, 3), (64, 4), (65, 8), (300, 1)])
 def test_router_where_one_workgroup_ends(rows, experts, k):
