@@ -6,7 +6,8 @@
 // are one kernel (the policy's 32768 rows of 128 classes in 32 bits 7.8 us, 4096 rows of 50001 in bf16 150 us, 5.5 TB/s).
 //
 // Some five operations per logit, so the bound is one read of the logits and one write of the gradient.  A row therefore stays in
-// registers between the two: of 8 to 64 lanes up to 1024 logits (2048 of bf16), of a workgroup of 256 to 1024 lanes beyond.  Rows longer than the registers
+// registers between the two: of 8 to 64 lanes up to 1024 logits (2048 of bf16), of a workgroup of 256 to 1024 lanes beyond.  (Of the policy's
+// rows 1024 lanes hold up to 131000 logits of bf16: 200 M logits in rows of 89855 take 162 us, read twice 235.)  Rows longer than the registers
 // of a workgroup are read twice, the second time through the caches, with a running maximum and sum per lane in the first pass.
 // A row's maximum is taken out of its exponents before they are formed, so that nothing overflows; sums are in 32 bits,
 // one per lane and then a tree.
@@ -139,13 +140,22 @@ template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane,
   for (int64_t k = lane; k < K; k += lanes) grad[k] = (OUT)0;  // (the last step of a row of nearly 2^31 passes 32 bits)
 }
 
+// Element `at` (not below 0, less than 4 GB on) of a row that a wavefront's lanes share: one address of the row and 32 bits per lane.
+template <class T> __device__ inline T* near_by(T* row, int at) {
+  return (T*)((uintptr_t)row + (uint32_t)at * (uint32_t)sizeof(T));
+}
+
 // LANES lanes hold a row, GROUPS groups of logits each.  LANES <= 64: 256 / LANES rows per workgroup.
 // Every load is a whole group without a condition (a condition per load would have each of them waited for before the next is sent), so groups
 // overlap at the ends of a row: group h begins at 8 h - m, moved into [0, K - 8] (4 instead of 8 in 32 bits), where m is how far a row of
 // a workgroup's begins behind a multiple of 16 bytes, so that all but the first and last group are aligned (4096 rows of 50001: 184 us with
 // m = 0, 152 so).  What a group shares with the one before is left out of its sum, and its gradient is written twice alike.
 template <class IN, class OUT, int LANES, int GROUPS, bool POLICY, bool FAR>
-__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 1) rfast_xent_kernel(Args a) {
+__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, LANES == 1024 && GROUPS <= 12 ? 8 : GROUPS >= 13 ? 4 : 1) rfast_xent_kernel(Args a) {
+  // Where groups begin is computed again for the gradient where registers are short: kept from the loads it takes one for each and spills
+  // (200 M logits in rows of 60000 of bf16: 189 -> 156 us, of 65000 in 32 bits 345 -> 312).  Elsewhere the two workgroups per compute unit that the
+  // registers then leave room for are the best number: with three, rows of 20000 in 32 bits take 291 us instead of 264.
+  constexpr bool AGAIN = GROUPS >= 16 || LANES == 1024;
   constexpr int N = Group<IN>::N, ROWS = LANES <= 64 ? 256 / LANES : 1, SPAN = LANES * N;
   __shared__ float box[2][16];
   const int lane = threadIdx.x % LANES;
@@ -169,7 +179,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
   Group<IN> v[GROUPS];
   if (LANES > 8 || GROUPS > 1 || last >= 0) {
 #pragma unroll
-    for (int q = 0; q < GROUPS; ++q) v[q].load(l + begin(q * LANES + lane));
+    for (int q = 0; q < GROUPS; ++q) v[q].load(AGAIN ? near_by(l, begin(q * LANES + lane)) : l + begin(q * LANES + lane));
   } else {
     v[0].load(l, a.K);
   }
@@ -213,9 +223,11 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
   }
   const float c = scale / sum;
   forget();
+  int mine = lane;
+  if constexpr (AGAIN) asm volatile("" : "+v"(mine));  // (a number that the compiler has not seen: nothing to keep)
 #pragma unroll
   for (int q = 0; q < GROUPS; ++q) {
-    const int h = q * LANES + lane, at = begin(h);
+    const int h = q * LANES + mine, at = begin(h);
     float g[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) g[j] = power(v[q].at(j), shift) * c;
@@ -225,7 +237,7 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES, GROUPS >= 13 ? 4 : 
     }
     if (h * N - m >= a.K) continue;
     if (LANES > 8 || GROUPS > 1 || last >= 0) {
-      store_group<N, FAR>(grad + at, g);
+      store_group<N, FAR>(AGAIN ? near_by(grad, at) : grad + at, g);
     } else {
 #pragma unroll
       for (int j = 0; j < N; j += 4)
@@ -335,6 +347,12 @@ template <class IN, class OUT, bool POLICY> hipError_t launch(const Args& a, hip
   RFAST_TRY(512, 10);
   RFAST_TRY(512, 13);
   RFAST_TRY(512, 16);
+  if constexpr (POLICY) {
+    RFAST_TRY(1024, 10);
+    RFAST_TRY(1024, 11);
+    RFAST_TRY(1024, 12);
+    RFAST_TRY(1024, 16);
+  }
   if constexpr (N == 4) {
     RFAST_TRY(1024, 16);
   }

@@ -515,7 +515,8 @@ class Policy:
         return [None if t is None else t.to(DEV) for t in (self.logits, self.actions, self.old, self.advantage, self.reference, self.weight)]
 
 
-POLICIES = [(1, 2), (1, 7), (3, 1), (70, 4), (33, 9), (64, 64), (50, 65), (40, 128), (30, 200), (20, 513), (17, 1025), (9, 4100), (5, 20011), (3, 50001), (2, 70003), (2, 131072)]
+POLICIES = [(1, 2), (1, 7), (3, 1), (70, 4), (33, 9), (64, 64), (50, 65), (40, 128), (30, 200), (20, 513), (17, 1025), (9, 4100), (5, 20011), (3, 50001), (2, 36285), (2, 44000), (2, 60000), (2, 70003), (2, 89855), (2, 97003), (2, 120001),
+            (2, 131065), (2, 131072)]
 
 
 @pytest.mark.parametrize("T,K", POLICIES)
