@@ -230,31 +230,39 @@ struct Rows {
   int32_t rows, k, d, sorted_rows;
 };
 
-// Work on columns: LANES lanes take a row, eight neighbouring columns each, and rows of more than 512 columns are cut into slabs, a wavefront
-// each.  WHOLE (d >= 8): the last group of a row is moved back to end with it and shares columns with the one before, which both write alike, so that
+// Work on columns: LANES lanes take a row, N neighbouring columns (16 bytes) each, and rows of more than 64 N columns are cut into slabs, a wavefront
+// each.  WHOLE (d >= N): the last group of a row is moved back to end with it and shares columns with the one before, which both write alike, so that
 // every access is a whole one; else a row is a single group, element by element.
 struct Spot {
   int64_t row;
   int col;   // the group's first column
-  int left;  // its columns (WHOLE: 8)
+  int left;  // its columns (WHOLE: N)
   bool in;
 };
-template <int LANES, bool WHOLE> __device__ inline Spot spot_of(int32_t rows, int32_t d, int slabs) {
+template <int LANES, bool WHOLE, int N> __device__ inline Spot spot_of(int32_t rows, int32_t d, int slabs) {
   const int64_t unit = (block_number() * kThreads + threadIdx.x) / LANES;
   Spot s;
   s.row = unit / slabs;
-  const int col = ((int)(unit - s.row * slabs) * LANES + threadIdx.x % LANES) * 8;
+  const int col = ((int)(unit - s.row * slabs) * LANES + threadIdx.x % LANES) * N;
   if constexpr (LANES == 64)  // (a wavefront's lanes have one row: what belongs to it is read once)
     s.row = (int64_t)__builtin_amdgcn_readfirstlane((int)(s.row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)s.row);
   s.in = s.row < rows && col < d;
-  s.col = WHOLE ? min(col, d - 8) : col;
-  s.left = WHOLE ? 8 : d - col;
+  s.col = WHOLE ? min(col, d - N) : col;
+  s.left = WHOLE ? N : d - col;
   return s;
+}
+template <int N, bool STREAM, class T> __device__ inline void load_some(const T* p, int left, float* v) {
+  if constexpr (N == 8) load_eight<STREAM>(p, left, v);
+  else load_four<STREAM>(p, left, v);
+}
+template <int N, bool STREAM, class T> __device__ inline void store_some(T* p, int left, const float* v) {
+  if constexpr (N == 8) store_eight<STREAM>(p, left, v);
+  else store_four<STREAM>(p, left, v);
 }
 
 // Units of 2 bytes, whatever the type.  FAR: the copies are written past the caches.
 template <int LANES, bool WHOLE, bool FAR> __global__ void __launch_bounds__(kThreads) rfast_route_gather_kernel(Rows a, int slabs) {
-  const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
+  const Spot s = spot_of<LANES, WHOLE, 8>(a.rows, a.d, slabs);
   if (!s.in) return;
   const u16* x = (const u16*)a.in + s.row * a.ld_in + s.col;
   any_u32x4 v = {};
@@ -277,14 +285,15 @@ template <int LANES, bool WHOLE, bool FAR> __global__ void __launch_bounds__(kTh
 // AT_ONCE choices' rows are under way together; one without a place reads row 0 and counts for nothing.  FAR: the rows are read past the caches.
 template <class IN, class OUT, int LANES, bool WHOLE, int AT_ONCE, bool FAR>
 __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, int slabs) {
-  const Spot s = spot_of<LANES, WHOLE>(a.rows, a.d, slabs);
+  constexpr int N = 16 / sizeof(IN);
+  const Spot s = spot_of<LANES, WHOLE, N>(a.rows, a.d, slabs);
   if (!s.in) return;
   const int32_t* place = a.place + s.row * a.k;
   const float* weight = a.weight ? a.weight + s.row * a.k : nullptr;
-  float y[8] = {};
+  float y[N] = {};
   if (a.sorted_rows > 0) {
     for (int first = 0; first < a.k; first += AT_ONCE) {
-      float w[AT_ONCE], v[AT_ONCE][8];
+      float w[AT_ONCE], v[AT_ONCE][N];
       bool live[AT_ONCE];
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
@@ -292,20 +301,20 @@ __global__ void __launch_bounds__(kThreads) rfast_route_combine_kernel(Rows a, i
         const int32_t from = place[j];
         live[i] = first + i < a.k && (uint32_t)from < (uint32_t)a.sorted_rows;
         w[i] = weight ? weight[j] : 1.f;
-        load_eight<FAR>((const IN*)a.in + (live[i] ? from : 0) * a.ld_in + s.col, s.left, v[i]);
+        load_some<N, FAR>((const IN*)a.in + (live[i] ? from : 0) * a.ld_in + s.col, s.left, v[i]);
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) y[c] += live[i] ? w[i] * v[i][c] : 0.f;
+        for (int c = 0; c < N; ++c) y[c] += live[i] ? w[i] * v[i][c] : 0.f;
     }
   }
-  store_eight<false>((OUT*)a.out + s.row * a.ld_out + s.col, s.left, y);
+  store_some<N, false>((OUT*)a.out + s.row * a.ld_out + s.col, s.left, y);
 }
 
 // AT_ONCE choices at a time, so that dy_t is read once for up to eight, LANES lanes per row, or the whole workgroup (LANES = 256), whose wavefronts' sums meet in LDS.
 template <class T, int LANES, bool WHOLE, int AT_ONCE, bool FAR> __global__ void __launch_bounds__(kThreads) rfast_route_combine_back(Rows a) {
-  constexpr int WAVES = LANES > 64 ? LANES / 64 : 1;
+  constexpr int WAVES = LANES > 64 ? LANES / 64 : 1, N = 16 / sizeof(T);
   __shared__ float box[LANES > 64 ? kChoicesMost : 1][WAVES];
   int64_t row = (block_number() * kThreads + threadIdx.x) / LANES;
   if constexpr (LANES >= 64)
@@ -327,37 +336,37 @@ template <class T, int LANES, bool WHOLE, int AT_ONCE, bool FAR> __global__ void
       w[i] = a.weight ? a.weight[row * a.k + j] : 1.f;
       dot[i] = 0.f;
     }
-    for (int64_t begin = lane * 8; begin < a.d; begin += LANES * 8) {
-      const int col = WHOLE ? (int)min(begin, (int64_t)a.d - 8) : (int)begin, left = WHOLE ? 8 : a.d - col;
+    for (int64_t begin = lane * N; begin < a.d; begin += LANES * N) {
+      const int col = WHOLE ? (int)min(begin, (int64_t)a.d - N) : (int)begin, left = WHOLE ? N : a.d - col;
       const int again = (int)begin - col;  // columns that the group before has too
-      float g[8], v[AT_ONCE][8];
-      load_eight<false>(dy + col, left, g);
+      float g[N], v[AT_ONCE][N];
+      load_some<N, false>(dy + col, left, g);
       if (dots) {
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) load_eight<FAR>((const T*)a.in + at[i] * a.ld_in + col, left, v[i]);
+        for (int i = 0; i < AT_ONCE; ++i) load_some<N, FAR>((const T*)a.in + at[i] * a.ld_in + col, left, v[i]);
       }
       if (a.out) {
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-          float o[8];
+          float o[N];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) o[c] = w[i] * g[c];
-          if (live[i]) store_eight<FAR>((T*)a.out + at[i] * a.ld_out + col, left, o);
+          for (int c = 0; c < N; ++c) o[c] = w[i] * g[c];
+          if (live[i]) store_some<N, FAR>((T*)a.out + at[i] * a.ld_out + col, left, o);
         }
       }
       if (dots) {
         if (again > 0) {
 #pragma unroll
-          for (int c = 0; c < 8; ++c) g[c] = c < again ? 0.f : g[c];
+          for (int c = 0; c < N; ++c) g[c] = c < again ? 0.f : g[c];
 #pragma unroll
           for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[i][c] = c < again ? 0.f : v[i][c];
+            for (int c = 0; c < N; ++c) v[i][c] = c < again ? 0.f : v[i][c];
         }
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-          for (int c = 0; c < 8; ++c) dot[i] += v[i][c] * g[c];
+          for (int c = 0; c < N; ++c) dot[i] += v[i][c] * g[c];
       }
     }
     if (a.dweight) {
@@ -385,15 +394,16 @@ template <class T, int LANES, bool WHOLE, int AT_ONCE, bool FAR> __global__ void
   }
 }
 
-// go(lanes per row, whole groups) for rows of `columns` columns.
-template <class F> hipError_t by_lanes(int64_t columns, F go) {
+// go(lanes per row, whole groups) for rows of `columns` columns, n of them to a lane.
+template <class F> hipError_t by_lanes(int64_t columns, int n, F go) {
   using std::integral_constant;
-  if (columns < 8) return go(integral_constant<int, 8>(), std::false_type());
-  if (columns <= 64) return go(integral_constant<int, 8>(), std::true_type());
-  if (columns <= 128) return go(integral_constant<int, 16>(), std::true_type());
-  if (columns <= 256) return go(integral_constant<int, 32>(), std::true_type());
+  if (columns < n) return go(integral_constant<int, 8>(), std::false_type());
+  if (columns <= 8 * n) return go(integral_constant<int, 8>(), std::true_type());
+  if (columns <= 16 * n) return go(integral_constant<int, 16>(), std::true_type());
+  if (columns <= 32 * n) return go(integral_constant<int, 32>(), std::true_type());
   return go(integral_constant<int, 64>(), std::true_type());
 }
+int slabs_of(int64_t columns, int n) { return (int)((columns + 64 * n - 1) / (64 * n)); }
 // go(choices at once)
 template <class F> hipError_t by_choices(int32_t k, F go) {
   using std::integral_constant;
@@ -405,13 +415,13 @@ template <class F> hipError_t by_choices(int32_t k, F go) {
 RfastArea area(const void* p, int64_t rows, int64_t ld, int64_t columns, int bytes) { return {p, rows, ld * bytes, columns * bytes}; }
 RfastArea area(const void* p, int64_t count) { return {p, 1, count * 4, count * 4}; }
 
-// Rows of 16 bits that begin at multiples of 16 bytes and are more than the last-level cache (256 MB) holds are read past the caches: 8192 x 4
-// of 4096 return in 56 us so and in 61 otherwise, their gradient takes 97 and 107; 30000 x 2 of 192, which the cache holds, return in 10.9
-// so and in 8.2 otherwise, and in 32 bits, where a lane reads two halves of 32 bytes, it costs whatever the size (4096 x 8 of 2048: 61 and 56).
+// Rows that begin at multiples of 16 bytes and are more than the last-level cache (256 MB) holds are read or written past the caches: 8192 x 4 of 4096
+// bf16 return in 56 us so and in 61 otherwise, 4096 x 8 of 2048 in 32 bits in 53 and 56; the gradient, which reads and writes as much, takes 102 and
+// 119 us, and what follows it 54 and 61; 7936 x 3 of 2312 in 32 bits 102 and 113.  30000 x 2 of 192, which the cache holds, return in 10.9 so and in 8.2 otherwise.
 // The dispatch writes units of 16 bytes whatever the type: 8192 x 8 rows of 8 KB in 99 us past the caches and in 114 otherwise, 60000 x 4 of 66 bytes
 // in 12.4 and 8.4.
 bool is_far(const void* sorted, int64_t pairs, int64_t ld, int64_t d, int bytes) {
-  return bytes == 2 && pairs * d * 2 >= (int64_t)1 << 28 && (uintptr_t)sorted % 16 == 0 && ld % 8 == 0;
+  return pairs * d * bytes >= (int64_t)1 << 28 && (uintptr_t)sorted % 16 == 0 && ld * bytes % 16 == 0;
 }
 
 bool counts_ok(int32_t rows, int32_t k, int32_t d, int32_t sorted_rows) {
@@ -535,10 +545,10 @@ extern "C" int rfast_route_gather(int32_t rows, int32_t k, int32_t d, const void
   const int64_t half = w / 2, columns = d * half;
   if (columns > kColumnsMost) return rfast_refuse(RFAST_EINVAL, "rows of nearly 2^32 bytes or more");
   const Rows a = {x, place, nullptr, nullptr, sorted, nullptr, ld_x * half, 0, ld_sorted * half, rows, k, (int32_t)columns, sorted_rows};
-  const hipError_t e = by_lanes(columns, [&](auto lanes, auto whole) {
+  const hipError_t e = by_lanes(columns, 8, [&](auto lanes, auto whole) {
     constexpr int L = decltype(lanes)::value;
     constexpr bool W = decltype(whole)::value;
-    const int slabs = (int)((columns + 511) / 512);
+    const int slabs = slabs_of(columns, 8);
     const auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads), dim3(kThreads), 0, (hipStream_t)hip_stream, a,
                          slabs);
@@ -567,23 +577,26 @@ extern "C" int rfast_route_combine(int32_t rows, int32_t k, int32_t d, const voi
   const Rows a = {sorted, place, weight, nullptr, y, nullptr, ld_sorted, 0, ld_y, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
   const bool far = is_far(sorted, pairs, ld_sorted, d, w);
-  const hipError_t e = by_lanes(d, [&](auto lanes, auto whole) {
+  const hipError_t e = by_lanes(d, 16 / w, [&](auto lanes, auto whole) {
     return by_choices(k, [&](auto choices) {
       constexpr int L = decltype(lanes)::value, C = decltype(choices)::value;
       constexpr bool W = decltype(whole)::value;
-      const int slabs = (int)(((int64_t)d + 511) / 512);
+      const int slabs = slabs_of(d, 16 / w);
       const dim3 grid = rfast_grid_of(((int64_t)rows * slabs * L + kThreads - 1) / kThreads);
       const auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, slabs);
         return hipGetLastError();
       };
       const bool yf = y_type == RFAST_F32;
-      if (type == RFAST_F32)
-        return yf ? go(rfast_route_combine_kernel<float, float, L, W, C, false>) : go(rfast_route_combine_kernel<float, u16, L, W, C, false>);
+      const auto types = [&](auto past) {
+        constexpr bool F = decltype(past)::value;
+        if (type == RFAST_F32) return yf ? go(rfast_route_combine_kernel<float, float, L, W, C, F>) : go(rfast_route_combine_kernel<float, u16, L, W, C, F>);
+        return yf ? go(rfast_route_combine_kernel<u16, float, L, W, C, F>) : go(rfast_route_combine_kernel<u16, u16, L, W, C, F>);
+      };
       if constexpr (L == 64) {
-        if (far) return yf ? go(rfast_route_combine_kernel<u16, float, L, W, C, true>) : go(rfast_route_combine_kernel<u16, u16, L, W, C, true>);
+        if (far) return types(std::true_type());
       }
-      return yf ? go(rfast_route_combine_kernel<u16, float, L, W, C, false>) : go(rfast_route_combine_kernel<u16, u16, L, W, C, false>);
+      return types(std::false_type());
     });
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return launch");
@@ -608,7 +621,7 @@ extern "C" int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, 
   if (const int bad = apart(in, 4, out, 2)) return bad;
   const Rows a = {sorted, place, weight, dy, writes ? dsorted : nullptr, dweight, ld_sorted, ld_dy, ld_dsorted, rows, k, d, sorted_rows};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const bool far = reads && is_far(sorted, pairs, ld_sorted, d, w);
+  const bool far = reads && is_far(sorted, 2 * pairs, ld_sorted, d, w);
   const hipError_t e = by_choices(k, [&](auto choices) {
     constexpr int C = decltype(choices)::value;
     const auto types = [&](auto lanes, auto whole) {
@@ -619,14 +632,13 @@ extern "C" int rfast_route_combine_backward(int32_t rows, int32_t k, int32_t d, 
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a);
         return hipGetLastError();
       };
-      if (type == RFAST_F32) return go(rfast_route_combine_back<float, L, W, C, false>);
       if constexpr (L >= 64) {
-        if (far) return go(rfast_route_combine_back<u16, L, W, C, true>);
+        if (far) return type == RFAST_F32 ? go(rfast_route_combine_back<float, L, W, C, true>) : go(rfast_route_combine_back<u16, L, W, C, true>);
       }
-      return go(rfast_route_combine_back<u16, L, W, C, false>);
+      return type == RFAST_F32 ? go(rfast_route_combine_back<float, L, W, C, false>) : go(rfast_route_combine_back<u16, L, W, C, false>);
     };
     if (d > 1024) return types(std::integral_constant<int, 256>(), std::true_type());  // (a wavefront alone would go round three times and more)
-    return by_lanes(d, types);
+    return by_lanes(d, 16 / w, types);
   });
   return e == hipSuccess ? RFAST_OK : rfast_refuse_hip(e, "return gradient launch");
 }
