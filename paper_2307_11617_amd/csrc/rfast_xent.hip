@@ -142,7 +142,7 @@ template <class OUT> __device__ inline void zero_row(OUT* grad, int K, int lane,
 
 // Element `at` (not below 0, less than 4 GB on) of a row that a wavefront's lanes share: one address of the row and 32 bits per lane.
 template <class T> __device__ inline T* near_by(T* row, int at) {
-  return (T*)((uintptr_t)row + (uint32_t)at * (uint32_t)sizeof(T));
+  return (T*)((const char*)row + (uint32_t)at * (uint32_t)sizeof(T));
 }
 
 // LANES lanes hold a row, GROUPS groups of logits each.  LANES <= 64: 256 / LANES rows per workgroup.
