@@ -208,45 +208,74 @@ __global__ void __launch_bounds__(kThreads) rfast_sort_place(Part a, int parts, 
 }
 
 // Up to kRankMost numbers without digits or passes: an element's place is how many numbers are smaller, or equal and before it.  A workgroup does that for
-// kRanked elements, 32 slices of all the numbers in LDS at a time: count^2 comparisons of two instructions.  1024 numbers take 3.8 us and 4096 take 6.4,
-// whatever their range (by passes in one workgroup 5 and 8 per digit, and more workgroups need launches); 8192 take 11, two passes 14 and one 6.
+// kRanked elements, 64 slices of all the numbers in LDS at a time: count^2 comparisons of two instructions.  1024 numbers take 3.9 us and 4096 take 6.1,
+// whatever their range (by passes in one workgroup 5 and 8 per digit, and more workgroups need launches); 8192 take 9.9 (one element to a lane 11), two
+// passes 14 and one 6.
 // What it writes to row_ptr, the place of the first element of each number, it counts as elements behind the others.
 __global__ void __launch_bounds__(kThreads) rfast_sort_rank(Part a, Beside beside) {
-  constexpr int SLICES = kThreads / kRanked;
+  constexpr int EACH = 2, LANES = kRanked / EACH, SLICES = kThreads / LANES;
   __shared__ int4 keys[kRankMost / 4];
-  __shared__ int32_t ranks[kRanked][SLICES + 1];
+  static_assert(LANES == 16, "a wavefront has four slices");
+  __shared__ int32_t ranks[kRanked][kWaves + 1];
   if ((int)blockIdx.x >= beside.blocks) return clear_beside(beside);
   int* const key = (int*)keys;
   const int groups = (a.count + 3) / 4;
-  for (int i = threadIdx.x; i < 4 * groups; i += kThreads) key[i] = i < a.count ? clip_key(a.key[i], a.keys) : 0x7fffffff;
+  for (int g = threadIdx.x; g < groups; g += kThreads) {
+    int4 q;
+    if (4 * g + 4 <= a.count) {
+      const any_u32x4 t = wide_load<any_u32x4, false>(a.key + 4 * g);
+      q = make_int4(clip_key(t.x, a.keys), clip_key(t.y, a.keys), clip_key(t.z, a.keys), clip_key(t.w, a.keys));
+    } else {
+      int k[4];
+      for (int j = 0; j < 4; ++j) k[j] = 4 * g + j < a.count ? clip_key(a.key[4 * g + j], a.keys) : 0x7fffffff;
+      q = make_int4(k[0], k[1], k[2], k[3]);
+    }
+    keys[g] = q;
+  }
   __syncthreads();
-  const int mine = threadIdx.x % kRanked, slice = threadIdx.x / kRanked, per = (groups + SLICES - 1) / SLICES;
-  const int64_t unit = (int64_t)blockIdx.x * kRanked + mine;
-  const bool element = unit < a.count;
-  const int index = element ? (int)unit : 0;
-  const uint32_t less = element ? (uint32_t)key[index] : (uint32_t)(unit - a.count), at_most = less + 1;  // (of row_ptr: no equal one is before)
-  const int lo = slice * per, hi = min(lo + per, groups), own = index / 4;
-  int32_t before = 0;
+  // EACH elements to a lane, so that what it reads of the others counts for both; slice s has the groups s, s + SLICES, ..: neighbouring
+  // slices, which a wavefront has, read neighbours
+  const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
+  uint32_t less[EACH], at_most[EACH];
+  int own[EACH];
+  int32_t before[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int64_t unit = (int64_t)blockIdx.x * kRanked + e * LANES + lane;
+    const bool element = unit < a.count;
+    less[e] = element ? (uint32_t)key[unit] : (uint32_t)(unit - a.count);
+    at_most[e] = less[e] + 1;
+    own[e] = element ? (int)unit / 4 : 0;  // (of row_ptr: no equal one is before)
+    before[e] = 0;
+    if (element && own[e] % SLICES == slice)
+      for (int i = 4 * own[e]; i < (int)unit; ++i) before[e] += (uint32_t)key[i] == less[e];
+  }
 #pragma unroll 4
-  for (int g = lo; g < hi; ++g) {
+  for (int g = slice; g < groups; g += SLICES) {
     const int4 q = keys[g];
-    const uint32_t bound = g < own ? at_most : less;
-    before += ((uint32_t)q.x < bound) + ((uint32_t)q.y < bound) + ((uint32_t)q.z < bound) + ((uint32_t)q.w < bound);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const uint32_t bound = g < own[e] ? at_most[e] : less[e];
+      before[e] += ((uint32_t)q.x < bound) + ((uint32_t)q.y < bound) + ((uint32_t)q.z < bound) + ((uint32_t)q.w < bound);
+    }
   }
-  if (element && own >= lo && own < hi) {
-    for (int i = 4 * own; i < index; ++i) before += (uint32_t)key[i] == less;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    before[e] += __shfl_xor(before[e], 16, 64);
+    before[e] += __shfl_xor(before[e], 32, 64);
+    if ((threadIdx.x & 63) < LANES) ranks[e * LANES + lane][threadIdx.x / 64] = before[e];
   }
-  ranks[mine][slice] = before;
   __syncthreads();
   if (threadIdx.x >= kRanked) return;
   int32_t to = 0;
 #pragma unroll
-  for (int i = 0; i < SLICES; ++i) to += ranks[mine][i];
-  if (element) {
-    const int32_t k = (int32_t)less;
+  for (int i = 0; i < kWaves; ++i) to += ranks[threadIdx.x][i];
+  const int64_t unit = (int64_t)blockIdx.x * kRanked + threadIdx.x;
+  if (unit < a.count) {
+    const int32_t k = key[unit];
     if (a.out_key) a.out_key[to] = k;
-    if (a.order) a.order[to] = k < a.keys ? index : -1;
-    if (a.place) a.place[index] = k < a.keys ? to : -1;
+    if (a.order) a.order[to] = k < a.keys ? (int32_t)unit : -1;
+    if (a.place) a.place[unit] = k < a.keys ? to : -1;
   } else if (a.row_ptr && unit - a.count <= a.keys) {
     a.row_ptr[unit - a.count] = to;
   }
